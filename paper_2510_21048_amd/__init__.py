@@ -16,3 +16,9 @@ from .binding import (  # noqa: F401
     BLOCK_DTYPE, RAW_EVENT_DTYPE, WINDOW_DTYPE, XMEM_PERSISTENT, attribute, lifecycles, orchestrate, xmem_attribute,
     xmem_lifecycles, xmem_orchestrate, xmem_prep_workspace_bytes,
 )
+from .ops import (  # noqa: F401
+    ACTIVATIONS, XMEM_BF16, XMEM_F16, XMEM_F32, XMEM_NS_MAX_STEPS, linear_backward, linear_forward, load_ops, muon_update,
+    ops_lib_path, policy_loss, token_logp,
+    xmem_linear_backward, xmem_linear_backward_workspace_bytes, xmem_linear_forward, xmem_linear_forward_workspace_bytes,
+    xmem_muon_update, xmem_muon_update_workspace_bytes, xmem_policy_loss, xmem_policy_loss_workspace_bytes,
+)

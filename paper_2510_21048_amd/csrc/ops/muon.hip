@@ -1,0 +1,280 @@
+// muon.hip -- momentum and the update orthogonalised by Newton-Schulz products, on MI355X (gfx950).
+//
+// X is kept as the caller's matrices lie: [long, short] where rows > cols, [short, long] else, so nothing is
+// transposed; the matrix product reads either layout.  With P = X X^T (short by short, symmetric) and
+// Q = b P + c P P, a step is X <- a X + Q X.
+//
+// Numbers.  The products take half-precision operands: 11 bits where bfloat16 has 8, and the range is no matter
+// since |X|_F <= 1 at the start and no singular value passes 1.3 afterwards; powers of two (kX for X, kP for P and Q) keep small
+// entries normal.  Three things hold the error near 7e-4 of the update (its bfloat16 rounding: 1.7e-3):
+//   - the diagonals of P and Q, which are far larger than the rest, are kept apart in 32 bits and the products take
+//     the matrices without them: (P P)_ij = (E E)_ij + (d_i + d_j) E_ij, and + d_i^2 on the diagonal;
+//   - the linear terms (a + q_ii) X_i take X from two halves of 11 bits, so that directions in which the
+//     gradient is weak, which a step multiplies by a, are not lost in the rounding of the strong ones;
+//   - Q is made from the same rounded P in both terms: b + 2 c p is near 0 where P is near 1, so that its error cancels.
+// On matrices of normal values the products alone, in bfloat16, leave 1e-2; in half precision without these, 1.5e-3;
+// where one direction holds most of a gradient, 1.6e-1 and 2e-2.
+#include "gemm.h"
+
+using namespace xops;
+
+namespace {
+
+constexpr float kX = 256.0f, kP = 1024.0f;
+constexpr float kNormEps = 1e-7f;
+constexpr int kThreads = 256;
+constexpr int kNormParts = 64;  // workgroups whose sums make one matrix's norm
+constexpr int64_t kMostCount = 65535, kMostSide = int64_t(1) << 24;
+
+struct Shape {
+  int64_t count, rows, cols, s, l;  // s <= l
+  int64_t lds, ldx;                 // row lengths of P, Q and of X, padded to 8
+  bool tall;                        // rows > cols: X lies as [l, s]
+};
+Shape shape_of(int64_t count, int64_t rows, int64_t cols) {
+  Shape h{count, rows, cols, rows < cols ? rows : cols, rows < cols ? cols : rows, 0, 0, rows > cols};
+  h.lds = (h.s + 7) & ~int64_t(7);
+  h.ldx = (cols + 7) & ~int64_t(7);
+  return h;
+}
+
+struct Ws {
+  f16 *x[2], *lo[2];  // X and its second half, before and after a step
+  f16 *p, *q;
+  float *dp, *dq;  // diagonals
+  double* part;
+  size_t bytes;
+};
+Ws carve(void* base, const Shape& h) {
+  Ws w;
+  char* at = static_cast<char*>(base);
+  const auto take = [&](size_t b) {
+    char* r = at;
+    at += up256(b);
+    return r;
+  };
+  const size_t nx = size_t(h.count) * h.rows * h.ldx * 2, np = size_t(h.count) * h.s * h.lds * 2;
+  for (int i = 0; i < 2; ++i) {
+    w.x[i] = reinterpret_cast<f16*>(take(nx));
+    w.lo[i] = reinterpret_cast<f16*>(take(nx));
+  }
+  w.p = reinterpret_cast<f16*>(take(np));
+  w.q = reinterpret_cast<f16*>(take(np));
+  w.dp = reinterpret_cast<float*>(take(size_t(h.count) * h.s * 4));
+  w.dq = reinterpret_cast<float*>(take(size_t(h.count) * h.s * 4));
+  w.part = reinterpret_cast<double*>(take(size_t(h.count) * kNormParts * 8));
+  w.bytes = size_t(at - static_cast<char*>(base));
+  return w;
+}
+
+// m <- mu m + g, and the squares of u summed in 64 bits (a matrix may have 2^48 entries of any size).
+template <class G>
+__global__ __launch_bounds__(kThreads) void k_momentum(const G* g, float* mom, int64_t per, float mu, bool nesterov, double* part) {
+  __shared__ double sums[kThreads / kWave];
+  const int64_t base = int64_t(blockIdx.y) * per;
+  double sum = 0.0;
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < per; i += int64_t(kNormParts) * kThreads) {
+    const float gi = float(g[base + i]), m = mu * mom[base + i] + gi;
+    mom[base + i] = m;
+    const double u = nesterov ? gi + mu * m : m;
+    sum += u * u;
+  }
+  sum = wave_sum(sum);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double v = 0.0;
+    for (int i = 0; i < kThreads / kWave; ++i) v += sums[i];
+    part[blockIdx.y * kNormParts + blockIdx.x] = v;
+  }
+}
+
+// X = u / (|u| + eps) in two halves; the columns that pad a row are 0.
+template <class G>
+__global__ __launch_bounds__(kThreads) void k_start(const G* g, const float* mom, int64_t rows, int64_t cols, int64_t ldx, float mu,
+                                                    bool nesterov, const double* part, f16* x, f16* lo) {
+  const int64_t b = blockIdx.y;
+  double v = part[b * kNormParts + (threadIdx.x & 63)];
+  v = wave_sum(v);
+  const float inv = kX / (float(sqrt(v)) + kNormEps);
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows * ldx; i += int64_t(gridDim.x) * kThreads) {
+    const int64_t r = i / ldx, c = i % ldx;
+    float e = 0.0f;
+    if (c < cols) {
+      const int64_t at = (b * rows + r) * cols + c;
+      const float m = mom[at];
+      e = (nesterov ? float(g[at]) + mu * m : m) * inv;
+    }
+    const f16 hi = f16(e);
+    x[b * rows * ldx + i] = hi;
+    lo[b * rows * ldx + i] = f16(e - float(hi));
+  }
+}
+
+// P = X X^T without its diagonal, which goes to d.  Only tiles on or below the diagonal are computed, and each
+// entry below it is written to its mirrored place too.
+struct GramEpilogue {
+  static constexpr bool kSymmetric = true;
+  f16* p;
+  float* d;
+  int64_t ld;
+
+  __device__ void operator()(int64_t m, int64_t n, f32x4 v, int z, int64_t ms, int64_t ns) const {
+    if (m >= ms) return;
+    f16* to = p + z * ms * ld;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (n + j > m || n + j >= ns) continue;
+      const float e = v[j] * (1.0f / (kX * kX));
+      if (n + j == m) d[z * ms + m] = e;
+      const f16 h = n + j == m ? f16(0.0f) : f16(e * kP);
+      to[m * ld + n + j] = h;
+      to[(n + j) * ld + m] = h;
+    }
+  }
+};
+
+// Q = b P + c P P without its diagonal.
+struct PolyEpilogue {
+  static constexpr bool kSymmetric = true;
+  const f16* p;
+  const float* dp;
+  f16* q;
+  float* dq;
+  int64_t ld;
+
+  __device__ void operator()(int64_t m, int64_t n, f32x4 v, int z, int64_t ms, int64_t ns) const {
+    if (m >= ms) return;
+    const f16* from = p + z * ms * ld;
+    f16* to = q + z * ms * ld;
+    const float dm = dp[z * ms + m];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (n + j > m || n + j >= ns) continue;
+      const float ee = v[j] * (1.0f / (kP * kP));
+      if (n + j == m) {
+        dq[z * ms + m] = XMEM_NS_B * dm + XMEM_NS_C * (ee + dm * dm);
+        to[m * ld + m] = f16(0.0f);
+      } else {
+        const float e = float(from[m * ld + n + j]) * (1.0f / kP), dn = dp[z * ms + n + j];
+        const f16 h = f16((XMEM_NS_B * e + XMEM_NS_C * (ee + (dm + dn) * e)) * kP);
+        to[m * ld + n + j] = h;
+        to[(n + j) * ld + m] = h;
+      }
+    }
+  }
+};
+
+// X <- (a + q_ii) X_i + (Q X)_i.  The diagonal's index is the row where X lies as [s, l], the column else.
+template <bool TALL>
+struct StepEpilogue {
+  static constexpr bool kSymmetric = false;
+  const f16 *x, *lo;
+  const float* dq;
+  f16 *nx, *nlo;
+  int64_t ld, s;
+  bf16* out;  // the last step writes the update instead
+  float scale;
+
+  __device__ void operator()(int64_t m, int64_t n, f32x4 v, int z, int64_t ms, int64_t ns) const {
+    if (m >= ms) return;
+    const int64_t row = (z * ms + m) * ld;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (n + j >= ns) continue;
+      const float d = XMEM_NS_A + dq[z * s + (TALL ? n + j : m)];
+      const float e = (d * (float(x[row + n + j]) + float(lo[row + n + j])) + v[j] * (1.0f / kP));  // times kX
+      if (out) {
+        out[(z * ms + m) * ns + n + j] = bf16(e * (scale / kX));
+      } else {
+        const f16 hi = f16(e);
+        nx[row + n + j] = hi;
+        nlo[row + n + j] = f16(e - float(hi));
+      }
+    }
+  }
+};
+
+__global__ __launch_bounds__(kThreads) void k_scaled(const f16* x, const f16* lo, int64_t rows, int64_t cols, int64_t ldx, float scale,
+                                                     bf16* out) {
+  const int64_t b = blockIdx.y;
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows * cols; i += int64_t(gridDim.x) * kThreads) {
+    const int64_t at = b * rows * ldx + i / cols * ldx + i % cols;
+    out[b * rows * cols + i] = bf16((float(x[at]) + float(lo[at])) * (scale / kX));
+  }
+}
+
+unsigned blocks_of(int64_t n) {
+  const int64_t b = (n + kThreads - 1) / kThreads;
+  return unsigned(b < 1 ? 1 : b > 4096 ? 4096 : b);
+}
+
+template <class G>
+int update(const G* g, float* mom, const Shape& h, float mu, bool nesterov, int steps, float scale, bf16* out, void* base,
+           hipStream_t st) {
+  Ws w = carve(base, h);
+  const int64_t per = h.rows * h.cols;
+  const unsigned z = unsigned(h.count);
+  k_momentum<G><<<dim3(kNormParts, z), kThreads, 0, st>>>(g, mom, per, mu, nesterov, w.part);
+  k_start<G><<<dim3(blocks_of(h.rows * h.ldx), z), kThreads, 0, st>>>(g, mom, h.rows, h.cols, h.ldx, mu, nesterov, w.part, w.x[0],
+                                                                   w.lo[0]);
+  int rc = launched();
+  if (steps == 0) {
+    k_scaled<<<dim3(blocks_of(per), z), kThreads, 0, st>>>(w.x[0], w.lo[0], h.rows, h.cols, h.ldx, scale, out);
+    return launched();
+  }
+  const int64_t sx = h.rows * h.ldx, sp = h.s * h.lds;
+  for (int i = 0; i < steps && rc == XMEM_OK; ++i) {
+    const f16 *x = w.x[i & 1], *lo = w.lo[i & 1];
+    bf16* to = i == steps - 1 ? out : nullptr;
+    GemmArgs gram{x, x, h.ldx, h.ldx, sx, sx, h.s, h.s, h.l, 0, 0};
+    GemmArgs poly{w.p, w.p, h.lds, h.lds, sp, sp, h.s, h.s, h.s, 0, 0};
+    const GramEpilogue ge{w.p, w.dp, h.lds};
+    const PolyEpilogue pe{w.p, w.dp, w.q, w.dq, h.lds};
+    rc = h.tall ? gemm<f16, false, false>(gram, ge, h.count, st) : gemm<f16, true, true>(gram, ge, h.count, st);
+    if (rc == XMEM_OK) rc = gemm<f16, true, true>(poly, pe, h.count, st);
+    if (rc != XMEM_OK) break;
+    if (h.tall) {
+      GemmArgs step{x, w.q, h.ldx, h.lds, sx, sp, h.l, h.s, h.s, 0, 0};
+      rc = gemm<f16, true, true>(step, StepEpilogue<true>{x, lo, w.dq, w.x[~i & 1], w.lo[~i & 1], h.ldx, h.s, to, scale}, h.count, st);
+    } else {
+      GemmArgs step{w.q, x, h.lds, h.ldx, sp, sx, h.s, h.l, h.s, 0, 0};
+      rc = gemm<f16, true, false>(step, StepEpilogue<false>{x, lo, w.dq, w.x[~i & 1], w.lo[~i & 1], h.ldx, h.s, to, scale}, h.count, st);
+    }
+  }
+  return rc;
+}
+
+bool sizes_ok(int64_t count, int64_t rows, int64_t cols) {
+  return count >= 0 && count <= kMostCount && rows >= 0 && cols >= 0 && rows < kMostSide && cols < kMostSide &&
+         ((rows + 127) / 128) * ((cols + 127) / 128) < (int64_t(1) << 31) &&
+         rows * cols < (int64_t(1) << 40);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t xmem_muon_update_workspace_bytes(int64_t count, int64_t rows, int64_t cols) {
+  if (!sizes_ok(count, rows, cols) || count == 0 || rows == 0 || cols == 0) return 0;
+  return carve(nullptr, shape_of(count, rows, cols)).bytes;
+}
+
+int xmem_muon_update(const void* d_grad, int grad_dtype, float* d_momentum, int64_t count, int64_t rows, int64_t cols,
+                     float mu, int nesterov, int steps, float scale, void* d_update, void* d_workspace,
+                     size_t workspace_bytes, void* hip_stream) {
+  if (!sizes_ok(count, rows, cols) || grad_dtype < XMEM_BF16 || grad_dtype > XMEM_F32 || steps < 0 || steps > XMEM_NS_MAX_STEPS)
+    return XMEM_EINVAL;
+  if (count == 0 || rows == 0 || cols == 0) return XMEM_OK;
+  if (!d_grad || !d_momentum || !d_update) return XMEM_EINVAL;
+  const Shape h = shape_of(count, rows, cols);
+  if (!d_workspace || workspace_bytes < xmem_muon_update_workspace_bytes(count, rows, cols) || !aligned(d_workspace, 256))
+    return XMEM_EWORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  bf16* out = static_cast<bf16*>(d_update);
+  if (grad_dtype == XMEM_BF16) return update(static_cast<const bf16*>(d_grad), d_momentum, h, mu, nesterov, steps, scale, out, d_workspace, st);
+  if (grad_dtype == XMEM_F16) return update(static_cast<const f16*>(d_grad), d_momentum, h, mu, nesterov, steps, scale, out, d_workspace, st);
+  return update(static_cast<const float*>(d_grad), d_momentum, h, mu, nesterov, steps, scale, out, d_workspace, st);
+}
+
+}  // extern "C"
