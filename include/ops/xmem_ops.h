@@ -56,7 +56,7 @@ size_t xmem_linear_forward_workspace_bytes(int64_t m, int64_t n, int64_t k);
  *                of an activation
  *   d_workspace: >= xmem_linear_forward_workspace_bytes(m, n, k), 256-byte aligned
  * k == 0 gives z = b.  No output may overlap another operand (d_residual apart).
- * Returns XMEM_OK, XMEM_EINVAL (null pointer, negative or too large size, ld too
+ * Returns XMEM_OK, XMEM_EINVAL (null pointer, negative or too large size (2^30 and more), ld too
  * small, unknown dtype or activation), XMEM_EWORKSPACE or XMEM_EHIP. */
 int xmem_linear_forward(const void* d_x, int64_t ldx, const void* d_w, int64_t ldw, const float* d_bias,
                         const void* d_residual, int64_t ldr, int64_t m, int64_t n, int64_t k, int dtype,

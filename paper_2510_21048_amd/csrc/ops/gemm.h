@@ -2,7 +2,7 @@
 // 16-bit operands, 32-bit sums on the matrix cores, and an epilogue that sees each sum once.
 //
 // Either operand may lie with k contiguous (A[m * ld + k]) or with its rows contiguous (A[k * ld + m]), so
-// the three products of a linear layer (x w^T, dz w, dz^T x) need no transposed copy.
+// the three products of a linear layer (x w^T, dz w, dz^T x) and of a Newton-Schulz step need no transposed copy.
 #pragma once
 #include "common.h"
 
@@ -14,35 +14,50 @@ struct GemmArgs {
   const void* a;
   const void* b;
   int64_t lda, ldb;
-  int64_t stride_a, stride_b;  // between the matrices of a batch (grid z), in elements
+  int64_t stride_a, stride_b;  // between the matrices of a batch, in elements
   int64_t m, n, k;
-  int tiles_m, tiles_n;
+  // the operand's storage holds whole rows of ld, a multiple of 8, and what pads a row is 0
+  bool pad_a = false, pad_b = false;
+  int64_t count = 1;
+  // set by the launch
+  int tiles_m = 0, tiles_n = 0, tiles = 0, splits = 1, span = 0;  // span: k tiles of a split
+  float* part = nullptr;
+};
+
+// A workgroup's tile and its wavefronts: WM by WN of them, each with BM / WM by BN / WN of the tile.
+template <int BM_, int BN_, int WM_, int WN_>
+struct Config {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, FM = BM / WM / 16, FN = BN / WN / 16, THREADS = 64 * WM * WN;
 };
 
 // One operand tile in LDS: R rows of kBK.  Chunks of 16 bytes are kept at swizzled places, so that the 16 lanes
 // that read one column of chunks meet 16 different bank groups.
 //   k contiguous:    [row][8 chunks of k],   chunk c at c ^ ((row >> 1) & 7)
 //   rows contiguous: [k][R / 8 chunks of rows], pairs of chunks (the 16 rows of one product) at p ^ h(k)
-template <class T, int R, bool KC>
+// PERM (k contiguous only): of each strip of 32 rows, place 16 t + 4 g + r holds row 8 g + 4 t + r.  A matrix
+// instruction leaves a lane group g the rows 4 g + r of its product, so with two products it has 8 neighbours, and
+// the epilogue moves 16 bytes a lane, 64 next to each other.
+template <class T, int R, bool KC, bool PERM>
 struct Tile {
   typedef typename Vec<T>::x8 x8;
   static constexpr int kBytes = R * kBK * 2;
   static constexpr int kChunks = R * kBK / 8;
 
   __device__ static int pair_hash(int k) { return ((k & 3) | ((k >> 1) & 4)) & (R / 16 - 1); }
-  // the row (or rows) and k of the chunk kept at place i
+  // the row (or first of eight rows) and the k (or first of eight) of the chunk kept at place i
   __device__ static void at(int i, int& row, int& k) {
     if constexpr (KC) {
-      row = i >> 3;
-      k = ((i & 7) ^ ((row >> 1) & 7)) * 8;
+      const int r = i >> 3;
+      k = ((i & 7) ^ ((r >> 1) & 7)) * 8;
+      row = PERM ? (r & ~31) + 8 * ((r >> 2) & 3) + 4 * ((r >> 4) & 1) + (r & 3) : r;
     } else {
       k = i / (R / 8);
       const int c = i % (R / 8);
       row = (((c >> 1) ^ pair_hash(k)) * 2 + (c & 1)) * 8;
     }
   }
-  // the operand of a 16x16x32 product: rows r0..r0+15 (r0 a multiple of 16), step s of the tile's k.
-  // Lane l holds row l % 16, k = 32 s + 8 (l / 16) + 0..7.
+  // the operand of a 16x16x32 product: places r0..r0+15 (r0 a multiple of 16), step s of the tile's k.
+  // Lane l holds place l % 16, k = 32 s + 8 (l / 16) + 0..7.
   __device__ static x8 frag(const char* t, int r0, int s, int lane) {
     if constexpr (KC) {
       const int row = r0 + (lane & 15), c = 4 * s + (lane >> 4);
@@ -70,132 +85,402 @@ __device__ inline f32x4 mfma(Vec<f16>::x8 a, Vec<f16>::x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// Eight elements from p, of which only those below `valid` exist (the others are 0).
-template <class T>
-__device__ inline u32x4 load8(const T* p, int64_t valid) {
-  u32x4 v = {0, 0, 0, 0};
-  if (valid >= 8) {
-    __builtin_memcpy(&v, p, 16);
-  } else if (valid > 0) {
-    T e[8];
+// A buffer load past num_records gives zeros, whose LDS place is written all the same.
+constexpr unsigned kNowhere = 0x80000000u;
+
+// One operand's loads straight from memory into LDS, 16 bytes a lane, for 16-byte aligned operands whose ld is a
+// multiple of 8, and whose contiguous side is one or padded to one.  The swizzle is in which chunk a lane fetches.
+template <class T, class Ti, int R, bool KC, int THREADS>
+struct Direct {
+  static constexpr int kLoads = Ti::kChunks / THREADS;
+  unsigned off[kLoads];
+  int kk;  // KC: the k of this lane's chunks within the tile
+
+  __device__ void init(const T*, int64_t ld, int64_t r0, int64_t rows, int) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = j < valid ? p[j] : T(0.0f);
-    __builtin_memcpy(&v, e, 16);
+    for (int j = 0; j < kLoads; ++j) {
+      int row, k;
+      Ti::at(j * THREADS + threadIdx.x, row, k);
+      off[j] = KC ? unsigned(row) * unsigned(ld * 2) + k * 2 : unsigned(k) * unsigned(ld * 2) + row * 2;
+      if (!KC && r0 + row >= rows) off[j] = kNowhere;
+      if (KC) kk = k;  // the same for every j: a pass of THREADS chunks is a multiple of 16 rows
+    }
   }
+  // tile t of the operand; past the last one it only clears LDS.  ld < 2^21, so that a tile's bytes fit 31 bits.
+  __device__ void issue(char* lds, const T* p, int64_t ld, int64_t r0, int64_t rows, int t, int ks, int wave) const {
+    const int k0 = t * kBK, left = ks - k0, step = int(ld);
+    const T* base = KC ? p + r0 * ld + k0 : p + k0 * ld + r0;
+    const int high = KC ? (rows - r0 < R ? int(rows - r0) : R) : (left < kBK ? left : kBK);
+    const int wide = ((KC ? left : int(rows - r0)) + 7) & ~7;
+    int bytes = ((high - 1) * step + wide) * 2;
+    bytes = left > 0 ? bytes : 0;
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, bytes, 0x00020000);
+    const bool out = KC && kk >= left;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + (j * THREADS + wave * 64) * 16),
+                                               16, out ? kNowhere : off[j], 0, 0, 0);
+  }
+};
+
+// v >> 16 s bits as one number of 128 bits, s = 0..8: the elements past the end of a row, dropped.
+__device__ inline u32x4 drop(u32x4 v, int s) {
+  if (s & 1) {
+    v[0] = (v[0] >> 16) | (v[1] << 16);
+    v[1] = (v[1] >> 16) | (v[2] << 16);
+    v[2] = (v[2] >> 16) | (v[3] << 16);
+    v[3] >>= 16;
+  }
+  if (s & 2) v = u32x4{v[1], v[2], v[3], 0};
+  if (s & 4) v = u32x4{v[2], v[3], 0, 0};
+  if (s & 8) v = u32x4{0, 0, 0, 0};
   return v;
 }
 
-// Loads one tile through registers, for operands of any alignment; rows and k past the matrix are 0.
-template <class T, int R, bool KC, int THREADS>
-__device__ inline void stage(char* lds, const T* p, int64_t ld, int64_t r0, int64_t rows, int64_t k0, int64_t ks) {
-  typedef Tile<T, R, KC> Ti;
+// One operand's loads through registers, for rows of any alignment.  A chunk that passes the end of its row is read
+// from further back, so that it ends there, and shifted: every load is 16 bytes and inside the matrix, none is
+// behind a branch.  Rows shorter than 8 elements are read one by one.
+template <class T, class Ti, int R, bool KC, int THREADS>
+struct Staged {
+  static constexpr int kLoads = Ti::kChunks / THREADS;
+  u32x4 v[kLoads];
+
+  __device__ void load(const T* p, int64_t ld, int64_t r0, int64_t rows, int t, int ks) {
+    const int64_t k0 = int64_t(t) * kBK;
+    const int64_t length = KC ? ks : rows;  // of the contiguous side
+    const bool inside = r0 + R <= rows && k0 + kBK <= ks;
 #pragma unroll
-  for (int j = 0; j < Ti::kChunks / THREADS; ++j) {
-    const int i = j * THREADS + threadIdx.x;
-    int row, k;
-    Ti::at(i, row, k);
-    const int64_t gr = r0 + row, gk = k0 + k;
-    u32x4 v = {0, 0, 0, 0};
-    if (gr < rows && gk < ks) v = KC ? load8(p + gr * ld + gk, ks - gk) : load8(p + gk * ld + gr, rows - gr);
-    *reinterpret_cast<u32x4*>(lds + i * 16) = v;
+    for (int j = 0; j < kLoads; ++j) {
+      int row, k;
+      Ti::at(j * THREADS + threadIdx.x, row, k);
+      const int64_t gr = r0 + row, gk = k0 + k;
+      if (inside) {
+        __builtin_memcpy(&v[j], KC ? p + gr * ld + gk : p + gk * ld + gr, 16);
+        continue;
+      }
+      const int64_t along = KC ? gk : gr, across = KC ? gr : gk, last = (KC ? rows : int64_t(ks)) - 1;
+      const int64_t valid = across <= last ? length - along : 0;
+      const T* line = p + (across <= last ? across : last) * ld;
+      if (length >= 8) {
+        const int s = valid >= 8 ? 0 : valid <= 0 ? 8 : int(8 - valid);
+        u32x4 e;
+        __builtin_memcpy(&e, line + (s == 8 ? 0 : along - s), 16);
+        v[j] = drop(e, s);
+      } else {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < valid ? line[along + i] : T(0.0f);
+        __builtin_memcpy(&v[j], e, 16);
+      }
+    }
+  }
+  __device__ void store(char* lds) const {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(lds + (j * THREADS + threadIdx.x) * 16) = v[j];
+  }
+};
+
+// Lays half a tile's work out for the compiler's scheduler: LOADS memory loads, then READS LDS reads (in that order,
+// which is the program's), spread among PRODUCTS matrix instructions; nothing moves past the end.
+template <int LOADS, int READS, int PRODUCTS>
+struct Order {
+  static constexpr int kEach = PRODUCTS * 7 / 8 / (LOADS + READS) > 0 ? PRODUCTS * 7 / 8 / (LOADS + READS) : 1;
+  template <int I>
+  __device__ static __attribute__((always_inline)) void slot() {
+    if constexpr (I < LOADS + READS) {
+      __builtin_amdgcn_sched_group_barrier(I < LOADS ? 0x20 : 0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, kEach, 0);
+      slot<I + 1>();
+    }
+  }
+  __device__ static __attribute__((always_inline)) void apply() {
+    slot<0>();
+    __builtin_amdgcn_sched_group_barrier(0x8, PRODUCTS, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+// Workgroups are dealt to the XCDs in turn: give each XCD a run of neighbouring tiles.
+__device__ inline int run_of(int id, int total) {
+  const int per = total / kXcds, rest = total % kXcds, x = id % kXcds;
+  return x * per + (x < rest ? x : rest) + id / kXcds;
+}
+
+// Tile number -> tile: in groups of 8 tile rows, so that what an XCD works on at one time shares operand rows in its
+// L2; of a symmetric product only the tiles on and below the diagonal, row by row.
+template <bool SYMMETRIC>
+__device__ inline void tile_of(int id, const GemmArgs& g, int& tm, int& tn) {
+  if constexpr (SYMMETRIC) {
+    tm = int((__builtin_sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.5f);
+    while ((tm + 1) * (tm + 2) / 2 <= id) ++tm;
+    while (tm * (tm + 1) / 2 > id) --tm;
+    tn = id - tm * (tm + 1) / 2;
+  } else {
+    const int group = 8 * g.tiles_n, first = id / group * 8, high = g.tiles_m - first < 8 ? g.tiles_m - first : 8;
+    tm = first + id % group % high;
+    tn = id % group / high;
   }
 }
 
-// Workgroups are dealt to the XCDs in turn: give each XCD a run of neighbouring tiles, and walk the tiles in
-// groups of 8 tile rows, so that what an XCD works on at one time shares operand rows in its L2.
-__device__ inline void tile_of(int id, int tiles_m, int tiles_n, int& tm, int& tn) {
-  const int total = tiles_m * tiles_n, per = total / kXcds, rest = total % kXcds;
-  const int x = id % kXcds, i = id / kXcds;
-  id = x * per + (x < rest ? x : rest) + i;
-  const int group = 8 * tiles_n, g = id / group, first = g * 8;
-  const int high = tiles_m - first < 8 ? tiles_m - first : 8;
-  tm = first + (id - g * group) % high;
-  tn = (id - g * group) / high;
+// What a lane has of a tile: FN products' four neighbours each, of FM rows.  The epilogue takes them W at a time.
+template <class C, bool PERM, class Epi>
+__device__ inline void finish(const f32x4 (&acc)[C::FM][C::FN], const Epi& epi, int64_t m0, int64_t n0, int z, const GemmArgs& g) {
+  constexpr int W = PERM ? 8 : 4, GROUPS = C::FN * 4 / W;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t mw = m0 + (wave / C::WN) * (C::BM / C::WM) + (lane & 15);
+  const int64_t nw = n0 + (wave % C::WN) * (C::BN / C::WN) + (lane >> 4) * W;
+  const bool full = m0 + C::BM <= g.m && n0 + C::BN <= g.n;
+#pragma unroll
+  for (int q = 0; q < GROUPS; ++q) {
+    const int64_t n = nw + q * 4 * W;
+    const int valid = full || g.n - n >= W ? W : g.n > n ? int(g.n - n) : 0;
+    const auto col = epi.template column<W>(n, valid, z, g);
+#pragma unroll
+    for (int i = 0; i < C::FM; ++i) {
+      float v[W];
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[j] = acc[i][q * (W / 4) + j / 4][j & 3];
+      const int64_t m = mw + 16 * i;
+      if (full || (m < g.m && valid > 0)) epi.template row<W>(m, n, v, valid, col, z, g);
+    }
+  }
 }
 
-// THREADS = 64 WM WN; each wavefront sums BM / WM by BN / WN.  The n side is the first operand of the matrix
-// instruction, so that a lane ends with four neighbouring n of one m and the epilogue reads and writes 8 bytes.
-template <class T, int BM, int BN, int WM, int WN, bool AKC, bool BKC, class Epi>
-__global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
-  typedef Tile<T, BM, AKC> TA;
-  typedef Tile<T, BN, BKC> TB;
-  constexpr int FM = BM / WM / 16, FN = BN / WN / 16, THREADS = 64 * WM * WN;
-  __shared__ __attribute__((aligned(1024))) char lds[TA::kBytes + TB::kBytes];
-  int tm, tn;
-  tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
-  if (Epi::kSymmetric && tm < tn) return;
-  const int z = blockIdx.z;
+// out += over this workgroup's k tiles.  Two LDS buffers, and half a tile's operands in registers ahead of the matrix
+// instructions: while the products of one half run, the other half's LDS reads are under way; one barrier a tile,
+// after which the tile just read is overwritten by the loads of the tile after next (direct) or the next tile,
+// which was loaded while the first half ran, is complete (staged).
+// The n side is the first operand of the matrix instruction, so that a lane ends with neighbouring n of one m.
+template <class T, class C, bool AKC, bool BKC, bool DIRECT, class Epi>
+__global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
+#ifdef __HIP_DEVICE_COMPILE__  // the host's pass knows no buffer resources, and wants the kernel's name only
+  constexpr int FM = C::FM, FN = C::FN;
+  constexpr bool PERM = BKC && FN % 2 == 0;
+  typedef Tile<T, C::BM, AKC, false> TA;
+  typedef Tile<T, C::BN, BKC, PERM> TB;
+  constexpr int BUF = TA::kBytes + TB::kBytes, kReads = FM * (AKC ? 1 : 2) + FN * (BKC ? 1 : 2);
+  typedef typename Vec<T>::x8 x8;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * BUF];
+  int id = run_of(blockIdx.x, gridDim.x), tm, tn;
+  const int z = id / (g.tiles * g.splits);
+  id -= z * g.tiles * g.splits;
+  const int split = id / g.tiles, tile = id % g.tiles;
+  tile_of<Epi::kSymmetric>(tile, g, tm, tn);
   const T* a = static_cast<const T*>(g.a) + z * g.stride_a;
   const T* b = static_cast<const T*>(g.b) + z * g.stride_b;
-  const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  const int64_t m0 = int64_t(tm) * C::BM, n0 = int64_t(tn) * C::BN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / C::WN) * (C::BM / C::WM), wn = (wave % C::WN) * (C::BN / C::WN);
+  const int t0 = split * g.span, ks = int(g.k) < (t0 + g.span) * kBK ? int(g.k) : (t0 + g.span) * kBK;
+  const int t1 = (ks + kBK - 1) / kBK;
   f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = {0, 0, 0, 0};
-  for (int64_t k0 = 0; k0 < g.k; k0 += kBK) {
-    stage<T, BM, AKC, THREADS>(lds, a, g.lda, m0, g.m, k0, g.k);
-    stage<T, BN, BKC, THREADS>(lds + TA::kBytes, b, g.ldb, n0, g.n, k0, g.k);
-    __syncthreads();
+  x8 a0[FM], b0[FN], a1[FM], b1[FN];
+  const auto read = [&](x8(&fa)[FM], x8(&fb)[FN], int t, int s) {
+    const char* from = lds + (t & 1) * BUF;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      typename Vec<T>::x8 fa[FM], fb[FN];
+    for (int j = 0; j < FN; ++j) fb[j] = TB::frag(from + TA::kBytes, wn + 16 * j, s, lane);
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = TA::frag(lds, wm + 16 * i, s, lane);
+    for (int i = 0; i < FM; ++i) fa[i] = TA::frag(from, wm + 16 * i, s, lane);
+  };
+  const auto multiply = [&](const x8(&fa)[FM], const x8(&fb)[FN]) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = TB::frag(lds + TA::kBytes, wn + 16 * j, s, lane);
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mfma(fb[j], fa[i], acc[i][j]);
+      for (int j = 0; j < FN; ++j) acc[i][j] = mfma(fb[j], fa[i], acc[i][j]);
+  };
+  if constexpr (DIRECT) {
+    Direct<T, TA, C::BM, AKC, C::THREADS> la;
+    Direct<T, TB, C::BN, BKC, C::THREADS> lb;
+    la.init(a, g.lda, m0, g.m, ks);
+    lb.init(b, g.ldb, n0, g.n, ks);
+    const auto fetch = [&](int t) {
+      char* to = lds + (t & 1) * BUF;
+      la.issue(to, a, g.lda, m0, g.m, t, ks, wave);
+      lb.issue(to + TA::kBytes, b, g.ldb, n0, g.n, t, ks, wave);
+    };
+    if (t0 < t1) {
+      fetch(t0);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      fetch(t0 + 1);
+      read(a0, b0, t0, 0);
+      for (int t = t0; t < t1; ++t) {
+        read(a1, b1, t, 1);
+        multiply(a0, b0);
+        Order<0, kReads, FM * FN>::apply();
+        // every read of this tile is done, and the next tile has come
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(t + 2);
+        read(a0, b0, t + 1, 0);
+        multiply(a1, b1);
+        Order<la.kLoads + lb.kLoads, kReads, FM * FN>::apply();
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    __syncthreads();
+  } else {
+    Staged<T, TA, C::BM, AKC, C::THREADS> la;
+    Staged<T, TB, C::BN, BKC, C::THREADS> lb;
+    const auto load = [&](int t) {
+      la.load(a, g.lda, m0, g.m, t, ks);
+      lb.load(b, g.ldb, n0, g.n, t, ks);
+    };
+    const auto store = [&](int t) {
+      char* to = lds + (t & 1) * BUF;
+      la.store(to);
+      lb.store(to + TA::kBytes);
+    };
+    if (t0 < t1) {
+      load(t0);
+      store(t0);
+      __syncthreads();
+      read(a0, b0, t0, 0);
+      for (int t = t0; t < t1; ++t) {
+        if (t + 1 < t1) load(t + 1);
+        read(a1, b1, t, 1);
+        multiply(a0, b0);
+        if (t + 1 < t1) store(t + 1);
+        __syncthreads();
+        if (t + 1 < t1) read(a0, b0, t + 1, 0);
+        multiply(a1, b1);
+      }
+    }
   }
+  if (g.splits > 1) {
+    f32x4* to = reinterpret_cast<f32x4*>(g.part) + ((int64_t(z) * g.tiles + tile) * g.splits + split) * (FM * FN * C::THREADS) + threadIdx.x;
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
-      epi(m0 + wm + 16 * i + (lane & 15), n0 + wn + 16 * j + 4 * (lane >> 4), acc[i][j], z, g.m, g.n);
+      for (int j = 0; j < FN; ++j) to[(i * FN + j) * C::THREADS] = acc[i][j];
+    return;
+  }
+  finish<C, PERM>(acc, epi, m0, n0, z, g);
+#endif
 }
 
-template <class T, bool AKC, bool BKC, class Epi>
-int gemm(GemmArgs g, const Epi& epi, int64_t count, hipStream_t st) {
-  if (g.m <= 0 || g.n <= 0 || count <= 0) return XMEM_OK;
-  g.tiles_m = int((g.m + 127) / 128);
-  g.tiles_n = int((g.n + 127) / 128);
-  k_gemm<T, 128, 128, 2, 2, AKC, BKC, Epi><<<dim3(unsigned(g.tiles_m) * g.tiles_n, 1, unsigned(count)), 256, 0, st>>>(g, epi);
+// The splits of a product, added in their order, and its epilogue: one workgroup a tile, its lanes as in k_gemm.
+template <class C, bool BKC, class Epi>
+__global__ __launch_bounds__(C::THREADS) void k_join(GemmArgs g, Epi epi) {
+  int tm, tn;
+  const int z = blockIdx.x / g.tiles, tile = blockIdx.x % g.tiles;
+  tile_of<Epi::kSymmetric>(tile, g, tm, tn);
+  const f32x4* from =
+      reinterpret_cast<const f32x4*>(g.part) + (int64_t(z) * g.tiles + tile) * g.splits * (C::FM * C::FN * C::THREADS) + threadIdx.x;
+  f32x4 acc[C::FM][C::FN];
+#pragma unroll
+  for (int i = 0; i < C::FM; ++i)
+#pragma unroll
+    for (int j = 0; j < C::FN; ++j) acc[i][j] = from[(i * C::FN + j) * C::THREADS];
+  for (int s = 1; s < g.splits; ++s) {
+    from += C::FM * C::FN * C::THREADS;
+#pragma unroll
+    for (int i = 0; i < C::FM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::FN; ++j) acc[i][j] += from[(i * C::FN + j) * C::THREADS];
+  }
+  finish<C, BKC && C::FN % 2 == 0>(acc, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
+}
+
+inline int64_t tiles_of(int64_t m, int64_t n, int bm, int bn, bool symmetric) {
+  const int64_t tm = (m + bm - 1) / bm, tn = (n + bn - 1) / bn;
+  return symmetric ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+// Which tile a product takes, and over how many workgroups a tile's k is split.
+struct Plan {
+  int side;  // 256, 128 or 64
+  int splits, span;
+};
+inline Plan plan_of(int64_t m, int64_t n, int64_t k, int64_t count, bool symmetric, bool may_split) {
+  const int64_t kt = (k + kBK - 1) / kBK;
+  Plan p{256, 1, int(kt)};
+  if (tiles_of(m, n, 256, 256, symmetric) * count < kCus * 3 / 4) p.side = 128;
+  if (p.side == 128 && tiles_of(m, n, 128, 128, symmetric) * count < kCus * 3 / 4) p.side = 64;
+  const int64_t tiles = tiles_of(m, n, p.side, p.side, symmetric) * count;
+  // four k tiles a workgroup at least: a split costs its part of the sums written and read
+  if (may_split && p.side == 64 && tiles < kCus && kt >= 8) {
+    int64_t s = (2 * kCus + tiles - 1) / tiles;
+    if (s > kt / 4) s = kt / 4;
+    p.span = int((kt + s - 1) / s);
+    p.splits = int((kt + p.span - 1) / p.span);
+  }
+  return p;
+}
+inline size_t part_bytes(int64_t m, int64_t n, int64_t k, int64_t count, bool symmetric) {
+  const Plan p = plan_of(m, n, k, count, symmetric, true);
+  return p.splits > 1 ? up256(size_t(tiles_of(m, n, p.side, p.side, symmetric)) * count * p.splits * p.side * p.side * 4) : 0;
+}
+
+inline bool direct_ok(const void* p, int64_t ld, int64_t stride, int64_t contiguous, bool padded) {
+  return aligned(p, 16) && ld % 8 == 0 && stride % 8 == 0 && ld < (int64_t(1) << 21) && (contiguous % 8 == 0 || padded);
+}
+
+template <class T, class C, bool AKC, bool BKC, class Epi>
+int launch(GemmArgs g, const Epi& epi, hipStream_t st) {
+  g.tiles_m = int((g.m + C::BM - 1) / C::BM);
+  g.tiles_n = int((g.n + C::BN - 1) / C::BN);
+  g.tiles = int(tiles_of(g.m, g.n, C::BM, C::BN, Epi::kSymmetric));
+  const unsigned blocks = unsigned(g.tiles * g.count);
+  const bool direct = direct_ok(g.a, g.lda, g.stride_a, AKC ? g.k : g.m, g.pad_a) && direct_ok(g.b, g.ldb, g.stride_b, BKC ? g.k : g.n, g.pad_b);
+  if (direct)
+    k_gemm<T, C, AKC, BKC, true, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
+  else if constexpr (C::BM <= 128)
+    k_gemm<T, C, AKC, BKC, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
+  else
+    return launch<T, Config<128, 128, 2, 2>, AKC, BKC>(g, epi, st);  // two tiles' registers would not fit
+  if constexpr (C::BM == 64)
+    if (g.splits > 1) k_join<C, BKC, Epi><<<blocks, C::THREADS, 0, st>>>(g, epi);
   return launched();
 }
 
-// Four neighbouring elements of one row: one 8-byte access where the row has them and the address allows it.
-template <class T>
-__device__ inline f32x4 get4(const T* p, int64_t valid, bool wide) {
-  f32x4 v = {0, 0, 0, 0};
-  if (wide && valid >= 4) {
-    const typename Vec<T>::x4 e = *reinterpret_cast<const typename Vec<T>::x4*>(p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = float(e[j]);
+// part: part_bytes() of workspace, or NULL to leave k whole.
+template <class T, bool AKC, bool BKC, class Epi>
+int gemm(GemmArgs g, const Epi& epi, void* part, hipStream_t st) {
+  if (g.m <= 0 || g.n <= 0 || g.count <= 0) return XMEM_OK;
+  const Plan p = plan_of(g.m, g.n, g.k, g.count, Epi::kSymmetric, part != nullptr);
+  g.splits = p.splits;
+  g.span = p.span;
+  g.part = static_cast<float*>(part);
+  if (p.side == 256) return launch<T, Config<256, 256, 2, 4>, AKC, BKC>(g, epi, st);
+  if (p.side == 128) return launch<T, Config<128, 128, 2, 2>, AKC, BKC>(g, epi, st);
+  return launch<T, Config<64, 64, 2, 2>, AKC, BKC>(g, epi, st);
+}
+
+// W neighbouring elements of a row, `valid` of which exist; whole ones move in one access of any alignment.
+template <class T, int W>
+__device__ inline void get(const T* p, int valid, float (&v)[W]) {
+  T e[W];
+  if (valid == W) {
+    __builtin_memcpy(e, p, sizeof(e));
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < valid) v[j] = float(p[j]);
+    for (int j = 0; j < W; ++j) e[j] = j < valid ? p[j] : T(0.0f);
   }
-  return v;
-}
-template <class T>
-__device__ inline void put4(T* p, f32x4 v, int64_t valid, bool wide) {
-  if (wide && valid >= 4) {
-    typename Vec<T>::x4 e;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) e[j] = T(v[j]);
-    *reinterpret_cast<typename Vec<T>::x4*>(p) = e;
+  for (int j = 0; j < W; ++j) v[j] = float(e[j]);
+}
+template <class T, int W>
+__device__ inline void put(T* p, int valid, const float (&v)[W]) {
+  T e[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) e[j] = T(v[j]);
+  if (valid == W) {
+    __builtin_memcpy(p, e, sizeof(e));
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < valid) p[j] = T(v[j]);
+    for (int j = 0; j < W; ++j)
+      if (j < valid) p[j] = e[j];
   }
 }
+
+template <int W>
+struct Column {  // what an epilogue keeps of its W columns
+  float v[W];
+};
 
 }  // namespace xops

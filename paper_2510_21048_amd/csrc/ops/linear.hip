@@ -7,13 +7,14 @@ namespace {
 
 constexpr float kGelu = 0.7978845608028654f, kCube = 0.044715f;  // sqrt(2 / pi)
 
-// tanh(u) = 1 - 2 / (1 + exp(2u)) has no difference of near numbers in the gate (1 + tanh) / 2, which is the
-// logistic function of 2u: gelu(z) = z s(2u), as silu(z) = z s(z).
-__device__ inline float logistic(float v) { return 1.0f / (1.0f + __expf(-v)); }
+// (1 + tanh(u)) / 2 is the logistic function of 2u, without a difference of near numbers: gelu(z) = z s(2u), as
+// silu(z) = z s(z).  exp and 1/x are the hardware's, good to 2^-22 of their values.
+__device__ inline float logistic(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
+__device__ inline float gelu_argument(float z) { return z * (2.0f * kGelu + (2.0f * kGelu * kCube) * (z * z)); }
 
 __device__ inline float activate(float z, int act) {
   if (act == XMEM_ACT_RELU) return z < 0.0f ? 0.0f : z;  // NaN stays
-  if (act == XMEM_ACT_GELU) return z * logistic(2.0f * kGelu * (z + kCube * z * z * z));
+  if (act == XMEM_ACT_GELU) return z * logistic(gelu_argument(z));
   if (act == XMEM_ACT_SILU) return z * logistic(z);
   return z;
 }
@@ -21,9 +22,8 @@ __device__ inline float activate(float z, int act) {
 __device__ inline float slope(float z, int act) {
   if (act == XMEM_ACT_RELU) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
   if (act == XMEM_ACT_GELU) {
-    const float s = logistic(2.0f * kGelu * (z + kCube * z * z * z));
-    const float w = s * (1.0f - s);  // 0 where the cube overflows
-    return w == 0.0f ? s : s + z * w * (2.0f * kGelu * (1.0f + 3.0f * kCube * z * z));
+    const float s = logistic(gelu_argument(z)), w = s * (1.0f - s);  // 0 where the cube overflows
+    return w == 0.0f ? s : s + z * w * (2.0f * kGelu + (6.0f * kGelu * kCube) * (z * z));
   }
   if (act == XMEM_ACT_SILU) {
     const float s = logistic(z), w = s * (1.0f - s);
@@ -41,20 +41,28 @@ struct LinearEpilogue {
   T* z;
   int64_t ldr, ldy, ldz;
   int act;
-  bool wide;  // every row of r, y and z is 8-byte aligned
 
-  __device__ void operator()(int64_t m, int64_t n, f32x4 v, int, int64_t ms, int64_t ns) const {
-    if (m >= ms || n >= ns) return;
-    const int64_t valid = ns - n;
-    if (bias)
+  template <int W>
+  __device__ Column<W> column(int64_t n, int valid, int, const GemmArgs&) const {
+    Column<W> c;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (j < valid) v[j] += bias[n + j];
-    if (z) put4(z + m * ldz + n, v, valid, wide);
+    for (int j = 0; j < W; ++j) c.v[j] = bias && j < valid ? bias[n + j] : 0.0f;
+    return c;
+  }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& c, int, const GemmArgs&) const {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = activate(v[j], act);
-    if (r) v += get4(r + m * ldr + n, valid, wide);
-    put4(y + m * ldy + n, v, valid, wide);
+    for (int j = 0; j < W; ++j) v[j] += c.v[j];
+    if (z) put<T, W>(z + m * ldz + n, valid, v);
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[j] = activate(v[j], act);
+    if (r) {
+      float e[W];
+      get<T, W>(r + m * ldr + n, valid, e);
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[j] += e[j];
+    }
+    put<T, W>(y + m * ldy + n, valid, v);
   }
 };
 
@@ -63,10 +71,13 @@ struct StoreEpilogue {
   static constexpr bool kSymmetric = false;
   T* y;
   int64_t ldy;
-  bool wide;
 
-  __device__ void operator()(int64_t m, int64_t n, f32x4 v, int, int64_t ms, int64_t ns) const {
-    if (m < ms && n < ns) put4(y + m * ldy + n, v, ns - n, wide);
+  struct None {};
+  template <int W>
+  __device__ None column(int64_t, int, int, const GemmArgs&) const { return {}; }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, None, int, const GemmArgs&) const {
+    put<T, W>(y + m * ldy + n, valid, v);
   }
 };
 
@@ -75,13 +86,19 @@ constexpr int kBandCols = 256;
 
 inline int64_t bands(int64_t m) { return (m + kBandRows - 1) / kBandRows; }
 inline int64_t padded(int64_t n) { return (n + 7) & ~int64_t(7); }
+inline size_t part_bytes_of(int64_t m, int64_t n) { return up256(size_t(bands(m)) * n * 4); }
+inline size_t dz_bytes(int64_t m, int64_t n, int act) { return act == XMEM_ACT_NONE ? 0 : up256(size_t(m) * padded(n) * 2); }
 
 // dz = dy act'(z), and the column sums of each band of rows before dz is rounded.
 template <class T>
 __global__ __launch_bounds__(kBandCols) void k_dz(const T* dy, int64_t lddy, const T* z, int64_t ldz, int64_t m, int64_t n,
                                                   int act, T* dz, int64_t lddz, float* part) {
   const int64_t c = int64_t(blockIdx.x) * kBandCols + threadIdx.x, r0 = int64_t(blockIdx.y) * kBandRows;
-  if (c >= n) return;
+  if (c >= n) {  // what pads a row is 0: the product that sums along it reads it
+    if (dz && c < lddz)
+      for (int64_t r = r0; r < m && r < r0 + kBandRows; ++r) dz[r * lddz + c] = T(0.0f);
+    return;
+  }
   float sum = 0.0f;
   for (int64_t r = r0; r < m && r < r0 + kBandRows; ++r) {
     float v = float(dy[r * lddy + c]);
@@ -100,7 +117,7 @@ __global__ void k_db(const float* part, int64_t nb, int64_t n, float* db) {
   db[c] = sum;
 }
 
-constexpr int64_t kMostSize = int64_t(1) << 31;
+constexpr int64_t kMostSize = int64_t(1) << 30;
 constexpr int64_t kMostLd = int64_t(1) << 40;
 
 bool sizes_ok(int64_t m, int64_t n, int64_t k) {
@@ -109,15 +126,12 @@ bool sizes_ok(int64_t m, int64_t n, int64_t k) {
          ((n + 63) / 64) * ((k + 63) / 64) < kMostSize && bands(m) <= kMostSize;
 }
 bool ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld < kMostLd; }
-bool rows8(const void* p, int64_t ld) { return !p || (aligned(p, 8) && ld % 4 == 0); }
 
 template <class T>
 int forward(const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias, const void* r, int64_t ldr, int64_t m,
-            int64_t n, int64_t k, int act, void* y, int64_t ldy, void* z, int64_t ldz, hipStream_t st) {
-  LinearEpilogue<T> e{bias, static_cast<const T*>(r), static_cast<T*>(y), static_cast<T*>(z), ldr, ldy, ldz, act,
-                      rows8(r, ldr) && rows8(y, ldy) && rows8(z, ldz)};
-  GemmArgs g{x, w, ldx, ldw, 0, 0, m, n, k, 0, 0};
-  return gemm<T, true, true>(g, e, 1, st);
+            int64_t n, int64_t k, int act, void* y, int64_t ldy, void* z, int64_t ldz, void* ws, hipStream_t st) {
+  const LinearEpilogue<T> e{bias, static_cast<const T*>(r), static_cast<T*>(y), static_cast<T*>(z), ldr, ldy, ldz, act};
+  return gemm<T, true, true>(GemmArgs{x, w, ldx, ldw, 0, 0, m, n, k}, e, ws, st);
 }
 
 template <class T>
@@ -128,29 +142,25 @@ int backward(const void* dy, int64_t lddy, const void* z, int64_t ldz, const voi
   int64_t ldd = lddy;
   T* dz = nullptr;
   float* part = static_cast<float*>(ws);
-  const size_t part_bytes = up256(size_t(bands(m)) * n * 4);
   if (act != XMEM_ACT_NONE && (dx || dw)) {
-    dz = reinterpret_cast<T*>(static_cast<char*>(ws) + part_bytes);
+    dz = reinterpret_cast<T*>(static_cast<char*>(ws) + part_bytes_of(m, n));
     d = dz;
     ldd = padded(n);
   }
   if ((dz || db) && m > 0 && n > 0)
     for (int64_t b0 = 0; b0 < bands(m); b0 += 32768) {  // grid y is at most 65535
       const int64_t r0 = b0 * kBandRows, high = bands(m) - b0 < 32768 ? bands(m) - b0 : 32768;
-      k_dz<T><<<dim3(unsigned((n + kBandCols - 1) / kBandCols), unsigned(high)), kBandCols, 0, st>>>(
+      k_dz<T><<<dim3(unsigned((padded(n) + kBandCols - 1) / kBandCols), unsigned(high)), kBandCols, 0, st>>>(
           static_cast<const T*>(dy) + r0 * lddy, lddy, z ? static_cast<const T*>(z) + r0 * ldz : nullptr, ldz, m - r0, n, act,
           dz ? dz + r0 * ldd : nullptr, ldd, db ? part + b0 * n : nullptr);
     }
   if (db && n > 0) k_db<<<unsigned((n + 255) / 256), 256, 0, st>>>(part, bands(m), n, db);
   int rc = launched();
-  if (rc == XMEM_OK && dx) {
-    GemmArgs g{d, w, ldd, ldw, 0, 0, m, k, n, 0, 0};
-    rc = gemm<T, true, false>(g, StoreEpilogue<T>{static_cast<T*>(dx), lddx, rows8(dx, lddx)}, 1, st);
-  }
-  if (rc == XMEM_OK && dw) {
-    GemmArgs g{d, x, ldd, ldx, 0, 0, n, k, m, 0, 0};
-    rc = gemm<T, false, false>(g, StoreEpilogue<T>{static_cast<T*>(dw), lddw, rows8(dw, lddw)}, 1, st);
-  }
+  void* split = static_cast<char*>(ws) + part_bytes_of(m, n) + dz_bytes(m, n, act);
+  if (rc == XMEM_OK && dx)
+    rc = gemm<T, true, false>(GemmArgs{d, w, ldd, ldw, 0, 0, m, k, n, dz != nullptr}, StoreEpilogue<T>{static_cast<T*>(dx), lddx}, split, st);
+  if (rc == XMEM_OK && dw)
+    rc = gemm<T, false, false>(GemmArgs{d, x, ldd, ldx, 0, 0, n, k, m, dz != nullptr}, StoreEpilogue<T>{static_cast<T*>(dw), lddw}, split, st);
   return rc;
 }
 
@@ -161,8 +171,7 @@ bool known(int dtype, int act) { return (dtype == XMEM_BF16 || dtype == XMEM_F16
 extern "C" {
 
 size_t xmem_linear_forward_workspace_bytes(int64_t m, int64_t n, int64_t k) {
-  (void)m, (void)n, (void)k;
-  return 0;
+  return sizes_ok(m, n, k) ? part_bytes(m, n, k, 1, false) : 0;
 }
 
 int xmem_linear_forward(const void* d_x, int64_t ldx, const void* d_w, int64_t ldw, const float* d_bias,
@@ -176,14 +185,16 @@ int xmem_linear_forward(const void* d_x, int64_t ldx, const void* d_w, int64_t l
   if (!d_y || (k > 0 && (!d_x || !d_w))) return XMEM_EINVAL;
   const size_t need = xmem_linear_forward_workspace_bytes(m, n, k);
   if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 256))) return XMEM_EWORKSPACE;
+  if (!need) d_workspace = nullptr;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   return (dtype == XMEM_BF16 ? forward<bf16> : forward<f16>)(d_x, ldx, d_w, ldw, d_bias, d_residual, ldr, m, n, k, activation,
-                                                             d_y, ldy, d_z, ldz, st);
+                                                             d_y, ldy, d_z, ldz, d_workspace, st);
 }
 
 size_t xmem_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int activation) {
   if (!sizes_ok(m, n, k) || !known(XMEM_BF16, activation)) return 0;
-  return up256(size_t(bands(m)) * n * 4) + (activation == XMEM_ACT_NONE ? 0 : up256(size_t(m) * padded(n) * 2));
+  const size_t sx = part_bytes(m, k, n, 1, false), sw = part_bytes(n, k, m, 1, false);
+  return part_bytes_of(m, n) + dz_bytes(m, n, activation) + (sx > sw ? sx : sw);
 }
 
 int xmem_linear_backward(const void* d_dy, int64_t lddy, const void* d_z, int64_t ldz, const void* d_x, int64_t ldx,

@@ -40,9 +40,10 @@ Shape shape_of(int64_t count, int64_t rows, int64_t cols) {
 
 struct Ws {
   f16 *x[2], *lo[2];  // X and its second half, before and after a step
-  f16 *p, *q;
+  f16 *p, *q;         // what pads their rows is 0, as X's is
   float *dp, *dq;  // diagonals
   double* part;
+  void* split;  // partial sums of products whose k is split
   size_t bytes;
 };
 Ws carve(void* base, const Shape& h) {
@@ -63,6 +64,9 @@ Ws carve(void* base, const Shape& h) {
   w.dp = reinterpret_cast<float*>(take(size_t(h.count) * h.s * 4));
   w.dq = reinterpret_cast<float*>(take(size_t(h.count) * h.s * 4));
   w.part = reinterpret_cast<double*>(take(size_t(h.count) * kNormParts * 8));
+  const size_t s1 = part_bytes(h.s, h.s, h.l, h.count, true), s2 = part_bytes(h.s, h.s, h.s, h.count, true),
+               s3 = h.tall ? part_bytes(h.l, h.s, h.s, h.count, false) : part_bytes(h.s, h.l, h.s, h.count, false);
+  w.split = take(s1 > s2 ? (s1 > s3 ? s1 : s3) : s2 > s3 ? s2 : s3);
   w.bytes = size_t(at - static_cast<char*>(base));
   return w;
 }
@@ -111,6 +115,14 @@ __global__ __launch_bounds__(kThreads) void k_start(const G* g, const float* mom
   }
 }
 
+struct None {};
+
+// Clears what pads the rows of a matrix [rows, cols] of row length ld.
+__global__ void k_clear_pads(f16* p, int64_t rows, int64_t cols, int64_t ld) {
+  const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, pad = ld - cols;
+  if (i < rows * pad) p[i / pad * ld + cols + i % pad] = f16(0.0f);
+}
+
 // P = X X^T without its diagonal, which goes to d.  Only tiles on or below the diagonal are computed, and each
 // entry below it is written to its mirrored place too.
 struct GramEpilogue {
@@ -119,18 +131,29 @@ struct GramEpilogue {
   float* d;
   int64_t ld;
 
-  __device__ void operator()(int64_t m, int64_t n, f32x4 v, int z, int64_t ms, int64_t ns) const {
-    if (m >= ms) return;
-    f16* to = p + z * ms * ld;
+  template <int W>
+  __device__ None column(int64_t, int, int, const GemmArgs&) const { return {}; }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, None, int z, const GemmArgs& g) const {
+    f16* to = p + z * g.m * ld;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (n + j > m || n + j >= ns) continue;
-      const float e = v[j] * (1.0f / (kX * kX));
-      if (n + j == m) d[z * ms + m] = e;
-      const f16 h = n + j == m ? f16(0.0f) : f16(e * kP);
-      to[m * ld + n + j] = h;
-      to[(n + j) * ld + m] = h;
+    for (int j = 0; j < W; ++j) {
+      v[j] *= kP / (kX * kX);
+      if (n + j == m) {
+        d[z * g.m + m] = v[j] * (1.0f / kP);
+        v[j] = 0.0f;
+      }
     }
+    mirror<W>(to, ld, m, n, v, valid);
+  }
+  template <int W>
+  __device__ static void mirror(f16* to, int64_t ld, int64_t m, int64_t n, const float (&v)[W], int valid) {
+    if (n > m) return;  // its mirrored place is written
+    const int own = m - n + 1 < valid ? int(m - n + 1) : valid;
+    put<f16, W>(to + m * ld + n, own, v);
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (j < own) to[(n + j) * ld + m] = f16(v[j]);
   }
 };
 
@@ -143,25 +166,26 @@ struct PolyEpilogue {
   float* dq;
   int64_t ld;
 
-  __device__ void operator()(int64_t m, int64_t n, f32x4 v, int z, int64_t ms, int64_t ns) const {
-    if (m >= ms) return;
-    const f16* from = p + z * ms * ld;
-    f16* to = q + z * ms * ld;
-    const float dm = dp[z * ms + m];
+  template <int W>
+  __device__ Column<W> column(int64_t n, int valid, int z, const GemmArgs& g) const {
+    Column<W> c;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (n + j > m || n + j >= ns) continue;
-      const float ee = v[j] * (1.0f / (kP * kP));
-      if (n + j == m) {
-        dq[z * ms + m] = XMEM_NS_B * dm + XMEM_NS_C * (ee + dm * dm);
-        to[m * ld + m] = f16(0.0f);
-      } else {
-        const float e = float(from[m * ld + n + j]) * (1.0f / kP), dn = dp[z * ms + n + j];
-        const f16 h = f16((XMEM_NS_B * e + XMEM_NS_C * (ee + (dm + dn) * e)) * kP);
-        to[m * ld + n + j] = h;
-        to[(n + j) * ld + m] = h;
-      }
+    for (int j = 0; j < W; ++j) c.v[j] = j < valid ? dp[z * g.m + n + j] : 0.0f;
+    return c;
+  }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& dn, int z, const GemmArgs& g) const {
+    if (n > m) return;
+    const float dm = dp[z * g.m + m];
+    float e[W];
+    get<f16, W>(p + z * g.m * ld + m * ld + n, valid, e);
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      if (n + j == m) dq[z * g.m + m] = XMEM_NS_B * dm + XMEM_NS_C * (v[j] * (1.0f / (kP * kP)) + dm * dm);
+      // times kP; E_ii is 0
+      v[j] = n + j == m ? 0.0f : XMEM_NS_B * e[j] + XMEM_NS_C * (v[j] * (1.0f / kP) + (dm + dn.v[j]) * e[j]);
     }
+    GramEpilogue::mirror<W>(q + z * g.m * ld, ld, m, n, v, valid);
   }
 };
 
@@ -176,21 +200,31 @@ struct StepEpilogue {
   bf16* out;  // the last step writes the update instead
   float scale;
 
-  __device__ void operator()(int64_t m, int64_t n, f32x4 v, int z, int64_t ms, int64_t ns) const {
-    if (m >= ms) return;
-    const int64_t row = (z * ms + m) * ld;
+  template <int W>
+  __device__ Column<W> column(int64_t n, int valid, int z, const GemmArgs&) const {
+    Column<W> c;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (n + j >= ns) continue;
-      const float d = XMEM_NS_A + dq[z * s + (TALL ? n + j : m)];
-      const float e = (d * (float(x[row + n + j]) + float(lo[row + n + j])) + v[j] * (1.0f / kP));  // times kX
-      if (out) {
-        out[(z * ms + m) * ns + n + j] = bf16(e * (scale / kX));
-      } else {
-        const f16 hi = f16(e);
-        nx[row + n + j] = hi;
-        nlo[row + n + j] = f16(e - float(hi));
-      }
+    for (int j = 0; j < W; ++j) c.v[j] = TALL && j < valid ? XMEM_NS_A + dq[z * s + n + j] : 0.0f;
+    return c;
+  }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& dn, int z, const GemmArgs& g) const {
+    const int64_t at = (z * g.m + m) * ld + n;
+    const float dm = TALL ? 0.0f : XMEM_NS_A + dq[z * s + m];
+    float hi[W], rest[W];
+    get<f16, W>(x + at, valid, hi);
+    get<f16, W>(lo + at, valid, rest);
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[j] = (TALL ? dn.v[j] : dm) * (hi[j] + rest[j]) + v[j] * (1.0f / kP);  // times kX
+    if (out) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[j] *= scale / kX;
+      put<bf16, W>(out + (z * g.m + m) * g.n + n, valid, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; ++j) rest[j] = v[j] - float(f16(v[j]));
+      put<f16, W>(nx + at, valid, v);
+      put<f16, W>(nlo + at, valid, rest);
     }
   }
 };
@@ -224,31 +258,38 @@ int update(const G* g, float* mom, const Shape& h, float mu, bool nesterov, int 
     return launched();
   }
   const int64_t sx = h.rows * h.ldx, sp = h.s * h.lds;
+  const auto clear = [&](f16* p, int64_t rows, int64_t cols, int64_t ld) {
+    if (ld > cols) k_clear_pads<<<unsigned((rows * (ld - cols) + 255) / 256), 256, 0, st>>>(p, rows, cols, ld);
+  };
+  clear(w.x[1], h.count * h.rows, h.cols, h.ldx);
+  clear(w.p, h.count * h.s, h.s, h.lds);
+  clear(w.q, h.count * h.s, h.s, h.lds);
   for (int i = 0; i < steps && rc == XMEM_OK; ++i) {
     const f16 *x = w.x[i & 1], *lo = w.lo[i & 1];
     bf16* to = i == steps - 1 ? out : nullptr;
-    GemmArgs gram{x, x, h.ldx, h.ldx, sx, sx, h.s, h.s, h.l, 0, 0};
-    GemmArgs poly{w.p, w.p, h.lds, h.lds, sp, sp, h.s, h.s, h.s, 0, 0};
+    const auto args = [&](const f16* a, int64_t lda, int64_t sa, const f16* b, int64_t ldb, int64_t sb, int64_t m, int64_t n, int64_t k) {
+      return GemmArgs{a, b, lda, ldb, sa, sb, m, n, k, true, true, h.count};
+    };
+    const GemmArgs gram = args(x, h.ldx, sx, x, h.ldx, sx, h.s, h.s, h.l);
     const GramEpilogue ge{w.p, w.dp, h.lds};
     const PolyEpilogue pe{w.p, w.dp, w.q, w.dq, h.lds};
-    rc = h.tall ? gemm<f16, false, false>(gram, ge, h.count, st) : gemm<f16, true, true>(gram, ge, h.count, st);
-    if (rc == XMEM_OK) rc = gemm<f16, true, true>(poly, pe, h.count, st);
+    rc = h.tall ? gemm<f16, false, false>(gram, ge, w.split, st) : gemm<f16, true, true>(gram, ge, w.split, st);
+    if (rc == XMEM_OK) rc = gemm<f16, true, true>(args(w.p, h.lds, sp, w.p, h.lds, sp, h.s, h.s, h.s), pe, w.split, st);
     if (rc != XMEM_OK) break;
-    if (h.tall) {
-      GemmArgs step{x, w.q, h.ldx, h.lds, sx, sp, h.l, h.s, h.s, 0, 0};
-      rc = gemm<f16, true, true>(step, StepEpilogue<true>{x, lo, w.dq, w.x[~i & 1], w.lo[~i & 1], h.ldx, h.s, to, scale}, h.count, st);
-    } else {
-      GemmArgs step{w.q, x, h.lds, h.ldx, sp, sx, h.s, h.l, h.s, 0, 0};
-      rc = gemm<f16, true, false>(step, StepEpilogue<false>{x, lo, w.dq, w.x[~i & 1], w.lo[~i & 1], h.ldx, h.s, to, scale}, h.count, st);
-    }
+    f16 *nx = w.x[~i & 1], *nlo = w.lo[~i & 1];
+    if (h.tall)
+      rc = gemm<f16, true, true>(args(x, h.ldx, sx, w.q, h.lds, sp, h.l, h.s, h.s),
+                                 StepEpilogue<true>{x, lo, w.dq, nx, nlo, h.ldx, h.s, to, scale}, w.split, st);
+    else
+      rc = gemm<f16, true, false>(args(w.q, h.lds, sp, x, h.ldx, sx, h.s, h.l, h.s),
+                                  StepEpilogue<false>{x, lo, w.dq, nx, nlo, h.ldx, h.s, to, scale}, w.split, st);
   }
   return rc;
 }
 
 bool sizes_ok(int64_t count, int64_t rows, int64_t cols) {
   return count >= 0 && count <= kMostCount && rows >= 0 && cols >= 0 && rows < kMostSide && cols < kMostSide &&
-         ((rows + 127) / 128) * ((cols + 127) / 128) < (int64_t(1) << 31) &&
-         rows * cols < (int64_t(1) << 40);
+         rows * cols < (int64_t(1) << 40) && count * ((rows + 63) / 64) * ((cols + 63) / 64) < (int64_t(1) << 28);
 }
 
 }  // namespace
