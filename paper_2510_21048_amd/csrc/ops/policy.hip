@@ -5,9 +5,6 @@ using namespace xops;
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWaves = kThreads / kWave;
-
 struct Policy {
   const void* x;
   int64_t ldl;
@@ -21,96 +18,238 @@ struct Policy {
   float* part;  // [3][tokens]
 };
 
-// (largest, sum of exp(. - largest)) of two sets of logits; the largest of no logits is -inf.
-__device__ inline void join(float& m, float& s, float m2, float s2) {
-  const float top = fmaxf(m, m2);
-  s = (m == top ? s : s * __expf(m - top)) + (m2 == top ? s2 : s2 * __expf(m2 - top));
-  m = top;
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <class T> constexpr int kPer = 16 / sizeof(T);  // elements of a chunk
+
+// Chunk i of a row of `vocab` elements; what the row does not have is -inf, whose exponential is 0.
+template <class T>
+__device__ inline u32x4 chunk_of(const T* x, int64_t i, int64_t vocab) {
+  constexpr int E = kPer<T>;
+  u32x4 c;
+  if ((i + 1) * E <= vocab) {
+    __builtin_memcpy(&c, x + i * E, 16);
+  } else {
+    T e[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) e[k] = i * E + k < vocab ? x[i * E + k] : T(-INFINITY);
+    __builtin_memcpy(&c, e, 16);
+  }
+  return c;
+}
+template <class T>
+__device__ inline void store_chunk(T* dx, int64_t i, int64_t vocab, const float* v) {
+  constexpr int E = kPer<T>;
+  T e[E];
+#pragma unroll
+  for (int k = 0; k < E; ++k) e[k] = T(v[k]);
+  if ((i + 1) * E <= vocab) {
+    __builtin_memcpy(dx + i * E, e, 16);
+  } else {
+#pragma unroll
+    for (int k = 0; k < E; ++k)
+      if (i * E + k < vocab) dx[i * E + k] = e[k];
+  }
+}
+template <class T>
+__device__ inline void values(u32x4 c, float (&v)[kPer<T>]) {
+  T e[kPer<T>];
+  __builtin_memcpy(e, &c, 16);
+#pragma unroll
+  for (int k = 0; k < kPer<T>; ++k) v[k] = float(e[k]);
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_policy(Policy p) {
-  __shared__ float sm[kWaves], ss[kWaves];
-  const int64_t t = blockIdx.x;
+struct Max {
+  __device__ static float of(float a, float b) { return fmaxf(a, b); }
+};
+struct Sum {
+  __device__ static float of(float a, float b) { return a + b; }
+};
+// Over the threads of a row: a wavefront, or a workgroup (whose wavefronts' values meet in `meet`).
+template <class Op, int THREADS>
+__device__ inline float over_row(float v, float* meet) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v = Op::of(v, __shfl_xor(v, d));
+  if constexpr (THREADS > kWave) {
+    if ((threadIdx.x & 63) == 0) meet[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = meet[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / kWave; ++i) v = Op::of(v, meet[i]);
+  }
+  return v;
+}
+
+// THREADS of a row (64: four rows a workgroup), NCH chunks of the row in each thread's registers: the logits are read
+// once and their gradient is written once.  NCH = 0: a row too long for that is read again for each of the largest
+// logit (with the sum, rescaled when a larger one comes) and the gradient.
+template <class T, int THREADS, int NCH>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS == 1024 ? 4 : 6) void k_policy(Policy p) {
+  constexpr int E = kPer<T>;
+  __shared__ float meet[2][THREADS / kWave], at_y[THREADS < 256 ? 4 : 1];
+  const int tid = threadIdx.x % THREADS, slot = threadIdx.x / THREADS;
+  const int64_t t = THREADS < 256 ? int64_t(blockIdx.x) * (256 / THREADS) + slot : blockIdx.x;
+  if (t >= p.tokens) return;  // a whole wavefront, of those that do not meet others
+  const int64_t vocab = p.vocab, chunks = (vocab + E - 1) / E;
+  // the token's scalars, asked for together
   const float wt = p.w ? p.w[t] : 1.0f / float(p.tokens);
+  const int64_t y = p.y[t];
+  const bool loss = p.old_lp;
+  const float old_lp = loss ? p.old_lp[t] : 0.0f, adv = loss ? p.adv[t] : 0.0f, ref = p.ref ? p.ref[t] : 0.0f;
   const T* x = static_cast<const T*>(p.x) + t * p.ldl;
   T* dx = p.dx ? static_cast<T*>(p.dx) + t * p.ldd : nullptr;
   if (wt == 0.0f) {
+    const float zero[E] = {};
     if (dx)
-      for (int64_t j = threadIdx.x; j < p.vocab; j += kThreads) dx[j] = T(0.0f);
-    if (threadIdx.x == 0) {
+      for (int64_t i = tid; i < chunks; i += THREADS) store_chunk<T>(dx, i, vocab, zero);
+    if (tid == 0) {
       p.lp[t] = 0.0f;
       if (p.part) p.part[t] = p.part[p.tokens + t] = p.part[2 * p.tokens + t] = 0.0f;
     }
     return;
   }
-  float m = -INFINITY, s = 0.0f;
-  bool nan = false;
-  for (int64_t j = threadIdx.x; j < p.vocab; j += kThreads) {
-    const float v = float(x[j]);
-    nan |= v != v;
-    if (v > m) s = s * __expf(m - v), m = v;
-    if (v > -INFINITY) s += __expf(v - m);
-  }
-  if (nan) m = INFINITY, s = NAN;
+  const bool in = y >= 0 && y < vocab;
+  const int64_t cy = in ? y / E : -1;
+  if (!in && tid == 0) at_y[THREADS < 256 ? slot : 0] = NAN;
+  float m = -INFINITY, s = 0.0f, v[E];
+  // the sampled token's logit, from the thread that has it: the row may be overwritten
+  const auto note = [&](int64_t i) {
+    if (i == cy)
 #pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    const float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d);
-    join(m, s, m2, s2);
+      for (int k = 0; k < E; ++k)
+        if (i * E + k == y) at_y[THREADS < 256 ? slot : 0] = v[k];
+  };
+  u32x4 c[NCH > 0 ? NCH : 1];
+  if constexpr (NCH > 0) {
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int i = j * THREADS + tid;
+      if (j * THREADS < chunks) c[j] = chunk_of(x, i, vocab);
+    }
+#pragma unroll
+    for (int j = 0; j < NCH; ++j)
+      if (j * THREADS < chunks) {
+        values<T>(c[j], v);
+        note(j * THREADS + tid);
+#pragma unroll
+        for (int k = 0; k < E; ++k) m = fmaxf(m, v[k]);
+      }
+    m = over_row<Max, THREADS>(m, meet[0]);
+#pragma unroll
+    for (int j = 0; j < NCH; ++j)
+      if (j * THREADS < chunks) {
+        values<T>(c[j], v);
+#pragma unroll
+        for (int k = 0; k < E; ++k) s += __builtin_amdgcn_exp2f((v[k] - m) * kLog2e);
+      }
+    s = over_row<Sum, THREADS>(s, meet[1]);
+  } else {
+    bool nan = false;
+    for (int64_t i = tid; i < chunks; i += THREADS) {
+      values<T>(chunk_of(x, i, vocab), v);
+      note(i);
+      float top = m;
+#pragma unroll
+      for (int k = 0; k < E; ++k) {
+        top = fmaxf(top, v[k]);
+        nan |= v[k] != v[k];
+      }
+      if (top > m) {
+        s *= __builtin_amdgcn_exp2f((m - top) * kLog2e);
+        m = top;
+      }
+      if (m > -INFINITY)
+#pragma unroll
+        for (int k = 0; k < E; ++k) s += __builtin_amdgcn_exp2f((v[k] - m) * kLog2e);
+    }
+    const float top = over_row<Max, THREADS>(m, meet[0]);
+    // a thread with nothing but -inf adds 0, unless no thread has more
+    s = nan ? NAN : m > -INFINITY || top == -INFINITY ? s * __builtin_amdgcn_exp2f((m - top) * kLog2e) : 0.0f;
+    m = top;
+    s = over_row<Sum, THREADS>(s, meet[1]);
   }
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m, ss[threadIdx.x >> 6] = s;
-  const int64_t y = p.y[t];
-  const bool in = y >= 0 && y < p.vocab;
-  const float xy = in ? float(x[in ? y : 0]) : NAN;  // before the row may be overwritten
-  __syncthreads();
-  m = sm[0], s = ss[0];
-  for (int i = 1; i < kWaves; ++i) join(m, s, sm[i], ss[i]);
-  const float lp = (xy - m) - logf(s);
+  if constexpr (THREADS == kWave) __builtin_amdgcn_wave_barrier();
+  const float lp = (at_y[THREADS < 256 ? slot : 0] - m) - logf(s);
   float grad = 0.0f;
-  if (p.old_lp) {
-    const float adv = p.adv[t], rho = expf(lp - p.old_lp[t]);
+  if (loss) {
+    const float rho = expf(lp - old_lp);
     const float free = rho * adv, held = fminf(fmaxf(rho, 1.0f - p.low), 1.0f + p.high) * adv;
     const bool clipped = held < free;
     float kl = 0.0f;
     grad = clipped ? 0.0f : -free;
     if (p.ref) {
-      const float d = p.ref[t] - lp, e = expm1f(d);
+      const float d = ref - lp, e = expm1f(d);
       kl = e - d;
       grad -= p.kl_coef * e;
     }
     grad *= wt;
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
       p.part[t] = wt * -(clipped ? held : free);
       p.part[p.tokens + t] = wt * kl;
       p.part[2 * p.tokens + t] = clipped ? wt : 0.0f;
     }
   }
-  if (threadIdx.x == 0) p.lp[t] = lp;
+  if (tid == 0) p.lp[t] = lp;
   if (!dx) return;
   grad *= p.grad_scale;
-  const float per = grad / s;
-  for (int64_t j = threadIdx.x; j < p.vocab; j += kThreads) {
-    const float v = float(x[j]);
-    dx[j] = T((j == y ? grad : 0.0f) - per * __expf(v - m));
+  const float per = -grad / s;
+  const auto emit = [&](u32x4 q, int64_t i) {
+    values<T>(q, v);
+#pragma unroll
+    for (int k = 0; k < E; ++k) v[k] = per * __builtin_amdgcn_exp2f((v[k] - m) * kLog2e);
+    if (i == cy)
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+        if (i * E + k == y) v[k] += grad;
+    store_chunk<T>(dx, i, vocab, v);
+  };
+  if constexpr (NCH > 0) {
+#pragma unroll
+    for (int j = 0; j < NCH; ++j)
+      if (j * THREADS < chunks) emit(c[j], j * THREADS + tid);
+  } else {
+    for (int64_t i = tid; i < chunks; i += THREADS) emit(chunk_of(x, i, vocab), i);
   }
 }
 
+// The sums of the three parts, in 64 bits and a fixed order.
 __global__ __launch_bounds__(1024) void k_policy_sums(const float* part, int64_t tokens, float kl_coef, float* stats) {
   __shared__ double sums[3][16];
+  double v[3] = {0, 0, 0};
+#pragma unroll 8
+  for (int64_t t = threadIdx.x; t < tokens; t += 1024)
+#pragma unroll
+    for (int q = 0; q < 3; ++q) v[q] += part[q * tokens + t];
+#pragma unroll
   for (int q = 0; q < 3; ++q) {
-    double v = 0.0;
-    for (int64_t t = threadIdx.x; t < tokens; t += 1024) v += part[q * tokens + t];
-    v = wave_sum(v);
-    if ((threadIdx.x & 63) == 0) sums[q][threadIdx.x >> 6] = v;
+    v[q] = wave_sum(v[q]);
+    if ((threadIdx.x & 63) == 0) sums[q][threadIdx.x >> 6] = v[q];
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    double v[3] = {0, 0, 0};
-    for (int q = 0; q < 3; ++q)
+    for (int q = 0; q < 3; ++q) {
+      v[q] = 0.0;
       for (int i = 0; i < 16; ++i) v[q] += sums[q][i];
+    }
     stats[0] = float(v[0] + double(kl_coef) * v[1]);
     stats[1] = float(v[0]), stats[2] = float(v[1]), stats[3] = float(v[2]);
   }
+}
+
+template <class T>
+void launch_policy(const Policy& p, hipStream_t st) {
+  const int64_t chunks = (p.vocab + kPer<T> - 1) / kPer<T>;
+  const unsigned rows = unsigned(p.tokens);
+  if (chunks <= 64 * 4)
+    k_policy<T, 64, 4><<<(rows + 3) / 4, 256, 0, st>>>(p);
+  else if (chunks <= 256 * 8)
+    k_policy<T, 256, 8><<<rows, 256, 0, st>>>(p);
+  else if (chunks <= 512 * 13)
+    k_policy<T, 512, 13><<<rows, 512, 0, st>>>(p);
+  else if (chunks <= 1024 * 16 && p.dx)
+    k_policy<T, 1024, 16><<<rows, 1024, 0, st>>>(p);
+  else
+    k_policy<T, 1024, 0><<<rows, 1024, 0, st>>>(p);
 }
 
 constexpr int64_t kMost = int64_t(1) << 31;
@@ -142,8 +281,7 @@ int xmem_policy_loss(const void* d_logits, int64_t ldl, const int64_t* d_tokens,
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   Policy p{d_logits, ldl, d_tokens, d_weights, d_old_logp, d_advantages, d_ref_logp, tokens, vocab, clip_low, clip_high, kl_coef,
            grad_scale, d_logp, d_dlogits, ldd, loss ? static_cast<float*>(d_workspace) : nullptr};
-  if (tokens > 0)
-    (dtype == XMEM_BF16 ? k_policy<bf16> : dtype == XMEM_F16 ? k_policy<f16> : k_policy<float>)<<<unsigned(tokens), kThreads, 0, st>>>(p);
+  if (tokens > 0) (dtype == XMEM_BF16 ? launch_policy<bf16> : dtype == XMEM_F16 ? launch_policy<f16> : launch_policy<float>)(p, st);
   if (loss) k_policy_sums<<<1, 1024, 0, st>>>(p.part, tokens, d_ref_logp ? kl_coef : 0.0f, d_stats);
   return launched();
 }
