@@ -82,38 +82,70 @@ struct StoreEpilogue {
 };
 
 constexpr int kBandRows = 64;  // rows whose column sums one workgroup of k_dz takes
-constexpr int kBandCols = 256;
+constexpr int kBandCols = 512;  // eight columns a lane
 
 inline int64_t bands(int64_t m) { return (m + kBandRows - 1) / kBandRows; }
 inline int64_t padded(int64_t n) { return (n + 7) & ~int64_t(7); }
 inline size_t part_bytes_of(int64_t m, int64_t n) { return up256(size_t(bands(m)) * n * 4); }
 inline size_t dz_bytes(int64_t m, int64_t n, int act) { return act == XMEM_ACT_NONE ? 0 : up256(size_t(m) * padded(n) * 2); }
 
-// dz = dy act'(z), and the column sums of each band of rows before dz is rounded.
+// dz = dy act'(z), and the column sums of each band of rows before dz is rounded.  A wavefront takes every fourth row of
+// the band, 16 bytes a lane; what pads a row of dz is 0, since the product that sums along it reads it.
 template <class T>
-__global__ __launch_bounds__(kBandCols) void k_dz(const T* dy, int64_t lddy, const T* z, int64_t ldz, int64_t m, int64_t n,
-                                                  int act, T* dz, int64_t lddz, float* part) {
-  const int64_t c = int64_t(blockIdx.x) * kBandCols + threadIdx.x, r0 = int64_t(blockIdx.y) * kBandRows;
-  if (c >= n) {  // what pads a row is 0: the product that sums along it reads it
-    if (dz && c < lddz)
-      for (int64_t r = r0; r < m && r < r0 + kBandRows; ++r) dz[r * lddz + c] = T(0.0f);
-    return;
+__global__ __launch_bounds__(256) void k_dz(const T* dy, int64_t lddy, const T* z, int64_t ldz, int64_t m, int64_t n, int act, T* dz,
+                                            int64_t lddz, float* part) {
+  __shared__ float sums[3][kBandCols];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = int64_t(blockIdx.x) * kBandCols + lane * 8, r0 = int64_t(blockIdx.y) * kBandRows;
+  const int valid = n - c >= 8 ? 8 : n > c ? int(n - c) : 0;
+  const int64_t end = m < r0 + kBandRows ? m : r0 + kBandRows;
+  float sum[8] = {};
+  if (valid > 0) {
+#pragma unroll 4
+    for (int64_t r = r0 + wave; r < end; r += 4) {
+      float v[8], w[8];
+      get<T, 8>(dy + r * lddy + c, valid, v);
+      if (z) {
+        get<T, 8>(z + r * ldz + c, valid, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= slope(w[j], act);
+      }
+      if (dz) {
+        if (valid < 8)  // where z is read as 0 past the end, dy is too
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = j < valid ? v[j] : 0.0f;
+        put<T, 8>(dz + r * lddz + c, 8, v);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += v[j];
+    }
   }
-  float sum = 0.0f;
-  for (int64_t r = r0; r < m && r < r0 + kBandRows; ++r) {
-    float v = float(dy[r * lddy + c]);
-    if (z) v *= slope(float(z[r * ldz + c]), act);
-    if (dz) dz[r * lddz + c] = T(v);
-    sum += v;
-  }
-  if (part) part[int64_t(blockIdx.y) * n + c] = sum;
+  if (!part) return;
+  if (wave > 0)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[wave - 1][lane * 8 + j] = sum[j];
+  __syncthreads();
+  if (wave == 0)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j < valid) part[int64_t(blockIdx.y) * n + c + j] = ((sum[j] + sums[0][lane * 8 + j]) + sums[1][lane * 8 + j]) + sums[2][lane * 8 + j];
+    }
 }
 
-__global__ void k_db(const float* part, int64_t nb, int64_t n, float* db) {
-  const int64_t c = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
-  if (c >= n) return;
+// The bands' sums, 16 runs of bands to a column and those in order.
+__global__ __launch_bounds__(1024) void k_db(const float* part, int64_t nb, int64_t n, float* db) {
+  __shared__ float sums[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = int64_t(blockIdx.x) * 64 + lane;
   float sum = 0.0f;
-  for (int64_t b = 0; b < nb; ++b) sum += part[b * n + c];
+  if (c < n)
+#pragma unroll 8
+    for (int64_t b = wave; b < nb; b += 16) sum += part[b * n + c];
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave > 0 || c >= n) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) sum += sums[i][lane];
   db[c] = sum;
 }
 
@@ -150,11 +182,12 @@ int backward(const void* dy, int64_t lddy, const void* z, int64_t ldz, const voi
   if ((dz || db) && m > 0 && n > 0)
     for (int64_t b0 = 0; b0 < bands(m); b0 += 32768) {  // grid y is at most 65535
       const int64_t r0 = b0 * kBandRows, high = bands(m) - b0 < 32768 ? bands(m) - b0 : 32768;
-      k_dz<T><<<dim3(unsigned((padded(n) + kBandCols - 1) / kBandCols), unsigned(high)), kBandCols, 0, st>>>(
+      float* sums = !db ? nullptr : bands(m) == 1 ? db : part + b0 * n;
+      k_dz<T><<<dim3(unsigned((n + kBandCols - 1) / kBandCols), unsigned(high)), 256, 0, st>>>(
           static_cast<const T*>(dy) + r0 * lddy, lddy, z ? static_cast<const T*>(z) + r0 * ldz : nullptr, ldz, m - r0, n, act,
-          dz ? dz + r0 * ldd : nullptr, ldd, db ? part + b0 * n : nullptr);
+          dz ? dz + r0 * ldd : nullptr, ldd, sums);
     }
-  if (db && n > 0) k_db<<<unsigned((n + 255) / 256), 256, 0, st>>>(part, bands(m), n, db);
+  if (db && n > 0 && bands(m) != 1) k_db<<<unsigned((n + 63) / 64), 1024, 0, st>>>(part, bands(m), n, db);
   int rc = launched();
   void* split = static_cast<char*>(ws) + part_bytes_of(m, n) + dz_bytes(m, n, act);
   if (rc == XMEM_OK && dx)
