@@ -24,11 +24,16 @@ struct GemmArgs {
   float* part = nullptr;
 };
 
-// A workgroup's tile and its wavefronts: WM by WN of them, each with BM / WM by BN / WN of the tile.
-template <int BM_, int BN_, int WM_, int WN_>
+// A workgroup's tile and its wavefronts: WM by WN of them, each with BM / WM by BN / WN of the tile; STAGES k tiles in
+// LDS, all but one of them on their way (a power of two); through registers, DEPTH k tiles on their way.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int DEPTH_>
 struct Config {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, FM = BM / WM / 16, FN = BN / WN / 16, THREADS = 64 * WM * WN;
+  static constexpr int STAGES = STAGES_, DEPTH = DEPTH_;
 };
+typedef Config<256, 256, 2, 4, 2, 0> Large;   // 128 KiB of LDS, two wavefronts on a SIMD: a CU to itself
+typedef Config<128, 128, 2, 2, 4, 1> Medium;  // 128 KiB
+typedef Config<64, 64, 2, 2, 8, 4> Small;     // 128 KiB
 
 // One operand tile in LDS: R rows of kBK.  Chunks of 16 bytes are kept at swizzled places, so that the 16 lanes
 // that read one column of chunks meet 16 different bank groups.
@@ -246,10 +251,10 @@ __device__ inline void finish(const f32x4 (&acc)[C::FM][C::FN], const Epi& epi, 
   }
 }
 
-// out += over this workgroup's k tiles.  Two LDS buffers, and half a tile's operands in registers ahead of the matrix
-// instructions: while the products of one half run, the other half's LDS reads are under way; one barrier a tile,
-// after which the tile just read is overwritten by the loads of the tile after next (direct) or the next tile,
-// which was loaded while the first half ran, is complete (staged).
+// One workgroup's tile.  Half a tile's operands are in registers ahead of the matrix instructions: while the products of
+// one half run, the other half's LDS reads are under way.  One barrier a k tile: after it the tile just read is
+// overwritten by the loads of the tile STAGES on (direct), or the next tile, stored from registers while the
+// first half ran, is complete (staged, two LDS buffers).
 // The n side is the first operand of the matrix instruction, so that a lane ends with neighbouring n of one m.
 template <class T, class C, bool AKC, bool BKC, bool DIRECT, class Epi>
 __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
@@ -260,7 +265,8 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
   typedef Tile<T, C::BN, BKC, PERM> TB;
   constexpr int BUF = TA::kBytes + TB::kBytes, kReads = FM * (AKC ? 1 : 2) + FN * (BKC ? 1 : 2);
   typedef typename Vec<T>::x8 x8;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * BUF];
+  constexpr int BUFS = DIRECT ? C::STAGES : 2, LOADS = (TA::kChunks + TB::kChunks) / C::THREADS;
+  __shared__ __attribute__((aligned(1024))) char lds[BUFS * BUF];
   int id = run_of(blockIdx.x, gridDim.x), tm, tn;
   const int z = id / (g.tiles * g.splits);
   id -= z * g.tiles * g.splits;
@@ -280,7 +286,7 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
     for (int j = 0; j < FN; ++j) acc[i][j] = {0, 0, 0, 0};
   x8 a0[FM], b0[FN], a1[FM], b1[FN];
   const auto read = [&](x8(&fa)[FM], x8(&fb)[FN], int t, int s) {
-    const char* from = lds + (t & 1) * BUF;
+    const char* from = lds + (t & (BUFS - 1)) * BUF;
 #pragma unroll
     for (int j = 0; j < FN; ++j) fb[j] = TB::frag(from + TA::kBytes, wn + 16 * j, s, lane);
 #pragma unroll
@@ -298,56 +304,69 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
     la.init(a, g.lda, m0, g.m, ks);
     lb.init(b, g.ldb, n0, g.n, ks);
     const auto fetch = [&](int t) {
-      char* to = lds + (t & 1) * BUF;
+      char* to = lds + (t & (BUFS - 1)) * BUF;
       la.issue(to, a, g.lda, m0, g.m, t, ks, wave);
       lb.issue(to + TA::kBytes, b, g.ldb, n0, g.n, t, ks, wave);
     };
     if (t0 < t1) {
-      fetch(t0);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      fetch(t0 + 1);
+#pragma unroll
+      for (int i = 0; i < BUFS; ++i) {
+        if (i == BUFS - 1) {
+          asm volatile("s_waitcnt vmcnt(%0)" ::"n"((BUFS - 2) * LOADS) : "memory");
+          __builtin_amdgcn_s_barrier();
+        }
+        fetch(t0 + i);
+      }
       read(a0, b0, t0, 0);
       for (int t = t0; t < t1; ++t) {
         read(a1, b1, t, 1);
         multiply(a0, b0);
         Order<0, kReads, FM * FN>::apply();
         // every read of this tile is done, and the next tile has come
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * LOADS) : "memory");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        fetch(t + 2);
+        fetch(t + BUFS);
         read(a0, b0, t + 1, 0);
         multiply(a1, b1);
-        Order<la.kLoads + lb.kLoads, kReads, FM * FN>::apply();
+        Order<LOADS, kReads, FM * FN>::apply();
       }
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
   } else {
-    Staged<T, TA, C::BM, AKC, C::THREADS> la;
-    Staged<T, TB, C::BN, BKC, C::THREADS> lb;
-    const auto load = [&](int t) {
-      la.load(a, g.lda, m0, g.m, t, ks);
-      lb.load(b, g.ldb, n0, g.n, t, ks);
-    };
-    const auto store = [&](int t) {
-      char* to = lds + (t & 1) * BUF;
-      la.store(to);
-      lb.store(to + TA::kBytes);
-    };
+    Staged<T, TA, C::BM, AKC, C::THREADS> la[C::DEPTH];
+    Staged<T, TB, C::BN, BKC, C::THREADS> lb[C::DEPTH];
     if (t0 < t1) {
-      load(t0);
-      store(t0);
+      const auto load = [&](int t, int i) {
+        if (t >= t1) return;
+        la[i].load(a, g.lda, m0, g.m, t, ks);
+        lb[i].load(b, g.ldb, n0, g.n, t, ks);
+      };
+      const auto store = [&](int t, int i) {
+        if (t >= t1) return;
+        char* to = lds + (t & (BUFS - 1)) * BUF;
+        la[i].store(to);
+        lb[i].store(to + TA::kBytes);
+      };
+      load(t0, 0);
+      store(t0, 0);
+#pragma unroll
+      for (int i = 0; i < C::DEPTH; ++i) load(t0 + 1 + i, i);
       __syncthreads();
       read(a0, b0, t0, 0);
-      for (int t = t0; t < t1; ++t) {
-        if (t + 1 < t1) load(t + 1);
-        read(a1, b1, t, 1);
-        multiply(a0, b0);
-        if (t + 1 < t1) store(t + 1);
-        __syncthreads();
-        if (t + 1 < t1) read(a0, b0, t + 1, 0);
-        multiply(a1, b1);
+      for (int tt = t0; tt < t1; tt += C::DEPTH) {
+#pragma unroll
+        for (int i = 0; i < C::DEPTH; ++i) {
+          const int t = tt + i;
+          if (t >= t1) break;
+          read(a1, b1, t, 1);
+          multiply(a0, b0);
+          store(t + 1, i);
+          load(t + 1 + C::DEPTH, i);
+          __syncthreads();
+          if (t + 1 < t1) read(a0, b0, t + 1, 0);
+          multiply(a1, b1);
+        }
       }
     }
   }
@@ -402,10 +421,10 @@ inline Plan plan_of(int64_t m, int64_t n, int64_t k, int64_t count, bool symmetr
   if (tiles_of(m, n, 256, 256, symmetric) * count < kCus * 3 / 4) p.side = 128;
   if (p.side == 128 && tiles_of(m, n, 128, 128, symmetric) * count < kCus * 3 / 4) p.side = 64;
   const int64_t tiles = tiles_of(m, n, p.side, p.side, symmetric) * count;
-  // four k tiles a workgroup at least: a split costs its part of the sums written and read
-  if (may_split && p.side == 64 && tiles < kCus && kt >= 8) {
+  // 16 k tiles a workgroup at least: a split costs its part of the sums, written and read, and another launch
+  if (may_split && p.side == 64 && tiles < kCus && kt >= 32) {
     int64_t s = (2 * kCus + tiles - 1) / tiles;
-    if (s > kt / 4) s = kt / 4;
+    if (s > kt / 16) s = kt / 16;
     p.span = int((kt + s - 1) / s);
     p.splits = int((kt + p.span - 1) / p.span);
   }
@@ -429,10 +448,10 @@ int launch(GemmArgs g, const Epi& epi, hipStream_t st) {
   const bool direct = direct_ok(g.a, g.lda, g.stride_a, AKC ? g.k : g.m, g.pad_a) && direct_ok(g.b, g.ldb, g.stride_b, BKC ? g.k : g.n, g.pad_b);
   if (direct)
     k_gemm<T, C, AKC, BKC, true, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
-  else if constexpr (C::BM <= 128)
+  else if constexpr (C::DEPTH > 0)
     k_gemm<T, C, AKC, BKC, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
   else
-    return launch<T, Config<128, 128, 2, 2>, AKC, BKC>(g, epi, st);  // two tiles' registers would not fit
+    return launch<T, Medium, AKC, BKC>(g, epi, st);  // a tile's registers would not fit
   if constexpr (C::BM == 64)
     if (g.splits > 1) k_join<C, BKC, Epi><<<blocks, C::THREADS, 0, st>>>(g, epi);
   return launched();
@@ -446,9 +465,9 @@ int gemm(GemmArgs g, const Epi& epi, void* part, hipStream_t st) {
   g.splits = p.splits;
   g.span = p.span;
   g.part = static_cast<float*>(part);
-  if (p.side == 256) return launch<T, Config<256, 256, 2, 4>, AKC, BKC>(g, epi, st);
-  if (p.side == 128) return launch<T, Config<128, 128, 2, 2>, AKC, BKC>(g, epi, st);
-  return launch<T, Config<64, 64, 2, 2>, AKC, BKC>(g, epi, st);
+  if (p.side == 256) return launch<T, Large, AKC, BKC>(g, epi, st);
+  if (p.side == 128) return launch<T, Medium, AKC, BKC>(g, epi, st);
+  return launch<T, Small, AKC, BKC>(g, epi, st);
 }
 
 // W neighbouring elements of a row, `valid` of which exist; whole ones move in one access of any alignment.

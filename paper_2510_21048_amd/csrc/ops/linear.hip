@@ -81,24 +81,25 @@ struct StoreEpilogue {
   }
 };
 
-constexpr int kBandRows = 64;  // rows whose column sums one workgroup of k_dz takes
-constexpr int kBandCols = 512;  // eight columns a lane
+constexpr int kBandCols = 512;  // columns of a workgroup of k_dz, eight a lane
 
-inline int64_t bands(int64_t m) { return (m + kBandRows - 1) / kBandRows; }
+// Rows whose column sums one workgroup of k_dz takes: 64, or 16 where that would leave most CUs without one.
+inline int64_t band_rows(int64_t m, int64_t n) { return (m + 63) / 64 * ((n + kBandCols - 1) / kBandCols) < 4 * kCus ? 16 : 64; }
+inline int64_t bands(int64_t m, int64_t n) { return (m + band_rows(m, n) - 1) / band_rows(m, n); }
 inline int64_t padded(int64_t n) { return (n + 7) & ~int64_t(7); }
-inline size_t part_bytes_of(int64_t m, int64_t n) { return up256(size_t(bands(m)) * n * 4); }
+inline size_t part_bytes_of(int64_t m, int64_t n) { return up256(size_t(bands(m, n)) * n * 4); }
 inline size_t dz_bytes(int64_t m, int64_t n, int act) { return act == XMEM_ACT_NONE ? 0 : up256(size_t(m) * padded(n) * 2); }
 
 // dz = dy act'(z), and the column sums of each band of rows before dz is rounded.  A wavefront takes every fourth row of
 // the band, 16 bytes a lane; what pads a row of dz is 0, since the product that sums along it reads it.
 template <class T>
 __global__ __launch_bounds__(256) void k_dz(const T* dy, int64_t lddy, const T* z, int64_t ldz, int64_t m, int64_t n, int act, T* dz,
-                                            int64_t lddz, float* part) {
+                                            int64_t lddz, float* part, int band) {
   __shared__ float sums[3][kBandCols];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = int64_t(blockIdx.x) * kBandCols + lane * 8, r0 = int64_t(blockIdx.y) * kBandRows;
+  const int64_t c = int64_t(blockIdx.x) * kBandCols + lane * 8, r0 = int64_t(blockIdx.y) * band;
   const int valid = n - c >= 8 ? 8 : n > c ? int(n - c) : 0;
-  const int64_t end = m < r0 + kBandRows ? m : r0 + kBandRows;
+  const int64_t end = m < r0 + band ? m : r0 + band;
   float sum[8] = {};
   if (valid > 0) {
 #pragma unroll 4
@@ -155,7 +156,7 @@ constexpr int64_t kMostLd = int64_t(1) << 40;
 bool sizes_ok(int64_t m, int64_t n, int64_t k) {
   return m >= 0 && n >= 0 && k >= 0 && m < kMostSize && n < kMostSize && k < kMostSize &&
          ((m + 63) / 64) * ((n + 63) / 64) < kMostSize && ((m + 63) / 64) * ((k + 63) / 64) < kMostSize &&
-         ((n + 63) / 64) * ((k + 63) / 64) < kMostSize && bands(m) <= kMostSize;
+         ((n + 63) / 64) * ((k + 63) / 64) < kMostSize;
 }
 bool ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld < kMostLd; }
 
@@ -180,14 +181,14 @@ int backward(const void* dy, int64_t lddy, const void* z, int64_t ldz, const voi
     ldd = padded(n);
   }
   if ((dz || db) && m > 0 && n > 0)
-    for (int64_t b0 = 0; b0 < bands(m); b0 += 32768) {  // grid y is at most 65535
-      const int64_t r0 = b0 * kBandRows, high = bands(m) - b0 < 32768 ? bands(m) - b0 : 32768;
-      float* sums = !db ? nullptr : bands(m) == 1 ? db : part + b0 * n;
+    for (int64_t b0 = 0; b0 < bands(m, n); b0 += 32768) {  // grid y is at most 65535
+      const int64_t r0 = b0 * band_rows(m, n), high = bands(m, n) - b0 < 32768 ? bands(m, n) - b0 : 32768;
+      float* sums = !db ? nullptr : bands(m, n) == 1 ? db : part + b0 * n;
       k_dz<T><<<dim3(unsigned((n + kBandCols - 1) / kBandCols), unsigned(high)), 256, 0, st>>>(
           static_cast<const T*>(dy) + r0 * lddy, lddy, z ? static_cast<const T*>(z) + r0 * ldz : nullptr, ldz, m - r0, n, act,
-          dz ? dz + r0 * ldd : nullptr, ldd, sums);
+          dz ? dz + r0 * ldd : nullptr, ldd, sums, int(band_rows(m, n)));
     }
-  if (db && n > 0 && bands(m) != 1) k_db<<<unsigned((n + 63) / 64), 1024, 0, st>>>(part, bands(m), n, db);
+  if (db && n > 0 && bands(m, n) != 1) k_db<<<unsigned((n + 63) / 64), 1024, 0, st>>>(part, bands(m, n), n, db);
   int rc = launched();
   void* split = static_cast<char*>(ws) + part_bytes_of(m, n) + dz_bytes(m, n, act);
   if (rc == XMEM_OK && dx)

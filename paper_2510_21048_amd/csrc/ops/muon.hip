@@ -23,7 +23,7 @@ namespace {
 constexpr float kX = 256.0f, kP = 1024.0f;
 constexpr float kNormEps = 1e-7f;
 constexpr int kThreads = 256;
-constexpr int kNormParts = 64;  // workgroups whose sums make one matrix's norm
+constexpr int kNormParts = 256;  // workgroups whose sums make one matrix's norm
 constexpr int64_t kMostCount = 65535, kMostSide = int64_t(1) << 24;
 
 struct Shape {
@@ -71,17 +71,25 @@ Ws carve(void* base, const Shape& h) {
   return w;
 }
 
-// m <- mu m + g, and the squares of u summed in 64 bits (a matrix may have 2^48 entries of any size).
+// m <- mu m + g, and the squares of u summed in 64 bits (their range is no matter then).  Eight elements a thread at a time.
 template <class G>
 __global__ __launch_bounds__(kThreads) void k_momentum(const G* g, float* mom, int64_t per, float mu, bool nesterov, double* part) {
   __shared__ double sums[kThreads / kWave];
-  const int64_t base = int64_t(blockIdx.y) * per;
+  g += int64_t(blockIdx.y) * per;
+  mom += int64_t(blockIdx.y) * per;
   double sum = 0.0;
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < per; i += int64_t(kNormParts) * kThreads) {
-    const float gi = float(g[base + i]), m = mu * mom[base + i] + gi;
-    mom[base + i] = m;
-    const double u = nesterov ? gi + mu * m : m;
-    sum += u * u;
+  for (int64_t i = (int64_t(blockIdx.x) * kThreads + threadIdx.x) * 8; i < per; i += int64_t(kNormParts) * kThreads * 8) {
+    const int valid = per - i >= 8 ? 8 : int(per - i);
+    float e[8], m[8];
+    get<G, 8>(g + i, valid, e);
+    get<float, 8>(mom + i, valid, m);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m[j] = mu * m[j] + e[j];
+      const double u = nesterov ? e[j] + mu * m[j] : m[j];
+      sum += u * u;
+    }
+    put<float, 8>(mom + i, valid, m);
   }
   sum = wave_sum(sum);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
@@ -98,30 +106,36 @@ template <class G>
 __global__ __launch_bounds__(kThreads) void k_start(const G* g, const float* mom, int64_t rows, int64_t cols, int64_t ldx, float mu,
                                                     bool nesterov, const double* part, f16* x, f16* lo) {
   const int64_t b = blockIdx.y;
-  double v = part[b * kNormParts + (threadIdx.x & 63)];
+  double v = 0.0;
+#pragma unroll
+  for (int i = 0; i < kNormParts / kWave; ++i) v += part[b * kNormParts + i * kWave + (threadIdx.x & 63)];
   v = wave_sum(v);
   const float inv = kX / (float(sqrt(v)) + kNormEps);
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows * ldx; i += int64_t(gridDim.x) * kThreads) {
-    const int64_t r = i / ldx, c = i % ldx;
-    float e = 0.0f;
-    if (c < cols) {
-      const int64_t at = (b * rows + r) * cols + c;
-      const float m = mom[at];
-      e = (nesterov ? float(g[at]) + mu * m : m) * inv;
+  const unsigned pieces = unsigned(ldx / 8);
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows * pieces; i += int64_t(gridDim.x) * kThreads) {
+    const int64_t r = i / pieces, c = (i - r * pieces) * 8, at = (b * rows + r) * cols + c;
+    const int valid = cols - c >= 8 ? 8 : int(cols - c);
+    float e[8], m[8];
+    get<float, 8>(mom + at, valid, m);
+    if (nesterov) get<G, 8>(g + at, valid, e);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m[j] = (nesterov ? e[j] + mu * m[j] : m[j]) * inv;
+      m[j] = j < valid ? m[j] : 0.0f;  // infinities and NaN in g must not reach the padding
+      e[j] = m[j] - float(f16(m[j]));
     }
-    const f16 hi = f16(e);
-    x[b * rows * ldx + i] = hi;
-    lo[b * rows * ldx + i] = f16(e - float(hi));
+    put<f16, 8>(x + (b * rows + r) * ldx + c, 8, m);
+    put<f16, 8>(lo + (b * rows + r) * ldx + c, 8, e);
   }
 }
-
-struct None {};
 
 // Clears what pads the rows of a matrix [rows, cols] of row length ld.
 __global__ void k_clear_pads(f16* p, int64_t rows, int64_t cols, int64_t ld) {
   const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, pad = ld - cols;
   if (i < rows * pad) p[i / pad * ld + cols + i % pad] = f16(0.0f);
 }
+
+struct None {};
 
 // P = X X^T without its diagonal, which goes to d.  Only tiles on or below the diagonal are computed, and each
 // entry below it is written to its mirrored place too.
@@ -250,7 +264,7 @@ int update(const G* g, float* mom, const Shape& h, float mu, bool nesterov, int 
   const int64_t per = h.rows * h.cols;
   const unsigned z = unsigned(h.count);
   k_momentum<G><<<dim3(kNormParts, z), kThreads, 0, st>>>(g, mom, per, mu, nesterov, w.part);
-  k_start<G><<<dim3(blocks_of(h.rows * h.ldx), z), kThreads, 0, st>>>(g, mom, h.rows, h.cols, h.ldx, mu, nesterov, w.part, w.x[0],
+  k_start<G><<<dim3(blocks_of(h.rows * h.ldx / 8), z), kThreads, 0, st>>>(g, mom, h.rows, h.cols, h.ldx, mu, nesterov, w.part, w.x[0],
                                                                    w.lo[0]);
   int rc = launched();
   if (steps == 0) {
