@@ -24,16 +24,17 @@ struct GemmArgs {
   float* part = nullptr;
 };
 
-// A workgroup's tile and its wavefronts: WM by WN of them, each with BM / WM by BN / WN of the tile; STAGES k tiles in
-// LDS, all but one of them on their way (a power of two); through registers, DEPTH k tiles on their way.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int DEPTH_>
+// A workgroup's tile and its wavefronts: WM by WN of them, each with BM / WM by BN / WN of the tile, WK times over: each
+// such group takes every WK-th k tile, and their sums are added in LDS.  STAGES k tiles of a group are in LDS, all but
+// one of them on their way (a power of two); through registers, DEPTH k tiles are.
+template <int BM_, int BN_, int WM_, int WN_, int WK_, int STAGES_, int DEPTH_>
 struct Config {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, FM = BM / WM / 16, FN = BN / WN / 16, THREADS = 64 * WM * WN;
-  static constexpr int STAGES = STAGES_, DEPTH = DEPTH_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WK = WK_, FM = BM / WM / 16, FN = BN / WN / 16;
+  static constexpr int GROUP = 64 * WM * WN, THREADS = GROUP * WK, STAGES = STAGES_, DEPTH = DEPTH_;
 };
-typedef Config<256, 256, 2, 4, 2, 0> Large;   // 128 KiB of LDS, two wavefronts on a SIMD: a CU to itself
-typedef Config<128, 128, 2, 2, 4, 1> Medium;  // 128 KiB
-typedef Config<64, 64, 2, 2, 8, 4> Small;     // 128 KiB
+typedef Config<256, 256, 2, 4, 1, 2, 0> Large;   // 128 KiB of LDS, two wavefronts on a SIMD: a CU to itself
+typedef Config<128, 128, 2, 2, 2, 2, 1> Medium;  // 128 KiB, two wavefronts on a SIMD
+typedef Config<64, 64, 2, 2, 4, 2, 1> Small;     // 128 KiB, four wavefronts on a SIMD
 
 // One operand tile in LDS: R rows of kBK.  Chunks of 16 bytes are kept at swizzled places, so that the 16 lanes
 // that read one column of chunks meet 16 different bank groups.
@@ -101,11 +102,11 @@ struct Direct {
   unsigned off[kLoads];
   int kk;  // KC: the k of this lane's chunks within the tile
 
-  __device__ void init(const T*, int64_t ld, int64_t r0, int64_t rows, int) {
+  __device__ void init(int tid, int64_t ld, int64_t r0, int64_t rows) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       int row, k;
-      Ti::at(j * THREADS + threadIdx.x, row, k);
+      Ti::at(j * THREADS + tid, row, k);
       off[j] = KC ? unsigned(row) * unsigned(ld * 2) + k * 2 : unsigned(k) * unsigned(ld * 2) + row * 2;
       if (!KC && r0 + row >= rows) off[j] = kNowhere;
       if (KC) kk = k;  // the same for every j: a pass of THREADS chunks is a multiple of 16 rows
@@ -150,14 +151,14 @@ struct Staged {
   static constexpr int kLoads = Ti::kChunks / THREADS;
   u32x4 v[kLoads];
 
-  __device__ void load(const T* p, int64_t ld, int64_t r0, int64_t rows, int t, int ks) {
+  __device__ void load(int tid, const T* p, int64_t ld, int64_t r0, int64_t rows, int t, int ks) {
     const int64_t k0 = int64_t(t) * kBK;
     const int64_t length = KC ? ks : rows;  // of the contiguous side
     const bool inside = r0 + R <= rows && k0 + kBK <= ks;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       int row, k;
-      Ti::at(j * THREADS + threadIdx.x, row, k);
+      Ti::at(j * THREADS + tid, row, k);
       const int64_t gr = r0 + row, gk = k0 + k;
       if (inside) {
         __builtin_memcpy(&v[j], KC ? p + gr * ld + gk : p + gk * ld + gr, 16);
@@ -179,9 +180,9 @@ struct Staged {
       }
     }
   }
-  __device__ void store(char* lds) const {
+  __device__ void store(int tid, char* lds) const {
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(lds + (j * THREADS + threadIdx.x) * 16) = v[j];
+    for (int j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(lds + (j * THREADS + tid) * 16) = v[j];
   }
 };
 
@@ -227,11 +228,12 @@ __device__ inline void tile_of(int id, const GemmArgs& g, int& tm, int& tn) {
   }
 }
 
-// What a lane has of a tile: FN products' four neighbours each, of FM rows.  The epilogue takes them W at a time.
-template <class C, bool PERM, class Epi>
-__device__ inline void finish(const f32x4 (&acc)[C::FM][C::FN], const Epi& epi, int64_t m0, int64_t n0, int z, const GemmArgs& g) {
-  constexpr int W = PERM ? 8 : 4, GROUPS = C::FN * 4 / W;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// What a lane has of a tile: FN products' four neighbours each, of FM rows.  The epilogue takes them W at a time, from
+// row i0 on every STEP-th; what it reads of memory is asked for four rows at a time, before anything of them is written.
+template <class C, bool PERM, int STEP, class Epi>
+__device__ inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0, int64_t n0, int z, const GemmArgs& g) {
+  constexpr int W = PERM ? 8 : 4, GROUPS = C::FN * 4 / W, ROWS = (C::FM + STEP - 1) / STEP, BATCH = 4;
+  const int lane = threadIdx.x & 63, wave = (threadIdx.x % C::GROUP) >> 6;
   const int64_t mw = m0 + (wave / C::WN) * (C::BM / C::WM) + (lane & 15);
   const int64_t nw = n0 + (wave % C::WN) * (C::BN / C::WN) + (lane >> 4) * W;
   const bool full = m0 + C::BM <= g.m && n0 + C::BN <= g.n;
@@ -241,12 +243,26 @@ __device__ inline void finish(const f32x4 (&acc)[C::FM][C::FN], const Epi& epi, 
     const int valid = full || g.n - n >= W ? W : g.n > n ? int(g.n - n) : 0;
     const auto col = epi.template column<W>(n, valid, z, g);
 #pragma unroll
-    for (int i = 0; i < C::FM; ++i) {
-      float v[W];
+    for (int h = 0; h < ROWS; h += BATCH) {
+      typename Epi::template Read<W> in[BATCH];
 #pragma unroll
-      for (int j = 0; j < W; ++j) v[j] = acc[i][q * (W / 4) + j / 4][j & 3];
-      const int64_t m = mw + 16 * i;
-      if (full || (m < g.m && valid > 0)) epi.template row<W>(m, n, v, valid, col, z, g);
+      for (int i = h; i < ROWS && i < h + BATCH; ++i) {
+        const int64_t m = mw + 16 * (i0 + i * STEP);
+        if (full || (m < g.m && valid > 0)) in[i - h] = epi.template read<W>(m, n, valid, z, g);
+      }
+#pragma unroll
+      for (int i = h; i < ROWS && i < h + BATCH; ++i) {
+        const int64_t m = mw + 16 * (i0 + i * STEP);
+        float v[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          v[j] = 0.0f;
+#pragma unroll
+          for (int k = 0; k < C::FM; ++k)  // acc is indexed by constants only
+            if (k == i0 + i * STEP) v[j] = acc[k][q * (W / 4) + j / 4][j & 3];
+        }
+        if (full || (m < g.m && valid > 0)) epi.template row<W>(m, n, v, valid, col, in[i - h], z, g);
+      }
     }
   }
 }
@@ -265,8 +281,9 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
   typedef Tile<T, C::BN, BKC, PERM> TB;
   constexpr int BUF = TA::kBytes + TB::kBytes, kReads = FM * (AKC ? 1 : 2) + FN * (BKC ? 1 : 2);
   typedef typename Vec<T>::x8 x8;
-  constexpr int BUFS = DIRECT ? C::STAGES : 2, LOADS = (TA::kChunks + TB::kChunks) / C::THREADS;
-  __shared__ __attribute__((aligned(1024))) char lds[BUFS * BUF];
+  constexpr int BUFS = DIRECT ? C::STAGES : 2, LOADS = (TA::kChunks + TB::kChunks) / C::GROUP;
+  constexpr int SUMS = C::WK > 1 ? FM * FN * 16 * C::THREADS : 0, BYTES = C::WK * BUFS * BUF;
+  __shared__ __attribute__((aligned(1024))) char all_lds[BYTES > SUMS ? BYTES : SUMS];
   int id = run_of(blockIdx.x, gridDim.x), tm, tn;
   const int z = id / (g.tiles * g.splits);
   id -= z * g.tiles * g.splits;
@@ -275,10 +292,14 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
   const T* a = static_cast<const T*>(g.a) + z * g.stride_a;
   const T* b = static_cast<const T*>(g.b) + z * g.stride_b;
   const int64_t m0 = int64_t(tm) * C::BM, n0 = int64_t(tn) * C::BN;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / C::GROUP), tid = threadIdx.x % C::GROUP;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  char* const lds = all_lds + group * (BUFS * BUF);
   const int wm = (wave / C::WN) * (C::BM / C::WM), wn = (wave % C::WN) * (C::BN / C::WN);
   const int t0 = split * g.span, ks = int(g.k) < (t0 + g.span) * kBK ? int(g.k) : (t0 + g.span) * kBK;
-  const int t1 = (ks + kBK - 1) / kBK;
+  // a group's tiles are t0 + group, + WK, ..., numbered 0 to passes; past the last k tile the operands are 0
+  const int passes = ((ks + kBK - 1) / kBK - t0 + C::WK - 1) / C::WK;
+  const auto tile_at = [&](int t) { return t0 + t * C::WK + group; };
   f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -299,26 +320,26 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
       for (int j = 0; j < FN; ++j) acc[i][j] = mfma(fb[j], fa[i], acc[i][j]);
   };
   if constexpr (DIRECT) {
-    Direct<T, TA, C::BM, AKC, C::THREADS> la;
-    Direct<T, TB, C::BN, BKC, C::THREADS> lb;
-    la.init(a, g.lda, m0, g.m, ks);
-    lb.init(b, g.ldb, n0, g.n, ks);
+    Direct<T, TA, C::BM, AKC, C::GROUP> la;
+    Direct<T, TB, C::BN, BKC, C::GROUP> lb;
+    la.init(tid, g.lda, m0, g.m);
+    lb.init(tid, g.ldb, n0, g.n);
     const auto fetch = [&](int t) {
       char* to = lds + (t & (BUFS - 1)) * BUF;
-      la.issue(to, a, g.lda, m0, g.m, t, ks, wave);
-      lb.issue(to + TA::kBytes, b, g.ldb, n0, g.n, t, ks, wave);
+      la.issue(to, a, g.lda, m0, g.m, tile_at(t), ks, wave);
+      lb.issue(to + TA::kBytes, b, g.ldb, n0, g.n, tile_at(t), ks, wave);
     };
-    if (t0 < t1) {
+    if (passes > 0) {
 #pragma unroll
       for (int i = 0; i < BUFS; ++i) {
         if (i == BUFS - 1) {
           asm volatile("s_waitcnt vmcnt(%0)" ::"n"((BUFS - 2) * LOADS) : "memory");
           __builtin_amdgcn_s_barrier();
         }
-        fetch(t0 + i);
+        fetch(i);
       }
-      read(a0, b0, t0, 0);
-      for (int t = t0; t < t1; ++t) {
+      read(a0, b0, 0, 0);
+      for (int t = 0; t < passes; ++t) {
         read(a1, b1, t, 1);
         multiply(a0, b0);
         Order<0, kReads, FM * FN>::apply();
@@ -334,75 +355,96 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
   } else {
-    Staged<T, TA, C::BM, AKC, C::THREADS> la[C::DEPTH];
-    Staged<T, TB, C::BN, BKC, C::THREADS> lb[C::DEPTH];
-    if (t0 < t1) {
+    Staged<T, TA, C::BM, AKC, C::GROUP> la[C::DEPTH];
+    Staged<T, TB, C::BN, BKC, C::GROUP> lb[C::DEPTH];
+    if (passes > 0) {
       const auto load = [&](int t, int i) {
-        if (t >= t1) return;
-        la[i].load(a, g.lda, m0, g.m, t, ks);
-        lb[i].load(b, g.ldb, n0, g.n, t, ks);
+        if (t >= passes) return;
+        la[i].load(tid, a, g.lda, m0, g.m, tile_at(t), ks);
+        lb[i].load(tid, b, g.ldb, n0, g.n, tile_at(t), ks);
       };
       const auto store = [&](int t, int i) {
-        if (t >= t1) return;
+        if (t >= passes) return;
         char* to = lds + (t & (BUFS - 1)) * BUF;
-        la[i].store(to);
-        lb[i].store(to + TA::kBytes);
+        la[i].store(tid, to);
+        lb[i].store(tid, to + TA::kBytes);
       };
-      load(t0, 0);
-      store(t0, 0);
+      load(0, 0);
+      store(0, 0);
 #pragma unroll
-      for (int i = 0; i < C::DEPTH; ++i) load(t0 + 1 + i, i);
+      for (int i = 0; i < C::DEPTH; ++i) load(1 + i, i);
       __syncthreads();
-      read(a0, b0, t0, 0);
-      for (int tt = t0; tt < t1; tt += C::DEPTH) {
+      read(a0, b0, 0, 0);
+      for (int tt = 0; tt < passes; tt += C::DEPTH) {
 #pragma unroll
         for (int i = 0; i < C::DEPTH; ++i) {
           const int t = tt + i;
-          if (t >= t1) break;
+          if (t >= passes) break;
           read(a1, b1, t, 1);
           multiply(a0, b0);
           store(t + 1, i);
           load(t + 1 + C::DEPTH, i);
           __syncthreads();
-          if (t + 1 < t1) read(a0, b0, t + 1, 0);
+          if (t + 1 < passes) read(a0, b0, t + 1, 0);
           multiply(a1, b1);
         }
       }
     }
   }
-  if (g.splits > 1) {
-    f32x4* to = reinterpret_cast<f32x4*>(g.part) + ((int64_t(z) * g.tiles + tile) * g.splits + split) * (FM * FN * C::THREADS) + threadIdx.x;
+  if constexpr (C::WK > 1) {  // the groups' sums, in their order: every group gets the rows that it finishes
+    __syncthreads();
+    f32x4* sums = reinterpret_cast<f32x4*>(all_lds);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) to[(i * FN + j) * C::THREADS] = acc[i][j];
+      for (int j = 0; j < FN; ++j) sums[((i * FN + j) * C::WK + group) * C::GROUP + tid] = acc[i][j];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+      if (i % C::WK == group)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          acc[i][j] = sums[(i * FN + j) * C::WK * C::GROUP + tid];
+#pragma unroll
+          for (int k = 1; k < C::WK; ++k) acc[i][j] += sums[((i * FN + j) * C::WK + k) * C::GROUP + tid];
+        }
+    if (group >= FM) return;
+  }
+  if (g.splits > 1) {
+    f32x4* to = reinterpret_cast<f32x4*>(g.part) + ((int64_t(z) * g.tiles + tile) * g.splits + split) * (FM * FN * C::GROUP) + tid;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+      if (i % C::WK == group)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) to[(i * FN + j) * C::GROUP] = acc[i][j];
     return;
   }
-  finish<C, PERM>(acc, epi, m0, n0, z, g);
+  finish<C, PERM, C::WK>(acc, group, epi, m0, n0, z, g);
 #endif
 }
 
-// The splits of a product, added in their order, and its epilogue: one workgroup a tile, its lanes as in k_gemm.
+// The splits of a product, added in their order, and its epilogue: a workgroup a tile, its lanes as one group of k_gemm.
 template <class C, bool BKC, class Epi>
-__global__ __launch_bounds__(C::THREADS) void k_join(GemmArgs g, Epi epi) {
+__global__ __launch_bounds__(C::GROUP) void k_join(GemmArgs g, Epi epi) {
   int tm, tn;
   const int z = blockIdx.x / g.tiles, tile = blockIdx.x % g.tiles;
   tile_of<Epi::kSymmetric>(tile, g, tm, tn);
   const f32x4* from =
-      reinterpret_cast<const f32x4*>(g.part) + (int64_t(z) * g.tiles + tile) * g.splits * (C::FM * C::FN * C::THREADS) + threadIdx.x;
+      reinterpret_cast<const f32x4*>(g.part) + (int64_t(z) * g.tiles + tile) * g.splits * (C::FM * C::FN * C::GROUP) + threadIdx.x;
   f32x4 acc[C::FM][C::FN];
 #pragma unroll
   for (int i = 0; i < C::FM; ++i)
 #pragma unroll
-    for (int j = 0; j < C::FN; ++j) acc[i][j] = from[(i * C::FN + j) * C::THREADS];
+    for (int j = 0; j < C::FN; ++j) acc[i][j] = from[(i * C::FN + j) * C::GROUP];
+#pragma unroll 4
   for (int s = 1; s < g.splits; ++s) {
-    from += C::FM * C::FN * C::THREADS;
+    from += C::FM * C::FN * C::GROUP;
 #pragma unroll
     for (int i = 0; i < C::FM; ++i)
 #pragma unroll
-      for (int j = 0; j < C::FN; ++j) acc[i][j] += from[(i * C::FN + j) * C::THREADS];
+      for (int j = 0; j < C::FN; ++j) acc[i][j] += from[(i * C::FN + j) * C::GROUP];
   }
-  finish<C, BKC && C::FN % 2 == 0>(acc, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
+  finish<C, BKC && C::FN % 2 == 0, 1>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
 }
 
 inline int64_t tiles_of(int64_t m, int64_t n, int bm, int bn, bool symmetric) {
@@ -453,7 +495,7 @@ int launch(GemmArgs g, const Epi& epi, hipStream_t st) {
   else
     return launch<T, Medium, AKC, BKC>(g, epi, st);  // a tile's registers would not fit
   if constexpr (C::BM == 64)
-    if (g.splits > 1) k_join<C, BKC, Epi><<<blocks, C::THREADS, 0, st>>>(g, epi);
+    if (g.splits > 1) k_join<C, BKC, Epi><<<blocks, C::GROUP, 0, st>>>(g, epi);
   return launched();
 }
 
@@ -497,9 +539,11 @@ __device__ inline void put(T* p, int valid, const float (&v)[W]) {
   }
 }
 
+// What an epilogue keeps of its W columns, or reads of a row of them.
 template <int W>
-struct Column {  // what an epilogue keeps of its W columns
+struct Column {
   float v[W];
 };
+struct None {};
 
 }  // namespace xops

@@ -50,18 +50,31 @@ struct LinearEpilogue {
     return c;
   }
   template <int W>
-  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& c, int, const GemmArgs&) const {
+  struct Read {  // of the residual, as it lies: half the registers
+    T v[W];
+  };
+  template <int W>
+  __device__ Read<W> read(int64_t m, int64_t n, int valid, int, const GemmArgs&) const {
+    Read<W> e;
+    if (!r) return e;
+    if (valid == W) {
+      __builtin_memcpy(e.v, r + m * ldr + n, sizeof(e.v));
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; ++j) e.v[j] = j < valid ? r[m * ldr + n + j] : T(0.0f);
+    }
+    return e;
+  }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& c, const Read<W>& e, int, const GemmArgs&) const {
 #pragma unroll
     for (int j = 0; j < W; ++j) v[j] += c.v[j];
     if (z) put<T, W>(z + m * ldz + n, valid, v);
 #pragma unroll
     for (int j = 0; j < W; ++j) v[j] = activate(v[j], act);
-    if (r) {
-      float e[W];
-      get<T, W>(r + m * ldr + n, valid, e);
+    if (r)
 #pragma unroll
-      for (int j = 0; j < W; ++j) v[j] += e[j];
-    }
+      for (int j = 0; j < W; ++j) v[j] += float(e.v[j]);
     put<T, W>(y + m * ldy + n, valid, v);
   }
 };
@@ -72,11 +85,13 @@ struct StoreEpilogue {
   T* y;
   int64_t ldy;
 
-  struct None {};
+  template <int W> using Read = None;
   template <int W>
   __device__ None column(int64_t, int, int, const GemmArgs&) const { return {}; }
   template <int W>
-  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, None, int, const GemmArgs&) const {
+  __device__ None read(int64_t, int64_t, int, int, const GemmArgs&) const { return {}; }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, None, None, int, const GemmArgs&) const {
     put<T, W>(y + m * ldy + n, valid, v);
   }
 };

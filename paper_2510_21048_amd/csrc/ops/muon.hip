@@ -135,8 +135,6 @@ __global__ void k_clear_pads(f16* p, int64_t rows, int64_t cols, int64_t ld) {
   if (i < rows * pad) p[i / pad * ld + cols + i % pad] = f16(0.0f);
 }
 
-struct None {};
-
 // P = X X^T without its diagonal, which goes to d.  Only tiles on or below the diagonal are computed, and each
 // entry below it is written to its mirrored place too.
 struct GramEpilogue {
@@ -147,8 +145,11 @@ struct GramEpilogue {
 
   template <int W>
   __device__ None column(int64_t, int, int, const GemmArgs&) const { return {}; }
+  template <int W> using Read = None;
   template <int W>
-  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, None, int z, const GemmArgs& g) const {
+  __device__ None read(int64_t, int64_t, int, int, const GemmArgs&) const { return {}; }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, None, None, int z, const GemmArgs& g) const {
     f16* to = p + z * g.m * ld;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
@@ -188,16 +189,28 @@ struct PolyEpilogue {
     return c;
   }
   template <int W>
-  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& dn, int z, const GemmArgs& g) const {
+  struct Read {  // as it lies: half the registers
+    typedef f16 part __attribute__((ext_vector_type(W)));
+    part e;
+    float dm;
+  };
+  template <int W>
+  __device__ Read<W> read(int64_t m, int64_t n, int, int z, const GemmArgs& g) const {
+    Read<W> r;
+    r.dm = dp[z * g.m + m];
+    // a row's storage is a multiple of 8 long: whole pieces, whatever of them is the matrix
+    __builtin_memcpy(&r.e, p + (z * g.m + m) * ld + n, sizeof(r.e));
+    return r;
+  }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& dn, const Read<W>& r, int z, const GemmArgs& g) const {
     if (n > m) return;
-    const float dm = dp[z * g.m + m];
-    float e[W];
-    get<f16, W>(p + z * g.m * ld + m * ld + n, valid, e);
+    const float dm = r.dm;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       if (n + j == m) dq[z * g.m + m] = XMEM_NS_B * dm + XMEM_NS_C * (v[j] * (1.0f / (kP * kP)) + dm * dm);
       // times kP; E_ii is 0
-      v[j] = n + j == m ? 0.0f : XMEM_NS_B * e[j] + XMEM_NS_C * (v[j] * (1.0f / kP) + (dm + dn.v[j]) * e[j]);
+      v[j] = n + j == m ? 0.0f : XMEM_NS_B * float(r.e[j]) + XMEM_NS_C * (v[j] * (1.0f / kP) + (dm + dn.v[j]) * float(r.e[j]));
     }
     GramEpilogue::mirror<W>(q + z * g.m * ld, ld, m, n, v, valid);
   }
@@ -222,14 +235,28 @@ struct StepEpilogue {
     return c;
   }
   template <int W>
-  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& dn, int z, const GemmArgs& g) const {
+  struct Read {  // as they lie: half the registers
+    typedef f16 part __attribute__((ext_vector_type(W)));
+    part hi, lo;
+    float dm;
+  };
+  template <int W>
+  __device__ Read<W> read(int64_t m, int64_t n, int, int z, const GemmArgs& g) const {
     const int64_t at = (z * g.m + m) * ld + n;
-    const float dm = TALL ? 0.0f : XMEM_NS_A + dq[z * s + m];
-    float hi[W], rest[W];
-    get<f16, W>(x + at, valid, hi);
-    get<f16, W>(lo + at, valid, rest);
+    Read<W> r;
+    r.dm = TALL ? 0.0f : XMEM_NS_A + dq[z * s + m];
+    // a row's storage is a multiple of 8 long: whole pieces, whatever of them is the matrix
+    __builtin_memcpy(&r.hi, x + at, sizeof(r.hi));
+    __builtin_memcpy(&r.lo, lo + at, sizeof(r.lo));
+    return r;
+  }
+  template <int W>
+  __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& dn, const Read<W>& r, int z, const GemmArgs& g) const {
+    const int64_t at = (z * g.m + m) * ld + n;
+    float rest[W];
 #pragma unroll
-    for (int j = 0; j < W; ++j) v[j] = (TALL ? dn.v[j] : dm) * (hi[j] + rest[j]) + v[j] * (1.0f / kP);  // times kX
+    for (int j = 0; j < W; ++j)
+      v[j] = (TALL ? dn.v[j] : r.dm) * (float(r.hi[j]) + float(r.lo[j])) + v[j] * (1.0f / kP);  // times kX
     if (out) {
 #pragma unroll
       for (int j = 0; j < W; ++j) v[j] *= scale / kX;
