@@ -229,42 +229,42 @@ __device__ inline void tile_of(int id, const GemmArgs& g, int& tm, int& tn) {
 }
 
 // What a lane has of a tile: FN products' four neighbours each, of FM rows.  The epilogue takes them W at a time, from
-// row i0 on every STEP-th; what it reads of memory is asked for four rows at a time, before anything of them is written.
-template <class C, bool PERM, int STEP, class Epi>
+// row i0 on every STEP-th; what it reads of memory is asked for four rows at a time, before anything of them is
+// written.  The Q-th W columns of a lane; recursive, so that acc is indexed by constants however long the epilogue is.
+template <class C, bool PERM, int STEP, int Q, class Epi>
 __device__ inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0, int64_t n0, int z, const GemmArgs& g) {
-  constexpr int W = PERM ? 8 : 4, GROUPS = C::FN * 4 / W, ROWS = (C::FM + STEP - 1) / STEP, BATCH = 4;
+  constexpr int W = PERM ? 8 : 4, GROUPS = C::FN * 4 / W, ROWS = (C::FM + STEP - 1) / STEP, BATCH = ROWS < 4 ? ROWS : 4;
+  static_assert(ROWS % BATCH == 0);
   const int lane = threadIdx.x & 63, wave = (threadIdx.x % C::GROUP) >> 6;
   const int64_t mw = m0 + (wave / C::WN) * (C::BM / C::WM) + (lane & 15);
-  const int64_t nw = n0 + (wave % C::WN) * (C::BN / C::WN) + (lane >> 4) * W;
+  const int64_t n = n0 + (wave % C::WN) * (C::BN / C::WN) + (lane >> 4) * W + Q * 4 * W;
   const bool full = m0 + C::BM <= g.m && n0 + C::BN <= g.n;
+  const int valid = full || g.n - n >= W ? W : g.n > n ? int(g.n - n) : 0;
+  const auto col = epi.template column<W>(n, valid, z, g);
 #pragma unroll
-  for (int q = 0; q < GROUPS; ++q) {
-    const int64_t n = nw + q * 4 * W;
-    const int valid = full || g.n - n >= W ? W : g.n > n ? int(g.n - n) : 0;
-    const auto col = epi.template column<W>(n, valid, z, g);
+  for (int h = 0; h < ROWS / BATCH; ++h) {
+    typename Epi::template Read<W> in[BATCH];
 #pragma unroll
-    for (int h = 0; h < ROWS; h += BATCH) {
-      typename Epi::template Read<W> in[BATCH];
+    for (int i = 0; i < BATCH; ++i) {
+      const int64_t m = mw + 16 * (i0 + (h * BATCH + i) * STEP);
+      if (full || (m < g.m && valid > 0)) in[i] = epi.template read<W>(m, n, valid, z, g);
+    }
 #pragma unroll
-      for (int i = h; i < ROWS && i < h + BATCH; ++i) {
-        const int64_t m = mw + 16 * (i0 + i * STEP);
-        if (full || (m < g.m && valid > 0)) in[i - h] = epi.template read<W>(m, n, valid, z, g);
+    for (int i = 0; i < BATCH; ++i) {
+      const int64_t m = mw + 16 * (i0 + (h * BATCH + i) * STEP);
+      float v[W];
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        v[j] = acc[h * BATCH + i][Q * (W / 4) + j / 4][j & 3];
+        if constexpr (STEP > 1)
+#pragma unroll
+          for (int k = 0; k < C::FM; ++k)
+            if (k == i0 + (h * BATCH + i) * STEP) v[j] = acc[k][Q * (W / 4) + j / 4][j & 3];
       }
-#pragma unroll
-      for (int i = h; i < ROWS && i < h + BATCH; ++i) {
-        const int64_t m = mw + 16 * (i0 + i * STEP);
-        float v[W];
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-          v[j] = 0.0f;
-#pragma unroll
-          for (int k = 0; k < C::FM; ++k)  // acc is indexed by constants only
-            if (k == i0 + i * STEP) v[j] = acc[k][q * (W / 4) + j / 4][j & 3];
-        }
-        if (full || (m < g.m && valid > 0)) epi.template row<W>(m, n, v, valid, col, in[i - h], z, g);
-      }
+      if (full || (m < g.m && valid > 0)) epi.template row<W>(m, n, v, valid, col, in[i], z, g);
     }
   }
+  if constexpr (Q + 1 < GROUPS) finish<C, PERM, STEP, Q + 1>(acc, i0, epi, m0, n0, z, g);
 }
 
 // One workgroup's tile.  Half a tile's operands are in registers ahead of the matrix instructions: while the products of
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
         for (int j = 0; j < FN; ++j) to[(i * FN + j) * C::GROUP] = acc[i][j];
     return;
   }
-  finish<C, PERM, C::WK>(acc, group, epi, m0, n0, z, g);
+  finish<C, PERM, C::WK, 0>(acc, group, epi, m0, n0, z, g);
 #endif
 }
 
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(C::GROUP) void k_join(GemmArgs g, Epi epi) {
 #pragma unroll
       for (int j = 0; j < C::FN; ++j) acc[i][j] += from[(i * C::FN + j) * C::GROUP];
   }
-  finish<C, BKC && C::FN % 2 == 0, 1>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
+  finish<C, BKC && C::FN % 2 == 0, 1, 0>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
 }
 
 inline int64_t tiles_of(int64_t m, int64_t n, int bm, int bn, bool symmetric) {

@@ -9,8 +9,8 @@
 // entries normal.  Three things hold the error near 7e-4 of the update (its bfloat16 rounding: 1.7e-3):
 //   - the diagonals of P and Q, which are far larger than the rest, are kept apart in 32 bits and the products take
 //     the matrices without them: (P P)_ij = (E E)_ij + (d_i + d_j) E_ij, and + d_i^2 on the diagonal;
-//   - the linear terms (a + q_ii) X_i take X from two halves of 11 bits, so that directions in which the
-//     gradient is weak, which a step multiplies by a, are not lost in the rounding of the strong ones;
+//   - the linear terms (a + q_ii) X_i take X from two halves of 11 bits (but in the last two steps), so that directions in
+//     which the gradient is weak, which a step multiplies by a, are not lost in the rounding of the strong ones;
 //   - Q is made from the same rounded P in both terms: b + 2 c p is near 0 where P is near 1, so that its error cancels.
 // On matrices of normal values the products alone, in bfloat16, leave 1e-2; in half precision without these, 1.5e-3;
 // where one direction holds most of a gradient, 1.6e-1 and 2e-2.
@@ -23,6 +23,9 @@ namespace {
 constexpr float kX = 256.0f, kP = 1024.0f;
 constexpr float kNormEps = 1e-7f;
 constexpr int kThreads = 256;
+// The steps at the end whose X is kept in one half: a rounding there is multiplied by a^2 at most, and on a gradient of
+// 16 strong directions over weak ones the error goes from 4e-4 to 1.3e-3; each such step moves 4 of 8 bytes less.
+constexpr int kOneHalf = 2;
 constexpr int kNormParts = 256;  // workgroups whose sums make one matrix's norm
 constexpr int64_t kMostCount = 65535, kMostSide = int64_t(1) << 24;
 
@@ -220,7 +223,7 @@ struct PolyEpilogue {
 template <bool TALL>
 struct StepEpilogue {
   static constexpr bool kSymmetric = false;
-  const f16 *x, *lo;
+  const f16 *x, *lo;  // lo, nlo: NULL where X is kept in one half
   const float* dq;
   f16 *nx, *nlo;
   int64_t ld, s;
@@ -247,7 +250,10 @@ struct StepEpilogue {
     r.dm = TALL ? 0.0f : XMEM_NS_A + dq[z * s + m];
     // a row's storage is a multiple of 8 long: whole pieces, whatever of them is the matrix
     __builtin_memcpy(&r.hi, x + at, sizeof(r.hi));
-    __builtin_memcpy(&r.lo, lo + at, sizeof(r.lo));
+    if (lo)
+      __builtin_memcpy(&r.lo, lo + at, sizeof(r.lo));
+    else
+      r.lo = typename Read<W>::part(f16(0.0f));
     return r;
   }
   template <int W>
@@ -262,10 +268,12 @@ struct StepEpilogue {
       for (int j = 0; j < W; ++j) v[j] *= scale / kX;
       put<bf16, W>(out + (z * g.m + m) * g.n + n, valid, v);
     } else {
-#pragma unroll
-      for (int j = 0; j < W; ++j) rest[j] = v[j] - float(f16(v[j]));
       put<f16, W>(nx + at, valid, v);
-      put<f16, W>(nlo + at, valid, rest);
+      if (nlo) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) rest[j] = v[j] - float(f16(v[j]));
+        put<f16, W>(nlo + at, valid, rest);
+      }
     }
   }
 };
@@ -306,7 +314,7 @@ int update(const G* g, float* mom, const Shape& h, float mu, bool nesterov, int 
   clear(w.p, h.count * h.s, h.s, h.lds);
   clear(w.q, h.count * h.s, h.s, h.lds);
   for (int i = 0; i < steps && rc == XMEM_OK; ++i) {
-    const f16 *x = w.x[i & 1], *lo = w.lo[i & 1];
+    const f16 *x = w.x[i & 1], *lo = i == 0 || i < steps - kOneHalf ? w.lo[i & 1] : nullptr;
     bf16* to = i == steps - 1 ? out : nullptr;
     const auto args = [&](const f16* a, int64_t lda, int64_t sa, const f16* b, int64_t ldb, int64_t sb, int64_t m, int64_t n, int64_t k) {
       return GemmArgs{a, b, lda, ldb, sa, sb, m, n, k, true, true, h.count};
@@ -317,7 +325,7 @@ int update(const G* g, float* mom, const Shape& h, float mu, bool nesterov, int 
     rc = h.tall ? gemm<f16, false, false>(gram, ge, w.split, st) : gemm<f16, true, true>(gram, ge, w.split, st);
     if (rc == XMEM_OK) rc = gemm<f16, true, true>(args(w.p, h.lds, sp, w.p, h.lds, sp, h.s, h.s, h.s), pe, w.split, st);
     if (rc != XMEM_OK) break;
-    f16 *nx = w.x[~i & 1], *nlo = w.lo[~i & 1];
+    f16 *nx = w.x[~i & 1], *nlo = i + 1 < steps - kOneHalf ? w.lo[~i & 1] : nullptr;
     if (h.tall)
       rc = gemm<f16, true, true>(args(x, h.ldx, sx, w.q, h.lds, sp, h.l, h.s, h.s),
                                  StepEpilogue<true>{x, lo, w.dq, nx, nlo, h.ldx, h.s, to, scale}, w.split, st);
