@@ -20,6 +20,7 @@ ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 XMEM_NS_MAX_STEPS = 16
 
 _lib = None
+_dtypes: dict = {}  # torch's types -> the C ABI's, filled when the library is loaded
 
 
 def ops_lib_path() -> Path:
@@ -46,6 +47,8 @@ def load_ops():
         ):
             f = getattr(lib, name)
             f.argtypes, f.restype = args, res
+        import torch
+        _dtypes.update({torch.bfloat16: XMEM_BF16, torch.float16: XMEM_F16, torch.float32: XMEM_F32})
         _lib = lib
     return _lib
 
@@ -101,14 +104,16 @@ def xmem_muon_update(d_grad, grad_dtype, d_momentum, count, rows, cols, mu, nest
 # ---------------------------------------------------------------- on torch tensors
 
 
+# A small call costs its host as much as the GPU: these look at each tensor once, and ask torch for little.
+
+
 def _check(rc: int, what: str) -> None:
     if rc != XMEM_OK:
         raise XmemError(f"{what}: {xmem_strerror(rc)} ({rc})")
 
 
 def _dtype(t, what: str, allow=(XMEM_BF16, XMEM_F16)) -> int:
-    import torch
-    code = {torch.bfloat16: XMEM_BF16, torch.float16: XMEM_F16, torch.float32: XMEM_F32}.get(t.dtype)
+    code = _dtypes.get(t.dtype)
     if code not in allow:
         raise XmemError(f"{what}: {t.dtype} is not supported here")
     return code
@@ -116,41 +121,48 @@ def _dtype(t, what: str, allow=(XMEM_BF16, XMEM_F16)) -> int:
 
 def _matrix(t, what: str, rows: int | None = None, cols: int | None = None, dtype=None, device=None) -> int:
     """Row distance of a 2-d tensor whose rows are contiguous; raises on anything else."""
-    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise XmemError(f"{what}: shape {tuple(t.shape)} where ({'*' if rows is None else rows}, {'*' if cols is None else cols}) is wanted")
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        raise XmemError(f"{what}: shape {tuple(shape)} where ({'*' if rows is None else rows}, {'*' if cols is None else cols}) is wanted")
     if dtype is not None and t.dtype != dtype:
         raise XmemError(f"{what}: {t.dtype} where {dtype} is wanted")
     if not t.is_cuda or (device is not None and t.device != device):
         raise XmemError(f"{what}: on {t.device}" + ("" if device is None else f" where {device} is wanted"))
-    if t.shape[1] > 1 and t.stride(1) != 1 and t.numel():
+    r, c = shape
+    ld, along = t.stride()
+    if c > 1 and along != 1 and r:
         raise XmemError(f"{what}: its rows are not contiguous (strides {t.stride()})")
-    if t.shape[0] <= 1:
-        return t.shape[1]
-    if t.numel() and t.stride(0) < t.shape[1]:
-        raise XmemError(f"{what}: its rows overlap (strides {t.stride()})")
-    return max(t.stride(0), t.shape[1])
+    if r <= 1:
+        return c
+    if ld < c:
+        if c and r:
+            raise XmemError(f"{what}: its rows overlap (strides {t.stride()})")
+        return c
+    return ld
 
 
 def _vector(t, what: str, n: int, dtype, device):
-    if t is None:
-        return None
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or t.device != device or (n > 1 and t.stride(0) != 1):
+    if t is not None and (t.shape != (n,) or t.dtype != dtype or t.device != device or (n > 1 and t.stride(0) != 1)):
         raise XmemError(f"{what}: a contiguous {dtype} [{n}] on {device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
 
 
 def _workspace(workspace, need: int, device):
-    import torch
     if need == 0:
         return None, 0
     if workspace is None or workspace.numel() < need:
+        import torch
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
     return workspace, workspace.numel()
 
 
 def _raw_stream(device, stream) -> int:
+    if stream is not None:
+        return stream
     import torch
-    return torch.cuda.current_stream(device).cuda_stream if stream is None else stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # what current_stream() wraps, at a tenth of its time
+    index = device.index
+    return raw(index) if raw is not None and index is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _activation(name: str) -> int:
@@ -164,6 +176,7 @@ def linear_forward(x, w, bias=None, residual=None, activation: str = "none", sav
     float16 (rows may be strided), bias float32 [n].  Returns (y, z): z = x w^T + bias where save_z (what
     ``linear_backward`` needs of an activation), else None."""
     import torch
+    lib = load_ops()
     act, code, dev = _activation(activation), _dtype(x, "x"), x.device
     ldx, ldw = _matrix(x, "x"), _matrix(w, "w", None, x.shape[1], x.dtype, x.device)
     (m, k), n = x.shape, w.shape[0]
@@ -171,7 +184,7 @@ def linear_forward(x, w, bias=None, residual=None, activation: str = "none", sav
     _vector(bias, "bias", n, torch.float32, dev)
     y = torch.empty((m, n), dtype=x.dtype, device=dev)
     z = torch.empty((m, n), dtype=x.dtype, device=dev) if save_z else None
-    workspace, size = _workspace(workspace, xmem_linear_forward_workspace_bytes(m, n, k), dev)
+    workspace, size = _workspace(workspace, lib.xmem_linear_forward_workspace_bytes(m, n, k), dev)
     _check(xmem_linear_forward(x, ldx, w, ldw, bias, residual, ldr, m, n, k, code, act, y, n, z, n, workspace, size,
                                _raw_stream(dev, stream)), "xmem_linear_forward")
     return y, z
@@ -183,6 +196,7 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", need_dx: bool = 
     Returns (dx [m, k], dw [n, k], db float32 [n]), None in the place of what is not needed.  The residual's gradient
     is dy itself."""
     import torch
+    load_ops()
     act, code, dev = _activation(activation), _dtype(dy, "dy"), dy.device
     lddy = _matrix(dy, "dy")
     m, n = dy.shape
@@ -207,6 +221,7 @@ def token_logp(logits, tokens, weights=None, stream=None):
     """Log-probabilities float32 [t] of the tokens (int64 [t]) under logits [t, v] (bfloat16, float16 or float32, rows
     may be strided); 0 where the weight is."""
     import torch
+    load_ops()
     code, dev, ldl = _dtype(logits, "logits", _ANY), logits.device, _matrix(logits, "logits")
     t, v = logits.shape
     _vector(tokens, "tokens", t, torch.int64, dev)
@@ -225,6 +240,7 @@ def policy_loss(logits, tokens, weights, old_logp, advantages, ref_logp=None, cl
     [4]: loss, policy part, KL part, clipped weight; logp float32 [t]; dlogits, which is logits itself with in_place,
     or None)."""
     import torch
+    load_ops()
     code, dev, ldl = _dtype(logits, "logits", _ANY), logits.device, _matrix(logits, "logits")
     t, v = logits.shape
     _vector(tokens, "tokens", t, torch.int64, dev)
@@ -249,6 +265,7 @@ def muon_update(grad, momentum, mu: float = 0.95, nesterov: bool = True, steps: 
     """Momentum (float32, updated in place) and the orthogonalised update (bfloat16, returned) of matrices: grad
     [rows, cols] or [count, rows, cols], contiguous, bfloat16, float16 or float32."""
     import torch
+    load_ops()
     code, dev = _dtype(grad, "grad", _ANY), grad.device
     if grad.dim() not in (2, 3) or not grad.is_cuda or not grad.is_contiguous():
         raise XmemError("grad: a contiguous CUDA tensor of 2 or 3 dimensions is wanted")
