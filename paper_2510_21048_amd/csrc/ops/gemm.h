@@ -231,15 +231,20 @@ __device__ inline void tile_of(int id, const GemmArgs& g, int& tm, int& tn) {
 // What a lane has of a tile: FN products' four neighbours each, of FM rows.  The epilogue takes them W at a time, from
 // row i0 on every STEP-th; what it reads of memory is asked for four rows at a time, before anything of them is
 // written.  The Q-th W columns of a lane; recursive, so that acc is indexed by constants however long the epilogue is.
-template <class C, bool PERM, int STEP, int Q, class Epi>
-__device__ inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0, int64_t n0, int z, const GemmArgs& g) {
+// HOW says what is known of the tile before it runs: whole (nothing of it is past the matrix) and past the L2s.
+template <bool WHOLE_, bool PAST_L2_>
+struct How {
+  static constexpr bool WHOLE = WHOLE_, PAST_L2 = PAST_L2_;
+};
+template <class C, bool PERM, int STEP, int Q, class HOW, class Epi>
+__device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0,
+                                                             int64_t n0, int z, const GemmArgs& g) {
   constexpr int W = PERM ? 8 : 4, GROUPS = C::FN * 4 / W, ROWS = (C::FM + STEP - 1) / STEP, BATCH = ROWS < 4 ? ROWS : 4;
   static_assert(ROWS % BATCH == 0);
   const int lane = threadIdx.x & 63, wave = (threadIdx.x % C::GROUP) >> 6;
   const int64_t mw = m0 + (wave / C::WN) * (C::BM / C::WM) + (lane & 15);
   const int64_t n = n0 + (wave % C::WN) * (C::BN / C::WN) + (lane >> 4) * W + Q * 4 * W;
-  const bool full = m0 + C::BM <= g.m && n0 + C::BN <= g.n;
-  const int valid = full || g.n - n >= W ? W : g.n > n ? int(g.n - n) : 0;
+  const int valid = HOW::WHOLE || g.n - n >= W ? W : g.n > n ? int(g.n - n) : 0;
   const auto col = epi.template column<W>(n, valid, z, g);
 #pragma unroll
   for (int h = 0; h < ROWS / BATCH; ++h) {
@@ -247,7 +252,7 @@ __device__ inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Ep
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
       const int64_t m = mw + 16 * (i0 + (h * BATCH + i) * STEP);
-      if (full || (m < g.m && valid > 0)) in[i] = epi.template read<W>(m, n, valid, z, g);
+      if (HOW::WHOLE || (m < g.m && valid > 0)) in[i] = epi.template read<W>(m, n, valid, z, g);
     }
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
@@ -261,10 +266,20 @@ __device__ inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Ep
           for (int k = 0; k < C::FM; ++k)
             if (k == i0 + (h * BATCH + i) * STEP) v[j] = acc[k][Q * (W / 4) + j / 4][j & 3];
       }
-      if (full || (m < g.m && valid > 0)) epi.template row<W>(m, n, v, valid, col, in[i], z, g);
+      if (HOW::WHOLE || (m < g.m && valid > 0)) epi.template row<W, HOW>(m, n, v, valid, col, in[i], z, g);
     }
   }
-  if constexpr (Q + 1 < GROUPS) finish<C, PERM, STEP, Q + 1>(acc, i0, epi, m0, n0, z, g);
+  if constexpr (Q + 1 < GROUPS) finish<C, PERM, STEP, Q + 1, HOW>(acc, i0, epi, m0, n0, z, g);
+}
+// An epilogue's choices are made once a tile, so that the code a tile runs through is short: it passes the
+// instruction cache once for each.
+template <class C, bool PERM, int STEP, class Epi>
+__device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0,
+                                                             int64_t n0, int z, const GemmArgs& g) {
+  if (m0 + C::BM <= g.m && n0 + C::BN <= g.n)
+    epi.chosen([&](const auto& e) __attribute__((always_inline)) { finish<C, PERM, STEP, 0, How<true, PERM && C::BM == 256>>(acc, i0, e, m0, n0, z, g); });
+  else
+    finish<C, PERM, STEP, 0, How<false, false>>(acc, i0, epi, m0, n0, z, g);
 }
 
 // One workgroup's tile.  Half a tile's operands are in registers ahead of the matrix instructions: while the products of
@@ -419,7 +434,7 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
         for (int j = 0; j < FN; ++j) to[(i * FN + j) * C::GROUP] = acc[i][j];
     return;
   }
-  finish<C, PERM, C::WK, 0>(acc, group, epi, m0, n0, z, g);
+  finish<C, PERM, C::WK>(acc, group, epi, m0, n0, z, g);
 #endif
 }
 
@@ -444,7 +459,7 @@ __global__ __launch_bounds__(C::GROUP) void k_join(GemmArgs g, Epi epi) {
 #pragma unroll
       for (int j = 0; j < C::FN; ++j) acc[i][j] += from[(i * C::FN + j) * C::GROUP];
   }
-  finish<C, BKC && C::FN % 2 == 0, 1, 0>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
+  finish<C, BKC && C::FN % 2 == 0, 1>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
 }
 
 inline int64_t tiles_of(int64_t m, int64_t n, int bm, int bn, bool symmetric) {
@@ -525,19 +540,31 @@ __device__ inline void get(const T* p, int valid, float (&v)[W]) {
 #pragma unroll
   for (int j = 0; j < W; ++j) v[j] = float(e[j]);
 }
-template <class T, int W>
+// HOW::PAST_L2: an output of the 256 x 256 tiles (24 MiB and more) stays in no L2 anyway; written past them it leaves the operands
+// there.  8192 x 8192 and its pre-activation 283 -> 244 us, 24 steps of 8192 x 2048 18.1 -> 17.2 ms; one of 1024 x 1024,
+// which the next kernel reads, 162 -> 171 us.  Pieces of 8 bytes are left to the L2 to put together: 258 -> 387 us.
+template <class T, int W, class HOW>
 __device__ inline void put(T* p, int valid, const float (&v)[W]) {
   T e[W];
 #pragma unroll
   for (int j = 0; j < W; ++j) e[j] = T(v[j]);
-  if (valid == W) {
-    __builtin_memcpy(p, e, sizeof(e));
+  if (HOW::WHOLE || valid == W) {
+    if constexpr (HOW::PAST_L2) {
+      typedef unsigned any4 __attribute__((ext_vector_type(4), aligned(2)));
+      static_assert(sizeof(e) == 16);
+      any4 q;
+      __builtin_memcpy(&q, e, 16);
+      __builtin_nontemporal_store(q, reinterpret_cast<any4*>(p));
+    } else {
+      __builtin_memcpy(p, e, sizeof(e));
+    }
   } else {
 #pragma unroll
     for (int j = 0; j < W; ++j)
       if (j < valid) p[j] = e[j];
   }
 }
+typedef How<false, false> Any;
 
 // What an epilogue keeps of its W columns, or reads of a row of them.
 template <int W>

@@ -32,7 +32,8 @@ __device__ inline float slope(float z, int act) {
   return 1.0f;
 }
 
-template <class T>
+// ACT < 0: the activation is `act`.
+template <class T, int ACT = -1>
 struct LinearEpilogue {
   static constexpr bool kSymmetric = false;
   const float* bias;
@@ -42,6 +43,17 @@ struct LinearEpilogue {
   int64_t ldr, ldy, ldz;
   int act;
 
+  template <class F>
+  __device__ __attribute__((always_inline)) void chosen(F f) const {
+    if (act == XMEM_ACT_GELU)
+      f(LinearEpilogue<T, XMEM_ACT_GELU>{bias, r, y, z, ldr, ldy, ldz, act});
+    else if (act == XMEM_ACT_SILU)
+      f(LinearEpilogue<T, XMEM_ACT_SILU>{bias, r, y, z, ldr, ldy, ldz, act});
+    else if (act == XMEM_ACT_RELU)
+      f(LinearEpilogue<T, XMEM_ACT_RELU>{bias, r, y, z, ldr, ldy, ldz, act});
+    else
+      f(LinearEpilogue<T, XMEM_ACT_NONE>{bias, r, y, z, ldr, ldy, ldz, act});
+  }
   template <int W>
   __device__ Column<W> column(int64_t n, int valid, int, const GemmArgs&) const {
     Column<W> c;
@@ -65,17 +77,17 @@ struct LinearEpilogue {
     }
     return e;
   }
-  template <int W>
+  template <int W, class HOW>
   __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& c, const Read<W>& e, int, const GemmArgs&) const {
 #pragma unroll
     for (int j = 0; j < W; ++j) v[j] += c.v[j];
-    if (z) put<T, W>(z + m * ldz + n, valid, v);
+    if (z) put<T, W, HOW>(z + m * ldz + n, valid, v);
 #pragma unroll
-    for (int j = 0; j < W; ++j) v[j] = activate(v[j], act);
+    for (int j = 0; j < W; ++j) v[j] = activate(v[j], ACT < 0 ? act : ACT);
     if (r)
 #pragma unroll
       for (int j = 0; j < W; ++j) v[j] += float(e.v[j]);
-    put<T, W>(y + m * ldy + n, valid, v);
+    put<T, W, HOW>(y + m * ldy + n, valid, v);
   }
 };
 
@@ -85,14 +97,16 @@ struct StoreEpilogue {
   T* y;
   int64_t ldy;
 
+  template <class F>
+  __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
   template <int W> using Read = None;
   template <int W>
   __device__ None column(int64_t, int, int, const GemmArgs&) const { return {}; }
   template <int W>
   __device__ None read(int64_t, int64_t, int, int, const GemmArgs&) const { return {}; }
-  template <int W>
+  template <int W, class HOW>
   __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, None, None, int, const GemmArgs&) const {
-    put<T, W>(y + m * ldy + n, valid, v);
+    put<T, W, HOW>(y + m * ldy + n, valid, v);
   }
 };
 
@@ -130,7 +144,7 @@ __global__ __launch_bounds__(256) void k_dz(const T* dy, int64_t lddy, const T* 
         if (valid < 8)  // where z is read as 0 past the end, dy is too
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = j < valid ? v[j] : 0.0f;
-        put<T, 8>(dz + r * lddz + c, 8, v);
+        put<T, 8, Any>(dz + r * lddz + c, 8, v);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] += v[j];

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void k_momentum(const G* g, float* mom, i
       const double u = nesterov ? e[j] + mu * m[j] : m[j];
       sum += u * u;
     }
-    put<float, 8>(mom + i, valid, m);
+    put<float, 8, Any>(mom + i, valid, m);
   }
   sum = wave_sum(sum);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
@@ -127,8 +127,8 @@ __global__ __launch_bounds__(kThreads) void k_start(const G* g, const float* mom
       m[j] = j < valid ? m[j] : 0.0f;  // infinities and NaN in g must not reach the padding
       e[j] = m[j] - float(f16(m[j]));
     }
-    put<f16, 8>(x + (b * rows + r) * ldx + c, 8, m);
-    put<f16, 8>(lo + (b * rows + r) * ldx + c, 8, e);
+    put<f16, 8, Any>(x + (b * rows + r) * ldx + c, 8, m);
+    put<f16, 8, Any>(lo + (b * rows + r) * ldx + c, 8, e);
   }
 }
 
@@ -142,6 +142,8 @@ __global__ void k_clear_pads(f16* p, int64_t rows, int64_t cols, int64_t ld) {
 // entry below it is written to its mirrored place too.
 struct GramEpilogue {
   static constexpr bool kSymmetric = true;
+  template <class F>
+  __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
   f16* p;
   float* d;
   int64_t ld;
@@ -151,7 +153,7 @@ struct GramEpilogue {
   template <int W> using Read = None;
   template <int W>
   __device__ None read(int64_t, int64_t, int, int, const GemmArgs&) const { return {}; }
-  template <int W>
+  template <int W, class HOW>
   __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, None, None, int z, const GemmArgs& g) const {
     f16* to = p + z * g.m * ld;
 #pragma unroll
@@ -168,7 +170,7 @@ struct GramEpilogue {
   __device__ static void mirror(f16* to, int64_t ld, int64_t m, int64_t n, const float (&v)[W], int valid) {
     if (n > m) return;  // its mirrored place is written
     const int own = m - n + 1 < valid ? int(m - n + 1) : valid;
-    put<f16, W>(to + m * ld + n, own, v);
+    put<f16, W, Any>(to + m * ld + n, own, v);
 #pragma unroll
     for (int j = 0; j < W; ++j)
       if (j < own) to[(n + j) * ld + m] = f16(v[j]);
@@ -178,6 +180,8 @@ struct GramEpilogue {
 // Q = b P + c P P without its diagonal.
 struct PolyEpilogue {
   static constexpr bool kSymmetric = true;
+  template <class F>
+  __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
   const f16* p;
   const float* dp;
   f16* q;
@@ -205,7 +209,7 @@ struct PolyEpilogue {
     __builtin_memcpy(&r.e, p + (z * g.m + m) * ld + n, sizeof(r.e));
     return r;
   }
-  template <int W>
+  template <int W, class HOW>
   __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& dn, const Read<W>& r, int z, const GemmArgs& g) const {
     if (n > m) return;
     const float dm = r.dm;
@@ -223,6 +227,8 @@ struct PolyEpilogue {
 template <bool TALL>
 struct StepEpilogue {
   static constexpr bool kSymmetric = false;
+  template <class F>
+  __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
   const f16 *x, *lo;  // lo, nlo: NULL where X is kept in one half
   const float* dq;
   f16 *nx, *nlo;
@@ -256,7 +262,7 @@ struct StepEpilogue {
       r.lo = typename Read<W>::part(f16(0.0f));
     return r;
   }
-  template <int W>
+  template <int W, class HOW>
   __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& dn, const Read<W>& r, int z, const GemmArgs& g) const {
     const int64_t at = (z * g.m + m) * ld + n;
     float rest[W];
@@ -266,13 +272,13 @@ struct StepEpilogue {
     if (out) {
 #pragma unroll
       for (int j = 0; j < W; ++j) v[j] *= scale / kX;
-      put<bf16, W>(out + (z * g.m + m) * g.n + n, valid, v);
+      put<bf16, W, HOW>(out + (z * g.m + m) * g.n + n, valid, v);
     } else {
-      put<f16, W>(nx + at, valid, v);
+      put<f16, W, HOW>(nx + at, valid, v);
       if (nlo) {
 #pragma unroll
         for (int j = 0; j < W; ++j) rest[j] = v[j] - float(f16(v[j]));
-        put<f16, W>(nlo + at, valid, rest);
+        put<f16, W, HOW>(nlo + at, valid, rest);
       }
     }
   }
