@@ -30,6 +30,7 @@ struct GemmArgs {
 template <int BM_, int BN_, int WM_, int WN_, int WK_, int STAGES_, int DEPTH_>
 struct Config {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WK = WK_, FM = BM / WM / 16, FN = BN / WN / 16;
+  static_assert(FN % 2 == 0);
   static constexpr int GROUP = 64 * WM * WN, THREADS = GROUP * WK, STAGES = STAGES_, DEPTH = DEPTH_;
 };
 typedef Config<256, 256, 2, 4, 1, 2, 0> Large;   // 128 KiB of LDS, two wavefronts on a SIMD: a CU to itself
@@ -40,10 +41,7 @@ typedef Config<64, 64, 2, 2, 4, 2, 1> Small;     // 128 KiB, four wavefronts on 
 // that read one column of chunks meet 16 different bank groups.
 //   k contiguous:    [row][8 chunks of k],   chunk c at c ^ ((row >> 1) & 7)
 //   rows contiguous: [k][R / 8 chunks of rows], pairs of chunks (the 16 rows of one product) at p ^ h(k)
-// PERM (k contiguous only): of each strip of 32 rows, place 16 t + 4 g + r holds row 8 g + 4 t + r.  A matrix
-// instruction leaves a lane group g the rows 4 g + r of its product, so with two products it has 8 neighbours, and
-// the epilogue moves 16 bytes a lane, 64 next to each other.
-template <class T, int R, bool KC, bool PERM>
+template <class T, int R, bool KC>
 struct Tile {
   typedef typename Vec<T>::x8 x8;
   static constexpr int kBytes = R * kBK * 2;
@@ -53,9 +51,8 @@ struct Tile {
   // the row (or first of eight rows) and the k (or first of eight) of the chunk kept at place i
   __device__ static void at(int i, int& row, int& k) {
     if constexpr (KC) {
-      const int r = i >> 3;
-      k = ((i & 7) ^ ((r >> 1) & 7)) * 8;
-      row = PERM ? (r & ~31) + 8 * ((r >> 2) & 3) + 4 * ((r >> 4) & 1) + (r & 3) : r;
+      row = i >> 3;
+      k = ((i & 7) ^ ((row >> 1) & 7)) * 8;
     } else {
       k = i / (R / 8);
       const int c = i % (R / 8);
@@ -228,22 +225,23 @@ __device__ inline void tile_of(int id, const GemmArgs& g, int& tm, int& tn) {
   }
 }
 
-// What a lane has of a tile: FN products' four neighbours each, of FM rows.  The epilogue takes them W at a time, from
-// row i0 on every STEP-th; what it reads of memory is asked for four rows at a time, before anything of them is
-// written.  The Q-th W columns of a lane; recursive, so that acc is indexed by constants however long the epilogue is.
+// What a lane has of a tile: FN products' four neighbours each, of FM rows.  Two products' fours, exchanged between the
+// lanes 16 apart, are eight neighbours of one or the other: the epilogue takes these, 16 bytes at a time and 64 next to
+// each other, from row i0 on every STEP-th; what it reads of memory is asked for four rows at a time, before anything
+// of them is written.  The Q-th eight of a lane; recursive, so that acc is indexed by constants however long the epilogue is.
 // HOW says what is known of the tile before it runs: whole (nothing of it is past the matrix) and past the L2s.
 template <bool WHOLE_, bool PAST_L2_>
 struct How {
   static constexpr bool WHOLE = WHOLE_, PAST_L2 = PAST_L2_;
 };
-template <class C, bool PERM, int STEP, int Q, class HOW, class Epi>
+template <class C, int STEP, int Q, class HOW, class Epi>
 __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0,
                                                              int64_t n0, int z, const GemmArgs& g) {
-  constexpr int W = PERM ? 8 : 4, GROUPS = C::FN * 4 / W, ROWS = (C::FM + STEP - 1) / STEP, BATCH = ROWS < 4 ? ROWS : 4;
+  constexpr int W = 8, GROUPS = C::FN / 2, ROWS = (C::FM + STEP - 1) / STEP, BATCH = ROWS < 4 ? ROWS : 4;
   static_assert(ROWS % BATCH == 0);
   const int lane = threadIdx.x & 63, wave = (threadIdx.x % C::GROUP) >> 6;
   const int64_t mw = m0 + (wave / C::WN) * (C::BM / C::WM) + (lane & 15);
-  const int64_t n = n0 + (wave % C::WN) * (C::BN / C::WN) + (lane >> 4) * W + Q * 4 * W;
+  const int64_t n = n0 + (wave % C::WN) * (C::BN / C::WN) + 32 * Q + 16 * ((lane >> 4) & 1) + 8 * (lane >> 5);
   const int valid = HOW::WHOLE || g.n - n >= W ? W : g.n > n ? int(g.n - n) : 0;
   const auto col = epi.template column<W>(n, valid, z, g);
 #pragma unroll
@@ -259,27 +257,30 @@ __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[
       const int64_t m = mw + 16 * (i0 + (h * BATCH + i) * STEP);
       float v[W];
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        v[j] = acc[h * BATCH + i][Q * (W / 4) + j / 4][j & 3];
+      for (int j = 0; j < 4; ++j) {
+        float lo = acc[h * BATCH + i][2 * Q][j], hi = acc[h * BATCH + i][2 * Q + 1][j];
         if constexpr (STEP > 1)
 #pragma unroll
           for (int k = 0; k < C::FM; ++k)
-            if (k == i0 + (h * BATCH + i) * STEP) v[j] = acc[k][Q * (W / 4) + j / 4][j & 3];
+            if (k == i0 + (h * BATCH + i) * STEP) lo = acc[k][2 * Q][j], hi = acc[k][2 * Q + 1][j];
+        const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(lo), __float_as_uint(hi), false, false);
+        v[j] = __uint_as_float(two[0]);
+        v[4 + j] = __uint_as_float(two[1]);
       }
       if (HOW::WHOLE || (m < g.m && valid > 0)) epi.template row<W, HOW>(m, n, v, valid, col, in[i], z, g);
     }
   }
-  if constexpr (Q + 1 < GROUPS) finish<C, PERM, STEP, Q + 1, HOW>(acc, i0, epi, m0, n0, z, g);
+  if constexpr (Q + 1 < GROUPS) finish<C, STEP, Q + 1, HOW>(acc, i0, epi, m0, n0, z, g);
 }
 // An epilogue's choices are made once a tile, so that the code a tile runs through is short: it passes the
 // instruction cache once for each.
-template <class C, bool PERM, int STEP, class Epi>
+template <class C, int STEP, class Epi>
 __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0,
                                                              int64_t n0, int z, const GemmArgs& g) {
   if (m0 + C::BM <= g.m && n0 + C::BN <= g.n)
-    epi.chosen([&](const auto& e) __attribute__((always_inline)) { finish<C, PERM, STEP, 0, How<true, PERM && C::BM == 256>>(acc, i0, e, m0, n0, z, g); });
+    epi.chosen([&](const auto& e) __attribute__((always_inline)) { finish<C, STEP, 0, How<true, C::BM == 256>>(acc, i0, e, m0, n0, z, g); });
   else
-    finish<C, PERM, STEP, 0, How<false, false>>(acc, i0, epi, m0, n0, z, g);
+    finish<C, STEP, 0, How<false, false>>(acc, i0, epi, m0, n0, z, g);
 }
 
 // One workgroup's tile.  Half a tile's operands are in registers ahead of the matrix instructions: while the products of
@@ -291,9 +292,8 @@ template <class T, class C, bool AKC, bool BKC, bool DIRECT, class Epi>
 __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
 #ifdef __HIP_DEVICE_COMPILE__  // the host's pass knows no buffer resources, and wants the kernel's name only
   constexpr int FM = C::FM, FN = C::FN;
-  constexpr bool PERM = BKC && FN % 2 == 0;
-  typedef Tile<T, C::BM, AKC, false> TA;
-  typedef Tile<T, C::BN, BKC, PERM> TB;
+  typedef Tile<T, C::BM, AKC> TA;
+  typedef Tile<T, C::BN, BKC> TB;
   constexpr int BUF = TA::kBytes + TB::kBytes, kReads = FM * (AKC ? 1 : 2) + FN * (BKC ? 1 : 2);
   typedef typename Vec<T>::x8 x8;
   constexpr int BUFS = DIRECT ? C::STAGES : 2, LOADS = (TA::kChunks + TB::kChunks) / C::GROUP;
@@ -434,12 +434,12 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
         for (int j = 0; j < FN; ++j) to[(i * FN + j) * C::GROUP] = acc[i][j];
     return;
   }
-  finish<C, PERM, C::WK>(acc, group, epi, m0, n0, z, g);
+  finish<C, C::WK>(acc, group, epi, m0, n0, z, g);
 #endif
 }
 
 // The splits of a product, added in their order, and its epilogue: a workgroup a tile, its lanes as one group of k_gemm.
-template <class C, bool BKC, class Epi>
+template <class C, class Epi>
 __global__ __launch_bounds__(C::GROUP) void k_join(GemmArgs g, Epi epi) {
   int tm, tn;
   const int z = blockIdx.x / g.tiles, tile = blockIdx.x % g.tiles;
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(C::GROUP) void k_join(GemmArgs g, Epi epi) {
 #pragma unroll
       for (int j = 0; j < C::FN; ++j) acc[i][j] += from[(i * C::FN + j) * C::GROUP];
   }
-  finish<C, BKC && C::FN % 2 == 0, 1>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
+  finish<C, 1>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
 }
 
 inline int64_t tiles_of(int64_t m, int64_t n, int bm, int bn, bool symmetric) {
@@ -510,7 +510,7 @@ int launch(GemmArgs g, const Epi& epi, hipStream_t st) {
   else
     return launch<T, Medium, AKC, BKC>(g, epi, st);  // a tile's registers would not fit
   if constexpr (C::BM == 64)
-    if (g.splits > 1) k_join<C, BKC, Epi><<<blocks, C::GROUP, 0, st>>>(g, epi);
+    if (g.splits > 1) k_join<C, Epi><<<blocks, C::GROUP, 0, st>>>(g, epi);
   return launched();
 }
 
@@ -542,7 +542,7 @@ __device__ inline void get(const T* p, int valid, float (&v)[W]) {
 }
 // HOW::PAST_L2: an output of the 256 x 256 tiles (24 MiB and more) stays in no L2 anyway; written past them it leaves the operands
 // there.  8192 x 8192 and its pre-activation 283 -> 244 us, 24 steps of 8192 x 2048 18.1 -> 17.2 ms; one of 1024 x 1024,
-// which the next kernel reads, 162 -> 171 us.  Pieces of 8 bytes are left to the L2 to put together: 258 -> 387 us.
+// which the next kernel reads, 162 -> 171 us.
 template <class T, int W, class HOW>
 __device__ inline void put(T* p, int valid, const float (&v)[W]) {
   T e[W];
