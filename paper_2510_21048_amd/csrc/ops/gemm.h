@@ -36,6 +36,7 @@ struct Config {
 typedef Config<256, 256, 2, 4, 1, 2, 0> Large;   // 128 KiB of LDS, two wavefronts on a SIMD: a CU to itself
 typedef Config<128, 128, 2, 2, 2, 2, 1> Medium;  // 128 KiB, two wavefronts on a SIMD
 typedef Config<64, 64, 2, 2, 4, 2, 1> Small;     // 128 KiB, four wavefronts on a SIMD
+typedef Config<64, 64, 2, 2, 2, 2, 1> Half;      // 64 KiB, two workgroups a CU: where there are more tiles than CUs
 
 // One operand tile in LDS: R rows of kBK.  Chunks of 16 bytes are kept at swizzled places, so that the 16 lanes
 // that read one column of chunks meet 16 different bank groups.
@@ -524,6 +525,7 @@ int gemm(GemmArgs g, const Epi& epi, void* part, hipStream_t st) {
   g.part = static_cast<float*>(part);
   if (p.side == 256) return launch<T, Large, AKC, BKC>(g, epi, st);
   if (p.side == 128) return launch<T, Medium, AKC, BKC>(g, epi, st);
+  if (p.splits == 1 && tiles_of(g.m, g.n, 64, 64, Epi::kSymmetric) * g.count > kCus) return launch<T, Half, AKC, BKC>(g, epi, st);
   return launch<T, Small, AKC, BKC>(g, epi, st);
 }
 
