@@ -41,9 +41,10 @@ extern "C" {
 #define XMEM_ACT_GELU 2 /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
 #define XMEM_ACT_SILU 3 /* z / (1 + exp(-z)) */
 
-/* Workspace of xmem_linear_forward (may be 0: then d_workspace may be NULL).
- * 0 for invalid sizes too. */
-size_t xmem_linear_forward_workspace_bytes(int64_t m, int64_t n, int64_t k);
+/* Workspace of xmem_linear_forward (may be 0: then d_workspace may be NULL):
+ * sums of products with few outputs, and copies of operands whose rows are no
+ * multiple of 8 elements apart or long.  0 for invalid sizes too. */
+size_t xmem_linear_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw);
 
 /* z = x w^T + b;  y = act(z) + r.  Sums and the epilogue are in 32 bits, y and
  * z are rounded once.
@@ -54,7 +55,7 @@ size_t xmem_linear_forward_workspace_bytes(int64_t m, int64_t n, int64_t k);
  *   d_y        : [m, n] of dtype, written
  *   d_z        : [m, n] of dtype or NULL, written: what the backward pass needs
  *                of an activation
- *   d_workspace: >= xmem_linear_forward_workspace_bytes(m, n, k), 256-byte aligned
+ *   d_workspace: >= its size, 256-byte aligned
  * k == 0 gives z = b.  No output may overlap another operand (d_residual apart).
  * Returns XMEM_OK, XMEM_EINVAL (null pointer, negative or too large size (2^30 and more), ld too
  * small, unknown dtype or activation), XMEM_EWORKSPACE or XMEM_EHIP. */
@@ -64,8 +65,9 @@ int xmem_linear_forward(const void* d_x, int64_t ldx, const void* d_w, int64_t l
                         size_t workspace_bytes, void* hip_stream);
 
 /* Workspace of xmem_linear_backward: it holds dz where an activation has one
- * (activation != XMEM_ACT_NONE), and partial sums. */
-size_t xmem_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int activation);
+ * (activation != XMEM_ACT_NONE), partial sums, and copies as above. */
+size_t xmem_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t lddy, int64_t ldx, int64_t ldw,
+                                            int activation);
 
 /* The gradients of xmem_linear_forward for an output gradient dy:
  *   dz = dy act'(z);  dx = dz w;  dw = dz^T x;  db = sum over rows of dz.
@@ -74,7 +76,8 @@ size_t xmem_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int
  *   d_dy : [m, n] of dtype
  *   d_z  : [m, n] of dtype as xmem_linear_forward wrote it; not looked at (and
  *          NULL allowed) where activation is XMEM_ACT_NONE
- *   d_x, d_w : as in the forward pass; d_x may be NULL without d_dw, d_w without d_dx
+ *   d_x, d_w : as in the forward pass; d_x may be NULL without d_dw, d_w without d_dx (their ld is
+ *          looked at all the same: the workspace goes by it)
  *   d_dx : [m, k] of dtype or NULL, written
  *   d_dw : [n, k] of dtype or NULL, written
  *   d_db : float32 [n] or NULL, written

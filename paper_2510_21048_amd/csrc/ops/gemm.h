@@ -275,11 +275,11 @@ __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[
 }
 // An epilogue's choices are made once a tile, so that the code a tile runs through is short: it passes the
 // instruction cache once for each.
-template <class C, int STEP, class Epi>
+template <class C, int STEP, bool PAST_L2, class Epi>
 __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0,
                                                              int64_t n0, int z, const GemmArgs& g) {
   if (m0 + C::BM <= g.m && n0 + C::BN <= g.n)
-    epi.chosen([&](const auto& e) __attribute__((always_inline)) { finish<C, STEP, 0, How<true, C::BM == 256>>(acc, i0, e, m0, n0, z, g); });
+    epi.chosen([&](const auto& e) __attribute__((always_inline)) { finish<C, STEP, 0, How<true, PAST_L2>>(acc, i0, e, m0, n0, z, g); });
   else
     finish<C, STEP, 0, How<false, false>>(acc, i0, epi, m0, n0, z, g);
 }
@@ -289,7 +289,7 @@ __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[
 // overwritten by the loads of the tile STAGES on (direct), or the next tile, stored from registers while the
 // first half ran, is complete (staged, two LDS buffers).
 // The n side is the first operand of the matrix instruction, so that a lane ends with neighbouring n of one m.
-template <class T, class C, bool AKC, bool BKC, bool DIRECT, class Epi>
+template <class T, class C, bool AKC, bool BKC, bool DIRECT, bool PAST_L2, class Epi>
 __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
 #ifdef __HIP_DEVICE_COMPILE__  // the host's pass knows no buffer resources, and wants the kernel's name only
   constexpr int FM = C::FM, FN = C::FN;
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
         for (int j = 0; j < FN; ++j) to[(i * FN + j) * C::GROUP] = acc[i][j];
     return;
   }
-  finish<C, C::WK>(acc, group, epi, m0, n0, z, g);
+  finish<C, C::WK, PAST_L2>(acc, group, epi, m0, n0, z, g);
 #endif
 }
 
@@ -460,7 +460,7 @@ __global__ __launch_bounds__(C::GROUP) void k_join(GemmArgs g, Epi epi) {
 #pragma unroll
       for (int j = 0; j < C::FN; ++j) acc[i][j] += from[(i * C::FN + j) * C::GROUP];
   }
-  finish<C, 1>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
+  finish<C, 1, false>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
 }
 
 inline int64_t tiles_of(int64_t m, int64_t n, int bm, int bn, bool symmetric) {
@@ -468,29 +468,75 @@ inline int64_t tiles_of(int64_t m, int64_t n, int bm, int bn, bool symmetric) {
   return symmetric ? tm * (tm + 1) / 2 : tm * tn;
 }
 
-// Which tile a product takes, and over how many workgroups a tile's k is split.
+// Which tile a product takes, and over how many workgroups a tile's k is split: what costs least by what was measured.
+// A round of workgroups over the CUs takes a time of its own and one per k tile:
+//   256: 10 + 1.45 us (4096 x 4096 x 64, 4096: 11.7, 110 us);  128: 7.5 + 0.5 (2048 x 2048 x 64, 8192: 9.0, 70.4);
+//   64: 6.5 + 0.24 up to one tile a CU (1024 x 1024 x 64, 4096: 6.6, 21.6), 6.7 + 0.33 for two (1024 tiles: 13.9, 97.3 at 8192).
+// 1536 x 1536 x 4096 takes 82, 38 and 51 us with the three, 1024 x 1024 x 4096 78, 36 and 22.  A split adds a launch, and its sums
+// go through memory.
 struct Plan {
   int side;  // 256, 128 or 64
   int splits, span;
 };
 inline Plan plan_of(int64_t m, int64_t n, int64_t k, int64_t count, bool symmetric, bool may_split) {
   const int64_t kt = (k + kBK - 1) / kBK;
-  Plan p{256, 1, int(kt)};
-  if (tiles_of(m, n, 256, 256, symmetric) * count < kCus * 3 / 4) p.side = 128;
-  if (p.side == 128 && tiles_of(m, n, 128, 128, symmetric) * count < kCus * 3 / 4) p.side = 64;
-  const int64_t tiles = tiles_of(m, n, p.side, p.side, symmetric) * count;
-  // 16 k tiles a workgroup at least: a split costs its part of the sums, written and read, and another launch
-  if (may_split && p.side == 64 && tiles < kCus && kt >= 32) {
-    int64_t s = (2 * kCus + tiles - 1) / tiles;
-    if (s > kt / 16) s = kt / 16;
-    p.span = int((kt + s - 1) / s);
-    p.splits = int((kt + p.span - 1) / p.span);
+  const auto rounds = [](int64_t w, int64_t at_once) { return double((w + at_once - 1) / at_once); };
+  const double large = rounds(tiles_of(m, n, 256, 256, symmetric) * count, kCus) * (10.0 + 1.45 * kt);
+  const double medium = rounds(tiles_of(m, n, 128, 128, symmetric) * count, kCus) * (7.5 + 0.5 * kt);
+  const int64_t tiles = tiles_of(m, n, 64, 64, symmetric) * count;
+  const auto small = [&](int64_t w, int64_t span) { return w <= kCus ? 6.5 + 0.24 * span : rounds(w, 2 * kCus) * (6.7 + 0.33 * span); };
+  Plan p{64, 1, int(kt)};
+  double least = small(tiles, kt);
+  for (int64_t s = 2; may_split && s <= kt / 4 && tiles * s <= 2 * kCus; ++s) {
+    const int64_t span = (kt + s - 1) / s;
+    const double cost = small(tiles * s, span) + 4.5 + double(tiles * s) * 0.008;
+    if (cost < least) least = cost, p = {64, int((kt + span - 1) / span), int(span)};
   }
+  if (medium < least) least = medium, p = {128, 1, int(kt)};
+  if (large < least) p = {256, 1, int(kt)};
   return p;
 }
 inline size_t part_bytes(int64_t m, int64_t n, int64_t k, int64_t count, bool symmetric) {
   const Plan p = plan_of(m, n, k, count, symmetric, true);
   return p.splits > 1 ? up256(size_t(tiles_of(m, n, p.side, p.side, symmetric)) * count * p.splits * p.side * p.side * 4) : 0;
+}
+
+// A matrix [rows, cols] whose rows allow no 16-byte loads, as one whose rows are a multiple of 8 long, with zeros behind them.
+struct Pack {
+  const void* from;
+  int64_t ld, rows, cols;
+  void* to;
+};
+
+__host__ __device__ inline int64_t packed_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
+template <class T>
+__global__ __launch_bounds__(256) void k_pack(Pack p0, Pack p1) {
+  const Pack p = blockIdx.y ? p1 : p0;
+  const unsigned pieces = unsigned(packed_ld(p.cols) / 8);
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < p.rows * pieces; i += int64_t(gridDim.x) * 256) {
+    const int64_t r = i / pieces, c = (i - r * pieces) * 8;
+    const T* from = static_cast<const T*>(p.from) + r * p.ld + c;
+    u32x4 v;
+    if (p.cols - c >= 8) {
+      __builtin_memcpy(&v, from, 16);
+    } else {
+      T e[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[j] = j < p.cols - c ? from[j] : T(0.0f);
+      __builtin_memcpy(&v, e, 16);
+    }
+    *reinterpret_cast<u32x4*>(static_cast<T*>(p.to) + i * 8) = v;
+  }
+}
+// One or two (from NULL: none) matrices in one launch.
+template <class T>
+inline void pack(const Pack& a, const Pack& b, hipStream_t st) {
+  const Pack& first = a.from ? a : b;
+  if (!first.from) return;
+  const bool both = a.from && b.from;
+  const auto work = [](const Pack& p) { return p.rows * (packed_ld(p.cols) / 8); };
+  const int64_t most = both && work(b) > work(a) ? work(b) : work(first), blocks = (most + 255) / 256;
+  if (blocks > 0) k_pack<T><<<dim3(unsigned(blocks < 8192 ? blocks : 8192), both ? 2 : 1), 256, 0, st>>>(first, b);
 }
 
 inline bool direct_ok(const void* p, int64_t ld, int64_t stride, int64_t contiguous, bool padded) {
@@ -504,10 +550,15 @@ int launch(GemmArgs g, const Epi& epi, hipStream_t st) {
   g.tiles = int(tiles_of(g.m, g.n, C::BM, C::BN, Epi::kSymmetric));
   const unsigned blocks = unsigned(g.tiles * g.count);
   const bool direct = direct_ok(g.a, g.lda, g.stride_a, AKC ? g.k : g.m, g.pad_a) && direct_ok(g.b, g.ldb, g.stride_b, BKC ? g.k : g.n, g.pad_b);
+  if constexpr (C::BM == 256 && Epi::kPastL2)
+    if (direct && epi.lines()) {
+      k_gemm<T, C, AKC, BKC, true, true, Epi><<<blocks, C::THREADS, 0, st>>>(g, epi);
+      return launched();
+    }
   if (direct)
-    k_gemm<T, C, AKC, BKC, true, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
+    k_gemm<T, C, AKC, BKC, true, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
   else if constexpr (C::DEPTH > 0)
-    k_gemm<T, C, AKC, BKC, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
+    k_gemm<T, C, AKC, BKC, false, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
   else
     return launch<T, Medium, AKC, BKC>(g, epi, st);  // a tile's registers would not fit
   if constexpr (C::BM == 64)
@@ -529,6 +580,9 @@ int gemm(GemmArgs g, const Epi& epi, void* part, hipStream_t st) {
   return launch<T, Small, AKC, BKC>(g, epi, st);
 }
 
+// Whether the 64 bytes that an epilogue writes of a row are one piece of memory.
+inline bool whole_lines(const void* p, int64_t ld) { return aligned(p, 64) && ld % 32 == 0; }
+
 // W neighbouring elements of a row, `valid` of which exist; whole ones move in one access of any alignment.
 template <class T, int W>
 __device__ inline void get(const T* p, int valid, float (&v)[W]) {
@@ -542,8 +596,8 @@ __device__ inline void get(const T* p, int valid, float (&v)[W]) {
 #pragma unroll
   for (int j = 0; j < W; ++j) v[j] = float(e[j]);
 }
-// HOW::PAST_L2: an output of the 256 x 256 tiles (24 MiB and more) stays in no L2 anyway; written past them it leaves the operands
-// there.  8192 x 8192 and its pre-activation 283 -> 244 us, 24 steps of 8192 x 2048 18.1 -> 17.2 ms; one of 1024 x 1024,
+// HOW::PAST_L2: an output of the 256 x 256 tiles stays in no L2 for long; written past them, where its rows are whole
+// pieces of 64 bytes, it leaves the operands there.  8192 x 8192 and its pre-activation 283 -> 244 us, 24 steps of 8192 x 2048 18.1 -> 17.2 ms; one of 1024 x 1024,
 // which the next kernel reads, 162 -> 171 us.
 template <class T, int W, class HOW>
 __device__ inline void put(T* p, int valid, const float (&v)[W]) {

@@ -35,7 +35,7 @@ __device__ inline float slope(float z, int act) {
 // ACT < 0: the activation is `act`.
 template <class T, int ACT = -1>
 struct LinearEpilogue {
-  static constexpr bool kSymmetric = false;
+  static constexpr bool kSymmetric = false, kPastL2 = true;
   const float* bias;
   const T* r;
   T* y;
@@ -43,6 +43,7 @@ struct LinearEpilogue {
   int64_t ldr, ldy, ldz;
   int act;
 
+  bool lines() const { return whole_lines(y, ldy) && whole_lines(z, ldz); }
   template <class F>
   __device__ __attribute__((always_inline)) void chosen(F f) const {
     if (act == XMEM_ACT_GELU)
@@ -93,10 +94,11 @@ struct LinearEpilogue {
 
 template <class T>
 struct StoreEpilogue {
-  static constexpr bool kSymmetric = false;
+  static constexpr bool kSymmetric = false, kPastL2 = true;
   T* y;
   int64_t ldy;
 
+  bool lines() const { return whole_lines(y, ldy); }
   template <class F>
   __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
   template <int W> using Read = None;
@@ -115,9 +117,18 @@ constexpr int kBandCols = 512;  // columns of a workgroup of k_dz, eight a lane
 // Rows whose column sums one workgroup of k_dz takes: 64, or 16 where that would leave most CUs without one.
 inline int64_t band_rows(int64_t m, int64_t n) { return (m + 63) / 64 * ((n + kBandCols - 1) / kBandCols) < 4 * kCus ? 16 : 64; }
 inline int64_t bands(int64_t m, int64_t n) { return (m + band_rows(m, n) - 1) / band_rows(m, n); }
-inline int64_t padded(int64_t n) { return (n + 7) & ~int64_t(7); }
-inline size_t part_bytes_of(int64_t m, int64_t n) { return up256(size_t(bands(m, n)) * n * 4); }
-inline size_t dz_bytes(int64_t m, int64_t n, int act) { return act == XMEM_ACT_NONE ? 0 : up256(size_t(m) * padded(n) * 2); }
+
+// Whether a matrix of `cols` columns is copied to rows of 16 bytes' alignment before a product of m n k multiplications: the
+// copy costs a launch and a pass over it.  1003 x 2047 x 1021 (2.1e9): 21 us with the copies and without; 4099 x 4097 x 4095: 210
+// against 365; 501 x 1023 x 511: 15 against 11.
+constexpr double kPackFrom = 4.0e9;
+inline bool packs(int64_t cols, int64_t ld, int64_t m, int64_t n, int64_t k) {
+  return (cols % 8 || ld % 8) && double(m) * double(n) * double(k) >= kPackFrom;
+}
+inline size_t packed_bytes(int64_t rows, int64_t cols) { return up256(size_t(rows) * packed_ld(cols) * 2); }
+inline size_t sums_bytes(int64_t m, int64_t n) { return up256(size_t(bands(m, n)) * n * 4); }
+// dz is kept where it is not dy, or dy's rows allow no 16-byte loads
+inline bool keeps_dz(int64_t m, int64_t n, int64_t k, int64_t lddy, int act) { return act != XMEM_ACT_NONE || packs(n, lddy, m, n, k); }
 
 // dz = dy act'(z), and the column sums of each band of rows before dz is rounded.  A wavefront takes every fourth row of
 // the band, 16 bytes a lane; what pads a row of dz is 0, since the product that sums along it reads it.
@@ -189,25 +200,62 @@ bool sizes_ok(int64_t m, int64_t n, int64_t k) {
 }
 bool ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld < kMostLd; }
 
+// The workspace, part after part.
+struct Carve {
+  char* at;
+  template <class P>
+  P* take(size_t bytes) {
+    char* r = at;
+    at += bytes;
+    return reinterpret_cast<P*>(r);
+  }
+};
+
+size_t forward_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
+  return (packs(k, ldx, m, n, k) ? packed_bytes(m, k) : 0) + (packs(k, ldw, m, n, k) ? packed_bytes(n, k) : 0) + part_bytes(m, n, k, 1, false);
+}
+
 template <class T>
 int forward(const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias, const void* r, int64_t ldr, int64_t m,
             int64_t n, int64_t k, int act, void* y, int64_t ldy, void* z, int64_t ldz, void* ws, hipStream_t st) {
+  Carve at{static_cast<char*>(ws)};
+  GemmArgs g{x, w, ldx, ldw, 0, 0, m, n, k};
+  Pack px{}, pw{};
+  if (packs(k, ldx, m, n, k)) {
+    px = {x, ldx, m, k, at.take<char>(packed_bytes(m, k))};
+    g.a = px.to, g.lda = packed_ld(k), g.pad_a = true;
+  }
+  if (packs(k, ldw, m, n, k)) {
+    pw = {w, ldw, n, k, at.take<char>(packed_bytes(n, k))};
+    g.b = pw.to, g.ldb = packed_ld(k), g.pad_b = true;
+  }
+  pack<T>(px, pw, st);
   const LinearEpilogue<T> e{bias, static_cast<const T*>(r), static_cast<T*>(y), static_cast<T*>(z), ldr, ldy, ldz, act};
-  return gemm<T, true, true>(GemmArgs{x, w, ldx, ldw, 0, 0, m, n, k}, e, ws, st);
+  return gemm<T, true, true>(g, e, at.at, st);
+}
+
+size_t backward_bytes(int64_t m, int64_t n, int64_t k, int64_t lddy, int64_t ldx, int64_t ldw, int act) {
+  const size_t sx = part_bytes(m, k, n, 1, false), sw = part_bytes(n, k, m, 1, false);
+  return sums_bytes(m, n) + (keeps_dz(m, n, k, lddy, act) ? packed_bytes(m, n) : 0) + (packs(k, ldx, m, n, k) ? packed_bytes(m, k) : 0) +
+         (packs(k, ldw, m, n, k) ? packed_bytes(n, k) : 0) + (sx > sw ? sx : sw);
 }
 
 template <class T>
 int backward(const void* dy, int64_t lddy, const void* z, int64_t ldz, const void* x, int64_t ldx, const void* w, int64_t ldw,
              int64_t m, int64_t n, int64_t k, int act, void* dx, int64_t lddx, void* dw, int64_t lddw, float* db, void* ws,
              hipStream_t st) {
+  Carve at{static_cast<char*>(ws)};
+  float* part = at.take<float>(sums_bytes(m, n));
   const void* d = dy;
   int64_t ldd = lddy;
   T* dz = nullptr;
-  float* part = static_cast<float*>(ws);
-  if (act != XMEM_ACT_NONE && (dx || dw)) {
-    dz = reinterpret_cast<T*>(static_cast<char*>(ws) + part_bytes_of(m, n));
-    d = dz;
-    ldd = padded(n);
+  if (keeps_dz(m, n, k, lddy, act)) {
+    T* to = at.take<T>(packed_bytes(m, n));
+    if (dx || dw) {
+      dz = to;
+      d = to;
+      ldd = packed_ld(n);
+    }
   }
   if ((dz || db) && m > 0 && n > 0)
     for (int64_t b0 = 0; b0 < bands(m, n); b0 += 32768) {  // grid y is at most 65535
@@ -221,12 +269,20 @@ int backward(const void* dy, int64_t lddy, const void* z, int64_t ldz, const voi
           dz ? dz + r0 * ldd : nullptr, ldd, sums, int(band_rows(m, n)));
     }
   if (db && n > 0 && bands(m, n) != 1) k_db<<<unsigned((n + 63) / 64), 1024, 0, st>>>(part, bands(m, n), n, db);
+  GemmArgs gx{d, w, ldd, ldw, 0, 0, m, k, n, dz != nullptr}, gw{d, x, ldd, ldx, 0, 0, n, k, m, dz != nullptr};
+  Pack px{}, pw{};
+  if (packs(k, ldx, m, n, k)) {
+    px = {dw ? x : nullptr, ldx, m, k, at.take<char>(packed_bytes(m, k))};
+    gw.b = px.to, gw.ldb = packed_ld(k), gw.pad_b = true;
+  }
+  if (packs(k, ldw, m, n, k)) {
+    pw = {dx ? w : nullptr, ldw, n, k, at.take<char>(packed_bytes(n, k))};
+    gx.b = pw.to, gx.ldb = packed_ld(k), gx.pad_b = true;
+  }
+  if (m > 0 && n > 0) pack<T>(px, pw, st);
   int rc = launched();
-  void* split = static_cast<char*>(ws) + part_bytes_of(m, n) + dz_bytes(m, n, act);
-  if (rc == XMEM_OK && dx)
-    rc = gemm<T, true, false>(GemmArgs{d, w, ldd, ldw, 0, 0, m, k, n, dz != nullptr}, StoreEpilogue<T>{static_cast<T*>(dx), lddx}, split, st);
-  if (rc == XMEM_OK && dw)
-    rc = gemm<T, false, false>(GemmArgs{d, x, ldd, ldx, 0, 0, n, k, m, dz != nullptr}, StoreEpilogue<T>{static_cast<T*>(dw), lddw}, split, st);
+  if (rc == XMEM_OK && dx) rc = gemm<T, true, false>(gx, StoreEpilogue<T>{static_cast<T*>(dx), lddx}, at.at, st);
+  if (rc == XMEM_OK && dw) rc = gemm<T, false, false>(gw, StoreEpilogue<T>{static_cast<T*>(dw), lddw}, at.at, st);
   return rc;
 }
 
@@ -236,8 +292,8 @@ bool known(int dtype, int act) { return (dtype == XMEM_BF16 || dtype == XMEM_F16
 
 extern "C" {
 
-size_t xmem_linear_forward_workspace_bytes(int64_t m, int64_t n, int64_t k) {
-  return sizes_ok(m, n, k) ? part_bytes(m, n, k, 1, false) : 0;
+size_t xmem_linear_forward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
+  return sizes_ok(m, n, k) && ld_ok(ldx, k) && ld_ok(ldw, k) ? forward_bytes(m, n, k, ldx, ldw) : 0;
 }
 
 int xmem_linear_forward(const void* d_x, int64_t ldx, const void* d_w, int64_t ldw, const float* d_bias,
@@ -249,7 +305,7 @@ int xmem_linear_forward(const void* d_x, int64_t ldx, const void* d_w, int64_t l
     return XMEM_EINVAL;
   if (m == 0 || n == 0) return XMEM_OK;
   if (!d_y || (k > 0 && (!d_x || !d_w))) return XMEM_EINVAL;
-  const size_t need = xmem_linear_forward_workspace_bytes(m, n, k);
+  const size_t need = forward_bytes(m, n, k, ldx, ldw);
   if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 256))) return XMEM_EWORKSPACE;
   if (!need) d_workspace = nullptr;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -257,10 +313,10 @@ int xmem_linear_forward(const void* d_x, int64_t ldx, const void* d_w, int64_t l
                                                              d_y, ldy, d_z, ldz, d_workspace, st);
 }
 
-size_t xmem_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int activation) {
-  if (!sizes_ok(m, n, k) || !known(XMEM_BF16, activation)) return 0;
-  const size_t sx = part_bytes(m, k, n, 1, false), sw = part_bytes(n, k, m, 1, false);
-  return part_bytes_of(m, n) + dz_bytes(m, n, activation) + (sx > sw ? sx : sw);
+size_t xmem_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t lddy, int64_t ldx, int64_t ldw, int activation) {
+  return sizes_ok(m, n, k) && ld_ok(lddy, n) && ld_ok(ldx, k) && ld_ok(ldw, k) && known(XMEM_BF16, activation)
+             ? backward_bytes(m, n, k, lddy, ldx, ldw, activation)
+             : 0;
 }
 
 int xmem_linear_backward(const void* d_dy, int64_t lddy, const void* d_z, int64_t ldz, const void* d_x, int64_t ldx,
@@ -269,7 +325,7 @@ int xmem_linear_backward(const void* d_dy, int64_t lddy, const void* d_z, int64_
                          size_t workspace_bytes, void* hip_stream) {
   if (!sizes_ok(m, n, k) || !known(dtype, activation)) return XMEM_EINVAL;
   if (activation == XMEM_ACT_NONE) d_z = nullptr;  // its slope is 1 everywhere
-  if (!ld_ok(lddy, n) || (d_z && !ld_ok(ldz, n)) || (d_dw && !ld_ok(ldx, k)) || (d_dx && !ld_ok(ldw, k)) ||
+  if (!ld_ok(lddy, n) || (d_z && !ld_ok(ldz, n)) || !ld_ok(ldx, k) || !ld_ok(ldw, k) ||
       (d_dx && !ld_ok(lddx, k)) || (d_dw && !ld_ok(lddw, k)))
     return XMEM_EINVAL;
   if (!d_dx && !d_dw && !d_db) return XMEM_OK;
@@ -277,7 +333,7 @@ int xmem_linear_backward(const void* d_dy, int64_t lddy, const void* d_z, int64_
     if (!d_dy || (activation != XMEM_ACT_NONE && !d_z)) return XMEM_EINVAL;
     if (k > 0 && ((d_dx && !d_w) || (d_dw && !d_x))) return XMEM_EINVAL;
   }
-  const size_t need = xmem_linear_backward_workspace_bytes(m, n, k, activation);
+  const size_t need = backward_bytes(m, n, k, lddy, ldx, ldw, activation);
   if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 256))) return XMEM_EWORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   return (dtype == XMEM_BF16 ? backward<bf16> : backward<f16>)(d_dy, lddy, d_z, ldz, d_x, ldx, d_w, ldw, m, n, k, activation,

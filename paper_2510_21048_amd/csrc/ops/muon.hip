@@ -31,13 +31,13 @@ constexpr int64_t kMostCount = 65535, kMostSide = int64_t(1) << 24;
 
 struct Shape {
   int64_t count, rows, cols, s, l;  // s <= l
-  int64_t lds, ldx;                 // row lengths of P, Q and of X, padded to 8
+  int64_t lds, ldx;                 // row lengths of P, Q and of X: whole pieces of 64 bytes
   bool tall;                        // rows > cols: X lies as [l, s]
 };
 Shape shape_of(int64_t count, int64_t rows, int64_t cols) {
   Shape h{count, rows, cols, rows < cols ? rows : cols, rows < cols ? cols : rows, 0, 0, rows > cols};
-  h.lds = (h.s + 7) & ~int64_t(7);
-  h.ldx = (cols + 7) & ~int64_t(7);
+  h.lds = (h.s + 31) & ~int64_t(31);
+  h.ldx = (cols + 31) & ~int64_t(31);
   return h;
 }
 
@@ -141,7 +141,7 @@ __global__ void k_clear_pads(f16* p, int64_t rows, int64_t cols, int64_t ld) {
 // P = X X^T without its diagonal, which goes to d.  Only tiles on or below the diagonal are computed, and each
 // entry below it is written to its mirrored place too.
 struct GramEpilogue {
-  static constexpr bool kSymmetric = true;
+  static constexpr bool kSymmetric = true, kPastL2 = false;  // what it writes is read next
   template <class F>
   __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
   f16* p;
@@ -179,7 +179,7 @@ struct GramEpilogue {
 
 // Q = b P + c P P without its diagonal.
 struct PolyEpilogue {
-  static constexpr bool kSymmetric = true;
+  static constexpr bool kSymmetric = true, kPastL2 = false;  // what it writes is read next
   template <class F>
   __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
   const f16* p;
@@ -226,13 +226,14 @@ struct PolyEpilogue {
 // X <- (a + q_ii) X_i + (Q X)_i.  The diagonal's index is the row where X lies as [s, l], the column else.
 template <bool TALL>
 struct StepEpilogue {
-  static constexpr bool kSymmetric = false;
+  static constexpr bool kSymmetric = false, kPastL2 = true;
+  bool lines() const { return out ? whole_lines(out, cols) : whole_lines(nx, ld) && whole_lines(nlo, ld); }
   template <class F>
   __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
   const f16 *x, *lo;  // lo, nlo: NULL where X is kept in one half
   const float* dq;
   f16 *nx, *nlo;
-  int64_t ld, s;
+  int64_t ld, s, cols;
   bf16* out;  // the last step writes the update instead
   float scale;
 
@@ -334,10 +335,10 @@ int update(const G* g, float* mom, const Shape& h, float mu, bool nesterov, int 
     f16 *nx = w.x[~i & 1], *nlo = i + 1 < steps - kOneHalf ? w.lo[~i & 1] : nullptr;
     if (h.tall)
       rc = gemm<f16, true, true>(args(x, h.ldx, sx, w.q, h.lds, sp, h.l, h.s, h.s),
-                                 StepEpilogue<true>{x, lo, w.dq, nx, nlo, h.ldx, h.s, to, scale}, w.split, st);
+                                 StepEpilogue<true>{x, lo, w.dq, nx, nlo, h.ldx, h.s, h.cols, to, scale}, w.split, st);
     else
       rc = gemm<f16, true, false>(args(w.q, h.lds, sp, x, h.ldx, sx, h.s, h.l, h.s),
-                                  StepEpilogue<false>{x, lo, w.dq, nx, nlo, h.ldx, h.s, to, scale}, w.split, st);
+                                  StepEpilogue<false>{x, lo, w.dq, nx, nlo, h.ldx, h.s, h.cols, to, scale}, w.split, st);
   }
   return rc;
 }

@@ -36,9 +36,9 @@ def load_ops():
         lib = ctypes.CDLL(str(_LIB_PATH))
         vp, i64, i32, f32, size = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
         for name, args, res in (
-            ("xmem_linear_forward_workspace_bytes", [i64] * 3, size),
+            ("xmem_linear_forward_workspace_bytes", [i64] * 5, size),
             ("xmem_linear_forward", [vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, size, vp], i32),
-            ("xmem_linear_backward_workspace_bytes", [i64] * 3 + [i32], size),
+            ("xmem_linear_backward_workspace_bytes", [i64] * 6 + [i32], size),
             ("xmem_linear_backward", [vp, i64] * 4 + [i64] * 3 + [i32] * 2 + [vp, i64] * 2 + [vp, vp, size, vp], i32),
             ("xmem_policy_loss_workspace_bytes", [i64] * 2, size),
             ("xmem_policy_loss", [vp, i64] + [vp] * 5 + [i64] * 2 + [i32] + [f32] * 4 + [vp] * 3 + [i64, vp, size, vp], i32),
@@ -56,8 +56,8 @@ def load_ops():
 # ---------------------------------------------------------------- the C ABI
 
 
-def xmem_linear_forward_workspace_bytes(m: int, n: int, k: int) -> int:
-    return load_ops().xmem_linear_forward_workspace_bytes(m, n, k)
+def xmem_linear_forward_workspace_bytes(m: int, n: int, k: int, ldx: int, ldw: int) -> int:
+    return load_ops().xmem_linear_forward_workspace_bytes(m, n, k, ldx, ldw)
 
 
 def xmem_linear_forward(d_x, ldx, d_w, ldw, d_bias, d_residual, ldr, m, n, k, dtype, activation, d_y, ldy, d_z, ldz,
@@ -67,8 +67,8 @@ def xmem_linear_forward(d_x, ldx, d_w, ldw, d_bias, d_residual, ldr, m, n, k, dt
                                           _ptr(stream))
 
 
-def xmem_linear_backward_workspace_bytes(m: int, n: int, k: int, activation: int) -> int:
-    return load_ops().xmem_linear_backward_workspace_bytes(m, n, k, activation)
+def xmem_linear_backward_workspace_bytes(m: int, n: int, k: int, lddy: int, ldx: int, ldw: int, activation: int) -> int:
+    return load_ops().xmem_linear_backward_workspace_bytes(m, n, k, lddy, ldx, ldw, activation)
 
 
 def xmem_linear_backward(d_dy, lddy, d_z, ldz, d_x, ldx, d_w, ldw, m, n, k, dtype, activation, d_dx, lddx, d_dw, lddw, d_db,
@@ -184,7 +184,7 @@ def linear_forward(x, w, bias=None, residual=None, activation: str = "none", sav
     _vector(bias, "bias", n, torch.float32, dev)
     y = torch.empty((m, n), dtype=x.dtype, device=dev)
     z = torch.empty((m, n), dtype=x.dtype, device=dev) if save_z else None
-    workspace, size = _workspace(workspace, lib.xmem_linear_forward_workspace_bytes(m, n, k), dev)
+    workspace, size = _workspace(workspace, lib.xmem_linear_forward_workspace_bytes(m, n, k, ldx, ldw), dev)
     _check(xmem_linear_forward(x, ldx, w, ldw, bias, residual, ldr, m, n, k, code, act, y, n, z, n, workspace, size,
                                _raw_stream(dev, stream)), "xmem_linear_forward")
     return y, z
@@ -208,7 +208,7 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", need_dx: bool = 
     dx = torch.empty((m, k), dtype=dy.dtype, device=dev) if need_dx else None
     dw = torch.empty((n, k), dtype=dy.dtype, device=dev) if need_dw else None
     db = torch.empty(n, dtype=torch.float32, device=dev) if need_db else None
-    workspace, size = _workspace(workspace, xmem_linear_backward_workspace_bytes(m, n, k, act), dev)
+    workspace, size = _workspace(workspace, xmem_linear_backward_workspace_bytes(m, n, k, lddy, ldx, ldw, act), dev)
     _check(xmem_linear_backward(dy, lddy, z, ldz, x, ldx, w, ldw, m, n, k, code, act, dx, k, dw, k, db, workspace, size,
                                 _raw_stream(dev, stream)), "xmem_linear_backward")
     return dx, dw, db

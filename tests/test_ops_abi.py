@@ -61,8 +61,8 @@ def test_linear_backward_refuses(over):
 
 
 def test_linear_backward_workspace():
-    need = xm.xmem_linear_backward_workspace_bytes(8, 32, 64, 2)
-    assert need > 0 and xm.xmem_linear_backward_workspace_bytes(8, -32, 64, 2) == 0
+    need = xm.xmem_linear_backward_workspace_bytes(8, 32, 64, 32, 64, 64, 2)
+    assert need > 0 and xm.xmem_linear_backward_workspace_bytes(8, -32, 64, 32, 64, 64, 2) == 0
     for over in (dict(size=need - 1), dict(ws=None), dict(ws=(1 << 20) + 8)):
         assert backward(**over) == EWORKSPACE
     assert backward(dx=None, dw=None, db=None) == OK
