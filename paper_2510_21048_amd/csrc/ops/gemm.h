@@ -25,18 +25,20 @@ struct GemmArgs {
 };
 
 // A workgroup's tile and its wavefronts: WM by WN of them, each with BM / WM by BN / WN of the tile, WK times over: each
-// such group takes every WK-th k tile, and their sums are added in LDS.  STAGES k tiles of a group are in LDS, all but
-// one of them on their way (a power of two); through registers, DEPTH k tiles are.
-template <int BM_, int BN_, int WM_, int WN_, int WK_, int STAGES_, int DEPTH_>
+// such group takes every WK-th k tile, and their sums are added in LDS.  Two k tiles of a group are in LDS, one of them
+// on its way.  STAGED: whether there is a form whose loads go through registers.
+// More k tiles on their way (four of the 128 tile, eight of the 64) in place of more groups: 1024 x 1024 x 1024 10.6 us against 9.4.
+template <int BM_, int BN_, int WM_, int WN_, int WK_, bool STAGED_>
 struct Config {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WK = WK_, FM = BM / WM / 16, FN = BN / WN / 16;
+  static constexpr int GROUP = 64 * WM * WN, THREADS = GROUP * WK;
+  static constexpr bool STAGED = STAGED_;
   static_assert(FN % 2 == 0);
-  static constexpr int GROUP = 64 * WM * WN, THREADS = GROUP * WK, STAGES = STAGES_, DEPTH = DEPTH_;
 };
-typedef Config<256, 256, 2, 4, 1, 2, 0> Large;   // 128 KiB of LDS, two wavefronts on a SIMD: a CU to itself
-typedef Config<128, 128, 2, 2, 2, 2, 1> Medium;  // 128 KiB, two wavefronts on a SIMD
-typedef Config<64, 64, 2, 2, 4, 2, 1> Small;     // 128 KiB, four wavefronts on a SIMD
-typedef Config<64, 64, 2, 2, 2, 2, 1> Half;      // 64 KiB, two workgroups a CU: where there are more tiles than CUs
+typedef Config<256, 256, 2, 4, 1, false> Large;  // 128 KiB of LDS, two wavefronts on a SIMD: a CU to itself
+typedef Config<128, 128, 2, 2, 2, true> Medium;  // 128 KiB, two wavefronts on a SIMD
+typedef Config<64, 64, 2, 2, 4, true> Small;     // 128 KiB, four wavefronts on a SIMD
+typedef Config<64, 64, 2, 2, 2, true> Half;      // 64 KiB, two workgroups a CU: where there are more tiles than CUs
 
 // One operand tile in LDS: R rows of kBK.  Chunks of 16 bytes are kept at swizzled places, so that the 16 lanes
 // that read one column of chunks meet 16 different bank groups.
@@ -286,8 +288,8 @@ __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[
 
 // One workgroup's tile.  Half a tile's operands are in registers ahead of the matrix instructions: while the products of
 // one half run, the other half's LDS reads are under way.  One barrier a k tile: after it the tile just read is
-// overwritten by the loads of the tile STAGES on (direct), or the next tile, stored from registers while the
-// first half ran, is complete (staged, two LDS buffers).
+// overwritten by the loads of the tile after next (direct), or the next tile, stored from registers while the
+// first half ran, is complete (staged).
 // The n side is the first operand of the matrix instruction, so that a lane ends with neighbouring n of one m.
 template <class T, class C, bool AKC, bool BKC, bool DIRECT, bool PAST_L2, class Epi>
 __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
@@ -297,8 +299,8 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
   typedef Tile<T, C::BN, BKC> TB;
   constexpr int BUF = TA::kBytes + TB::kBytes, kReads = FM * (AKC ? 1 : 2) + FN * (BKC ? 1 : 2);
   typedef typename Vec<T>::x8 x8;
-  constexpr int BUFS = DIRECT ? C::STAGES : 2, LOADS = (TA::kChunks + TB::kChunks) / C::GROUP;
-  constexpr int SUMS = C::WK > 1 ? FM * FN * 16 * C::THREADS : 0, BYTES = C::WK * BUFS * BUF;
+  constexpr int LOADS = (TA::kChunks + TB::kChunks) / C::GROUP;
+  constexpr int SUMS = C::WK > 1 ? FM * FN * 16 * C::THREADS : 0, BYTES = C::WK * 2 * BUF;
   __shared__ __attribute__((aligned(1024))) char all_lds[BYTES > SUMS ? BYTES : SUMS];
   int id = run_of(blockIdx.x, gridDim.x), tm, tn;
   const int z = id / (g.tiles * g.splits);
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
   const int64_t m0 = int64_t(tm) * C::BM, n0 = int64_t(tn) * C::BN;
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / C::GROUP), tid = threadIdx.x % C::GROUP;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  char* const lds = all_lds + group * (BUFS * BUF);
+  char* const lds = all_lds + group * (2 * BUF);
   const int wm = (wave / C::WN) * (C::BM / C::WM), wn = (wave % C::WN) * (C::BN / C::WN);
   const int t0 = split * g.span, ks = int(g.k) < (t0 + g.span) * kBK ? int(g.k) : (t0 + g.span) * kBK;
   // a group's tiles are t0 + group, + WK, ..., numbered 0 to passes; past the last k tile the operands are 0
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
     for (int j = 0; j < FN; ++j) acc[i][j] = {0, 0, 0, 0};
   x8 a0[FM], b0[FN], a1[FM], b1[FN];
   const auto read = [&](x8(&fa)[FM], x8(&fb)[FN], int t, int s) {
-    const char* from = lds + (t & (BUFS - 1)) * BUF;
+    const char* from = lds + (t & 1) * BUF;
 #pragma unroll
     for (int j = 0; j < FN; ++j) fb[j] = TB::frag(from + TA::kBytes, wn + 16 * j, s, lane);
 #pragma unroll
@@ -341,29 +343,25 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
     la.init(tid, g.lda, m0, g.m);
     lb.init(tid, g.ldb, n0, g.n);
     const auto fetch = [&](int t) {
-      char* to = lds + (t & (BUFS - 1)) * BUF;
+      char* to = lds + (t & 1) * BUF;
       la.issue(to, a, g.lda, m0, g.m, tile_at(t), ks, wave);
       lb.issue(to + TA::kBytes, b, g.ldb, n0, g.n, tile_at(t), ks, wave);
     };
     if (passes > 0) {
-#pragma unroll
-      for (int i = 0; i < BUFS; ++i) {
-        if (i == BUFS - 1) {
-          asm volatile("s_waitcnt vmcnt(%0)" ::"n"((BUFS - 2) * LOADS) : "memory");
-          __builtin_amdgcn_s_barrier();
-        }
-        fetch(i);
-      }
+      fetch(0);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      fetch(1);
       read(a0, b0, 0, 0);
       for (int t = 0; t < passes; ++t) {
         read(a1, b1, t, 1);
         multiply(a0, b0);
         Order<0, kReads, FM * FN>::apply();
         // every read of this tile is done, and the next tile has come
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * LOADS) : "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        fetch(t + BUFS);
+        fetch(t + 2);
         read(a0, b0, t + 1, 0);
         multiply(a1, b1);
         Order<LOADS, kReads, FM * FN>::apply();
@@ -371,39 +369,31 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
   } else {
-    Staged<T, TA, C::BM, AKC, C::GROUP> la[C::DEPTH];
-    Staged<T, TB, C::BN, BKC, C::GROUP> lb[C::DEPTH];
+    Staged<T, TA, C::BM, AKC, C::GROUP> la;
+    Staged<T, TB, C::BN, BKC, C::GROUP> lb;
+    const auto load = [&](int t) {
+      la.load(tid, a, g.lda, m0, g.m, tile_at(t), ks);
+      lb.load(tid, b, g.ldb, n0, g.n, tile_at(t), ks);
+    };
+    const auto store = [&](int t) {
+      char* to = lds + (t & 1) * BUF;
+      la.store(tid, to);
+      lb.store(tid, to + TA::kBytes);
+    };
     if (passes > 0) {
-      const auto load = [&](int t, int i) {
-        if (t >= passes) return;
-        la[i].load(tid, a, g.lda, m0, g.m, tile_at(t), ks);
-        lb[i].load(tid, b, g.ldb, n0, g.n, tile_at(t), ks);
-      };
-      const auto store = [&](int t, int i) {
-        if (t >= passes) return;
-        char* to = lds + (t & (BUFS - 1)) * BUF;
-        la[i].store(tid, to);
-        lb[i].store(tid, to + TA::kBytes);
-      };
-      load(0, 0);
-      store(0, 0);
-#pragma unroll
-      for (int i = 0; i < C::DEPTH; ++i) load(1 + i, i);
+      load(0);
+      store(0);
+      if (passes > 1) load(1);
       __syncthreads();
       read(a0, b0, 0, 0);
-      for (int tt = 0; tt < passes; tt += C::DEPTH) {
-#pragma unroll
-        for (int i = 0; i < C::DEPTH; ++i) {
-          const int t = tt + i;
-          if (t >= passes) break;
-          read(a1, b1, t, 1);
-          multiply(a0, b0);
-          store(t + 1, i);
-          load(t + 1 + C::DEPTH, i);
-          __syncthreads();
-          if (t + 1 < passes) read(a0, b0, t + 1, 0);
-          multiply(a1, b1);
-        }
+      for (int t = 0; t < passes; ++t) {
+        read(a1, b1, t, 1);
+        multiply(a0, b0);
+        if (t + 1 < passes) store(t + 1);
+        if (t + 2 < passes) load(t + 2);
+        __syncthreads();
+        if (t + 1 < passes) read(a0, b0, t + 1, 0);
+        multiply(a1, b1);
       }
     }
   }
@@ -557,7 +547,7 @@ int launch(GemmArgs g, const Epi& epi, hipStream_t st) {
     }
   if (direct)
     k_gemm<T, C, AKC, BKC, true, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
-  else if constexpr (C::DEPTH > 0)
+  else if constexpr (C::STAGED)
     k_gemm<T, C, AKC, BKC, false, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
   else
     return launch<T, Medium, AKC, BKC>(g, epi, st);  // a tile's registers would not fit

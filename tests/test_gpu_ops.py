@@ -86,6 +86,50 @@ def test_linear_backward(i, size, dtype):
                 within(a, v, b, f"{name} {size} {act} pad={pad}")
 
 
+# Large tiles, whole and cut, in each of the three products; operands copied to aligned rows; k split over workgroups
+BIG = [(4096, 4096, 96), (4000, 4104, 136), (4104, 72, 4000), (72, 4104, 4000), (2049, 2051, 1023), (1500, 1528, 1030), (200, 136, 9000),
+       (64, 96, 20000), (30000, 64, 40), (5, 9001, 2048), (130, 130, 40)]
+
+
+@pytest.mark.parametrize("i,size", list(enumerate(BIG)), ids=["x".join(map(str, s)) for s in BIG])
+def test_linear_large_and_split(i, size):
+    m, n, k = size
+    for j, pad in enumerate((0, 3)):
+        dtype, act = (BF, HF)[(i + j) % 2], ACTS[(i + j) % 4]
+        g = torch.Generator().manual_seed(7000 + 10 * i + j)
+        x, xc = rows(g, m, k, dtype, pad)
+        w, wc = rows(g, n, k, dtype, pad, 1 / math.sqrt(k))
+        r, rc = rows(g, m, n, dtype, pad)
+        dy, dyc = rows(g, m, n, dtype, pad)
+        b = torch.randn(n, generator=g)
+        log(f"[ops] linear {size} {dtype} {act} pad={pad}")
+        y, z = xm.linear_forward(x, w, b.cuda(), r, activation=act, save_z=True)
+        torch.cuda.synchronize()
+        wy, wz, by, bz = ref.forward(xc, wc, b, rc, act)
+        within(y, wy, by, f"y {size} {act} pad={pad}")
+        within(z, wz, bz, f"z {size} {act} pad={pad}")
+        zc = z.cpu()
+        got = xm.linear_backward(dy, x, w, z, act)
+        torch.cuda.synchronize()
+        want, bound = ref.backward(dyc, xc, wc, zc, act)
+        for name, a, v, c in zip(("dx", "dw", "db"), got, want, bound):
+            within(a, v, c, f"{name} {size} {act} pad={pad}")
+
+
+def test_linear_unaligned_base():
+    """Operands that begin between 16-byte boundaries, though their rows are a multiple of 8 apart."""
+    g = torch.Generator().manual_seed(12)
+    m, n, k = 200, 168, 256
+    hold = [torch.randn(r * c + 8, generator=g).to(BF).cuda() for r, c in ((m, k), (n, k), (m, n))]
+    for off in (1, 4):
+        x, w, dy = (h[off:off + r * c].view(r, c) for h, (r, c) in zip(hold, ((m, k), (n, k), (m, n))))
+        wy, _, by, _ = ref.forward(x.cpu(), w.cpu(), None, None, "none")
+        within(xm.linear_forward(x, w)[0], wy, by, f"y off={off}")
+        want, bound = ref.backward(dy.cpu(), x.cpu(), w.cpu(), dy.cpu(), "none")
+        for name, a, v, c in zip(("dx", "dw", "db"), xm.linear_backward(dy, x, w), want, bound):
+            within(a, v, c, f"{name} off={off}")
+
+
 @pytest.mark.parametrize("act", ["none", "gelu", "silu"])
 def test_linear_gradients_against_differences(act):
     """dx and dw against central differences of sum(dy y) in 64 bits, step 1e-4 (its own error ~1e-8): what is left is
@@ -327,6 +371,21 @@ def test_muon_update(count, r, c, dtype):
         again = mom.cuda()
         assert torch.equal(up, xm.muon_update(grad.cuda(), again, mu=mu, nesterov=nesterov, steps=steps, scale=scale))
         assert torch.equal(m, again)
+
+
+@pytest.mark.parametrize("count,r,c", [(60, 520, 1040), (60, 1040, 520), (1, 3000, 2500), (2, 72, 9000), (2, 9000, 40)])
+def test_muon_update_large(count, r, c):
+    """Large tiles, whole and cut, and few rows with many columns (k split); the reference is computed on the GPU in 64 bits."""
+    g = torch.Generator(device="cuda").manual_seed(r)
+    grad = (1e-3 * torch.randn(count, r, c, generator=g, device="cuda")).to(BF)
+    mom = 1e-2 * torch.randn(count, r, c, generator=g, device="cuda")
+    m = mom.clone()
+    log(f"[ops] muon {count}x{r}x{c}")
+    up = xm.muon_update(grad, m)
+    wm, wu = ref.muon(grad, mom, 0.95, True, 5, 1.0)
+    assert float((m.double() - wm).abs().max()) <= 4 * ref.E * float(wm.abs().max() + 1)
+    far = ((up.double() - wu).flatten(1).norm(dim=1) / wu.flatten(1).norm(dim=1)).max()
+    assert float(far) < 1e-2, float(far)
 
 
 def test_muon_weak_directions():
