@@ -16,7 +16,7 @@ struct GemmArgs {
   int64_t lda, ldb;
   int64_t stride_a, stride_b;  // between the matrices of a batch, in elements
   int64_t m, n, k;
-  // the operand's storage holds whole rows of ld, a multiple of 8, and what pads a row is 0
+  // the operand's rows have room behind their ends up to a multiple of 8, and it holds zeros
   bool pad_a = false, pad_b = false;
   int64_t count = 1;
   // set by the launch
@@ -212,15 +212,27 @@ __device__ inline int run_of(int id, int total) {
   return x * per + (x < rest ? x : rest) + id / kXcds;
 }
 
-// Tile number -> tile: in groups of 8 tile rows, so that what an XCD works on at one time shares operand rows in its
-// L2; of a symmetric product only the tiles on and below the diagonal, row by row.
+// Tile number -> tile: in groups of 8 tile rows, column by column, so that what an XCD works on at one time shares operand
+// rows in its L2.  Of a symmetric product only the tiles on and below the diagonal: a group's columns left of its
+// rows' diagonal block, then that block row by row.
 template <bool SYMMETRIC>
 __device__ inline void tile_of(int id, const GemmArgs& g, int& tm, int& tn) {
   if constexpr (SYMMETRIC) {
-    tm = int((__builtin_sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.5f);
-    while ((tm + 1) * (tm + 2) / 2 <= id) ++tm;
-    while (tm * (tm + 1) / 2 > id) --tm;
-    tn = id - tm * (tm + 1) / 2;
+    int q = int((__builtin_sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.0625f);  // the groups before q hold 32 q q + 4 q tiles
+    while (32 * (q + 1) * (q + 1) + 4 * (q + 1) <= id) ++q;
+    while (32 * q * q + 4 * q > id) --q;
+    id -= 32 * q * q + 4 * q;
+    const int first = 8 * q, high = g.tiles_m - first < 8 ? g.tiles_m - first : 8;
+    if (id < high * first) {
+      tm = first + id % high;
+      tn = id / high;
+    } else {
+      id -= high * first;
+      int r = 0;
+      while ((r + 1) * (r + 2) / 2 <= id) ++r;
+      tm = first + r;
+      tn = first + id - r * (r + 1) / 2;
+    }
   } else {
     const int group = 8 * g.tiles_n, first = id / group * 8, high = g.tiles_m - first < 8 ? g.tiles_m - first : 8;
     tm = first + id % group % high;
@@ -491,14 +503,15 @@ inline size_t part_bytes(int64_t m, int64_t n, int64_t k, int64_t count, bool sy
   return p.splits > 1 ? up256(size_t(tiles_of(m, n, p.side, p.side, symmetric)) * count * p.splits * p.side * p.side * 4) : 0;
 }
 
-// A matrix [rows, cols] whose rows allow no 16-byte loads, as one whose rows are a multiple of 8 long, with zeros behind them.
+// Rows of copies and of workspace matrices are whole lines of 128 bytes, with zeros behind what they hold: a k tile of a row is
+// one line then, not two (5 steps of 5 matrices of 3859 x 4242 with rows of 64 bytes' multiples: PAD_FIGURES).
 struct Pack {
   const void* from;
   int64_t ld, rows, cols;
   void* to;
 };
 
-__host__ __device__ inline int64_t packed_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
+__host__ __device__ inline int64_t packed_ld(int64_t cols) { return (cols + 63) / 64 * 64; }
 template <class T>
 __global__ __launch_bounds__(256) void k_pack(Pack p0, Pack p1) {
   const Pack p = blockIdx.y ? p1 : p0;
@@ -566,7 +579,7 @@ int gemm(GemmArgs g, const Epi& epi, void* part, hipStream_t st) {
   g.part = static_cast<float*>(part);
   if (p.side == 256) return launch<T, Large, AKC, BKC>(g, epi, st);
   if (p.side == 128) return launch<T, Medium, AKC, BKC>(g, epi, st);
-  if (p.splits == 1 && tiles_of(g.m, g.n, 64, 64, Epi::kSymmetric) * g.count > kCus) return launch<T, Half, AKC, BKC>(g, epi, st);
+  if (tiles_of(g.m, g.n, 64, 64, Epi::kSymmetric) * g.count * p.splits > kCus) return launch<T, Half, AKC, BKC>(g, epi, st);
   return launch<T, Small, AKC, BKC>(g, epi, st);
 }
 

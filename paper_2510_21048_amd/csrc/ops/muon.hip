@@ -31,19 +31,19 @@ constexpr int64_t kMostCount = 65535, kMostSide = int64_t(1) << 24;
 
 struct Shape {
   int64_t count, rows, cols, s, l;  // s <= l
-  int64_t lds, ldx;                 // row lengths of P, Q and of X: whole pieces of 64 bytes
+  int64_t lds, ldx;                 // row lengths of P, Q and of X: whole lines
   bool tall;                        // rows > cols: X lies as [l, s]
 };
 Shape shape_of(int64_t count, int64_t rows, int64_t cols) {
   Shape h{count, rows, cols, rows < cols ? rows : cols, rows < cols ? cols : rows, 0, 0, rows > cols};
-  h.lds = (h.s + 31) & ~int64_t(31);
-  h.ldx = (cols + 31) & ~int64_t(31);
+  h.lds = packed_ld(h.s);
+  h.ldx = packed_ld(cols);
   return h;
 }
 
 struct Ws {
   f16 *x[2], *lo[2];  // X and its second half, before and after a step
-  f16 *p, *q;         // what pads their rows is 0, as X's is
+  f16 *p, *q;         // behind their rows' ends are zeros, as behind X's
   float *dp, *dq;  // diagonals
   double* part;
   void* split;  // partial sums of products whose k is split
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(kThreads) void k_momentum(const G* g, float* mom, i
   }
 }
 
-// X = u / (|u| + eps) in two halves; the columns that pad a row are 0.
+// X = u / (|u| + eps) in two halves; 0 behind a row's end, up to a multiple of 8.
 template <class G>
 __global__ __launch_bounds__(kThreads) void k_start(const G* g, const float* mom, int64_t rows, int64_t cols, int64_t ldx, float mu,
                                                     bool nesterov, const double* part, f16* x, f16* lo) {
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kThreads) void k_start(const G* g, const float* mom
   for (int i = 0; i < kNormParts / kWave; ++i) v += part[b * kNormParts + i * kWave + (threadIdx.x & 63)];
   v = wave_sum(v);
   const float inv = kX / (float(sqrt(v)) + kNormEps);
-  const unsigned pieces = unsigned(ldx / 8);
+  const unsigned pieces = unsigned((cols + 7) / 8);
   for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows * pieces; i += int64_t(gridDim.x) * kThreads) {
     const int64_t r = i / pieces, c = (i - r * pieces) * 8, at = (b * rows + r) * cols + c;
     const int valid = cols - c >= 8 ? 8 : int(cols - c);
@@ -132,9 +132,10 @@ __global__ __launch_bounds__(kThreads) void k_start(const G* g, const float* mom
   }
 }
 
-// Clears what pads the rows of a matrix [rows, cols] of row length ld.
+// Clears what is behind the rows of a matrix [rows, cols] of row length ld, up to a multiple of 8: what a piece of 16 bytes
+// reads with them.
 __global__ void k_clear_pads(f16* p, int64_t rows, int64_t cols, int64_t ld) {
-  const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, pad = ld - cols;
+  const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, pad = -cols & 7;
   if (i < rows * pad) p[i / pad * ld + cols + i % pad] = f16(0.0f);
 }
 
@@ -306,7 +307,7 @@ int update(const G* g, float* mom, const Shape& h, float mu, bool nesterov, int 
   const int64_t per = h.rows * h.cols;
   const unsigned z = unsigned(h.count);
   k_momentum<G><<<dim3(kNormParts, z), kThreads, 0, st>>>(g, mom, per, mu, nesterov, w.part);
-  k_start<G><<<dim3(blocks_of(h.rows * h.ldx / 8), z), kThreads, 0, st>>>(g, mom, h.rows, h.cols, h.ldx, mu, nesterov, w.part, w.x[0],
+  k_start<G><<<dim3(blocks_of(h.rows * ((h.cols + 7) / 8)), z), kThreads, 0, st>>>(g, mom, h.rows, h.cols, h.ldx, mu, nesterov, w.part, w.x[0],
                                                                    w.lo[0]);
   int rc = launched();
   if (steps == 0) {
@@ -315,7 +316,7 @@ int update(const G* g, float* mom, const Shape& h, float mu, bool nesterov, int 
   }
   const int64_t sx = h.rows * h.ldx, sp = h.s * h.lds;
   const auto clear = [&](f16* p, int64_t rows, int64_t cols, int64_t ld) {
-    if (ld > cols) k_clear_pads<<<unsigned((rows * (ld - cols) + 255) / 256), 256, 0, st>>>(p, rows, cols, ld);
+    if (cols % 8) k_clear_pads<<<unsigned((rows * (-cols & 7) + 255) / 256), 256, 0, st>>>(p, rows, cols, ld);
   };
   clear(w.x[1], h.count * h.rows, h.cols, h.ldx);
   clear(w.p, h.count * h.s, h.s, h.lds);
