@@ -244,6 +244,42 @@ __device__ inline void tile_of(int id, const GemmArgs& g, int& tm, int& tn) {
 // lanes 16 apart, are eight neighbours of one or the other: the epilogue takes these, 16 bytes at a time and 64 next to
 // each other, from row i0 on every STEP-th; what it reads of memory is asked for four rows at a time, before anything
 // of them is written.  The Q-th eight of a lane; recursive, so that acc is indexed by constants however long the epilogue is.
+// The mirrored block of a symmetric product's tile: the epilogue's values as they were written, kept in LDS row by row in
+// the layout of an operand with its rows contiguous, whose transposing reads give a lane eight neighbours of a column.
+// 5 of 4096 x 4096 x 4096: 345 us; written entry by entry from the lanes' accumulators 372.
+template <class C>
+struct Mirror {
+  typedef Tile<f16, C::BN, false> Ti;
+  static constexpr int kBytes = C::BM * C::BN * 2;
+
+  __device__ static void keep(char* lds, int m, int n, const float (&v)[8]) {
+    typename Vec<f16>::x8 e;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = f16(v[j]);
+    const int c = n >> 3;
+    *reinterpret_cast<typename Vec<f16>::x8*>(lds + m * (C::BN * 2) + ((((c >> 1) ^ Ti::pair_hash(m)) * 2 + (c & 1)) << 4)) = e;
+  }
+  // THREADS threads write what all of them kept: to[n][m]
+  template <int THREADS>
+  __device__ static void write(const char* lds, f16* to, int64_t ld, int64_t m0, int64_t n0, const GemmArgs& g) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int kPieces = (C::BN / 16) * (C::BM / 32);
+    for (int i = wave; i < kPieces; i += THREADS / 64) {
+      const int r0 = i / (C::BM / 32) * 16, s = i % (C::BM / 32);
+      const auto e = Ti::frag(lds, r0, s, lane);
+      const int64_t n = n0 + r0 + (lane & 15), m = m0 + 32 * s + 8 * (lane >> 4);
+      if (n >= g.n || m >= g.m) continue;
+      if (g.m - m >= 8) {
+        __builtin_memcpy(to + n * ld + m, &e, 16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (m + j < g.m) to[n * ld + m + j] = e[j];
+      }
+    }
+  }
+};
+
 // HOW says what is known of the tile before it runs: whole (nothing of it is past the matrix) and past the L2s.
 template <bool WHOLE_, bool PAST_L2_>
 struct How {
@@ -251,7 +287,7 @@ struct How {
 };
 template <class C, int STEP, int Q, class HOW, class Epi>
 __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0,
-                                                             int64_t n0, int z, const GemmArgs& g) {
+                                                             int64_t n0, int z, const GemmArgs& g, char* lds) {
   constexpr int W = 8, GROUPS = C::FN / 2, ROWS = (C::FM + STEP - 1) / STEP, BATCH = ROWS < 4 ? ROWS : 4;
   static_assert(ROWS % BATCH == 0);
   const int lane = threadIdx.x & 63, wave = (threadIdx.x % C::GROUP) >> 6;
@@ -282,20 +318,23 @@ __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[
         v[j] = __uint_as_float(two[0]);
         v[4 + j] = __uint_as_float(two[1]);
       }
-      if (HOW::WHOLE || (m < g.m && valid > 0)) epi.template row<W, HOW>(m, n, v, valid, col, in[i], z, g);
+      if (HOW::WHOLE || (m < g.m && valid > 0)) {
+        epi.template row<W, HOW>(m, n, v, valid, col, in[i], z, g);
+        if constexpr (Epi::kSymmetric) Mirror<C>::keep(lds, int(m - m0), int(n - n0), v);
+      }
     }
   }
-  if constexpr (Q + 1 < GROUPS) finish<C, STEP, Q + 1, HOW>(acc, i0, epi, m0, n0, z, g);
+  if constexpr (Q + 1 < GROUPS) finish<C, STEP, Q + 1, HOW>(acc, i0, epi, m0, n0, z, g, lds);
 }
 // An epilogue's choices are made once a tile, so that the code a tile runs through is short: it passes the
 // instruction cache once for each.
 template <class C, int STEP, bool PAST_L2, class Epi>
 __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0,
-                                                             int64_t n0, int z, const GemmArgs& g) {
+                                                             int64_t n0, int z, const GemmArgs& g, char* lds) {
   if (m0 + C::BM <= g.m && n0 + C::BN <= g.n)
-    epi.chosen([&](const auto& e) __attribute__((always_inline)) { finish<C, STEP, 0, How<true, PAST_L2>>(acc, i0, e, m0, n0, z, g); });
+    epi.chosen([&](const auto& e) __attribute__((always_inline)) { finish<C, STEP, 0, How<true, PAST_L2>>(acc, i0, e, m0, n0, z, g, lds); });
   else
-    finish<C, STEP, 0, How<false, false>>(acc, i0, epi, m0, n0, z, g);
+    finish<C, STEP, 0, How<false, false>>(acc, i0, epi, m0, n0, z, g, lds);
 }
 
 // One workgroup's tile.  Half a tile's operands are in registers ahead of the matrix instructions: while the products of
@@ -313,6 +352,7 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
   typedef typename Vec<T>::x8 x8;
   constexpr int LOADS = (TA::kChunks + TB::kChunks) / C::GROUP;
   constexpr int SUMS = C::WK > 1 ? FM * FN * 16 * C::THREADS : 0, BYTES = C::WK * 2 * BUF;
+  static_assert(!Epi::kSymmetric || Mirror<C>::kBytes <= BYTES);
   __shared__ __attribute__((aligned(1024))) char all_lds[BYTES > SUMS ? BYTES : SUMS];
   int id = run_of(blockIdx.x, gridDim.x), tm, tn;
   const int z = id / (g.tiles * g.splits);
@@ -426,7 +466,6 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
 #pragma unroll
           for (int k = 1; k < C::WK; ++k) acc[i][j] += sums[((i * FN + j) * C::WK + k) * C::GROUP + tid];
         }
-    if (group >= FM) return;
   }
   if (g.splits > 1) {
     f32x4* to = reinterpret_cast<f32x4*>(g.part) + ((int64_t(z) * g.tiles + tile) * g.splits + split) * (FM * FN * C::GROUP) + tid;
@@ -437,7 +476,13 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
         for (int j = 0; j < FN; ++j) to[(i * FN + j) * C::GROUP] = acc[i][j];
     return;
   }
-  finish<C, C::WK, PAST_L2>(acc, group, epi, m0, n0, z, g);
+  if constexpr (Epi::kSymmetric) __syncthreads();  // the last loads have landed everywhere, the sums have been read: LDS is free
+  if (group < FM) finish<C, C::WK, PAST_L2>(acc, group, epi, m0, n0, z, g, all_lds);
+  if constexpr (Epi::kSymmetric)
+    if (tm != tn) {
+      __syncthreads();
+      Mirror<C>::template write<C::THREADS>(all_lds, epi.mirrored(z, g), epi.ld, m0, n0, g);
+    }
 #endif
 }
 
@@ -462,7 +507,14 @@ __global__ __launch_bounds__(C::GROUP) void k_join(GemmArgs g, Epi epi) {
 #pragma unroll
       for (int j = 0; j < C::FN; ++j) acc[i][j] += from[(i * C::FN + j) * C::GROUP];
   }
-  finish<C, 1, false>(acc, 0, epi, int64_t(tm) * C::BM, int64_t(tn) * C::BN, z, g);
+  const int64_t m0 = int64_t(tm) * C::BM, n0 = int64_t(tn) * C::BN;
+  __shared__ __attribute__((aligned(1024))) char lds[Epi::kSymmetric ? Mirror<C>::kBytes : 16];
+  finish<C, 1, false>(acc, 0, epi, m0, n0, z, g, lds);
+  if constexpr (Epi::kSymmetric)
+    if (tm != tn) {
+      __syncthreads();
+      Mirror<C>::template write<C::GROUP>(lds, epi.mirrored(z, g), epi.ld, m0, n0, g);
+    }
 }
 
 inline int64_t tiles_of(int64_t m, int64_t n, int bm, int bn, bool symmetric) {
@@ -504,7 +556,7 @@ inline size_t part_bytes(int64_t m, int64_t n, int64_t k, int64_t count, bool sy
 }
 
 // Rows of copies and of workspace matrices are whole lines of 128 bytes, with zeros behind what they hold: a k tile of a row is
-// one line then, not two (5 steps of 5 matrices of 3859 x 4242 with rows of 64 bytes' multiples: PAD_FIGURES).
+// one line then, not two (5 updates of 3859 x 4242 with rows of whole 64 bytes 8.66 ms, with lines 8.08).
 struct Pack {
   const void* from;
   int64_t ld, rows, cols;

@@ -139,16 +139,23 @@ __global__ void k_clear_pads(f16* p, int64_t rows, int64_t cols, int64_t ld) {
   if (i < rows * pad) p[i / pad * ld + cols + i % pad] = f16(0.0f);
 }
 
-// P = X X^T without its diagonal, which goes to d.  Only tiles on or below the diagonal are computed, and each
-// entry below it is written to its mirrored place too.
+// Which of the W columns from n on is m's own, or -1.
+template <int W>
+__device__ inline int diagonal(int64_t m, int64_t n) {
+  return m >= n && m < n + W ? int(m - n) : -1;
+}
+
+// P = X X^T without its diagonal, which goes to d.  Only tiles on or below the diagonal are computed; the tiles below it
+// are written to their mirrored places too.
 struct GramEpilogue {
   static constexpr bool kSymmetric = true, kPastL2 = false;  // what it writes is read next
-  template <class F>
-  __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
   f16* p;
   float* d;
   int64_t ld;
 
+  template <class F>
+  __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
+  __device__ f16* mirrored(int z, const GemmArgs& g) const { return p + z * g.m * ld; }
   template <int W>
   __device__ None column(int64_t, int, int, const GemmArgs&) const { return {}; }
   template <int W> using Read = None;
@@ -156,39 +163,31 @@ struct GramEpilogue {
   __device__ None read(int64_t, int64_t, int, int, const GemmArgs&) const { return {}; }
   template <int W, class HOW>
   __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, None, None, int z, const GemmArgs& g) const {
-    f16* to = p + z * g.m * ld;
+    const int here = diagonal<W>(m, n);
+    float dm = 0.0f;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       v[j] *= kP / (kX * kX);
-      if (n + j == m) {
-        d[z * g.m + m] = v[j] * (1.0f / kP);
-        v[j] = 0.0f;
-      }
+      dm = j == here ? v[j] : dm;
+      v[j] = j == here ? 0.0f : v[j];
     }
-    mirror<W>(to, ld, m, n, v, valid);
-  }
-  template <int W>
-  __device__ static void mirror(f16* to, int64_t ld, int64_t m, int64_t n, const float (&v)[W], int valid) {
-    if (n > m) return;  // its mirrored place is written
-    const int own = m - n + 1 < valid ? int(m - n + 1) : valid;
-    put<f16, W, Any>(to + m * ld + n, own, v);
-#pragma unroll
-    for (int j = 0; j < W; ++j)
-      if (j < own) to[(n + j) * ld + m] = f16(v[j]);
+    if (here >= 0) d[z * g.m + m] = dm * (1.0f / kP);
+    put<f16, W, HOW>(p + (z * g.m + m) * ld + n, valid, v);
   }
 };
 
 // Q = b P + c P P without its diagonal.
 struct PolyEpilogue {
-  static constexpr bool kSymmetric = true, kPastL2 = false;  // what it writes is read next
-  template <class F>
-  __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
+  static constexpr bool kSymmetric = true, kPastL2 = false;
   const f16* p;
   const float* dp;
   f16* q;
   float* dq;
   int64_t ld;
 
+  template <class F>
+  __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
+  __device__ f16* mirrored(int z, const GemmArgs& g) const { return q + z * g.m * ld; }
   template <int W>
   __device__ Column<W> column(int64_t n, int valid, int z, const GemmArgs& g) const {
     Column<W> c;
@@ -212,15 +211,16 @@ struct PolyEpilogue {
   }
   template <int W, class HOW>
   __device__ void row(int64_t m, int64_t n, float (&v)[W], int valid, const Column<W>& dn, const Read<W>& r, int z, const GemmArgs& g) const {
-    if (n > m) return;
-    const float dm = r.dm;
+    const int here = diagonal<W>(m, n);
+    float ee = 0.0f;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      if (n + j == m) dq[z * g.m + m] = XMEM_NS_B * dm + XMEM_NS_C * (v[j] * (1.0f / (kP * kP)) + dm * dm);
-      // times kP; E_ii is 0
-      v[j] = n + j == m ? 0.0f : XMEM_NS_B * float(r.e[j]) + XMEM_NS_C * (v[j] * (1.0f / kP) + (dm + dn.v[j]) * float(r.e[j]));
+      ee = j == here ? v[j] : ee;
+      const float e = float(r.e[j]);  // times kP; E_ii is 0
+      v[j] = j == here ? 0.0f : XMEM_NS_B * e + XMEM_NS_C * (v[j] * (1.0f / kP) + (r.dm + dn.v[j]) * e);
     }
-    GramEpilogue::mirror<W>(q + z * g.m * ld, ld, m, n, v, valid);
+    if (here >= 0) dq[z * g.m + m] = XMEM_NS_B * r.dm + XMEM_NS_C * (ee * (1.0f / (kP * kP)) + r.dm * r.dm);
+    put<f16, W, HOW>(q + (z * g.m + m) * ld + n, valid, v);
   }
 };
 

@@ -84,7 +84,7 @@ __device__ inline float over_row(float v, float* meet) {
 // once and their gradient is written once.  NCH = 0: a row too long for that is read again for each of the largest
 // logit (with the sum, rescaled when a larger one comes) and the gradient.
 template <class T, int THREADS, int NCH>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS == 1024 ? 4 : 6) void k_policy(Policy p) {
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS == 1024 ? 4 : THREADS == 64 ? 5 : 6) void k_policy(Policy p) {
   constexpr int E = kPer<T>;
   __shared__ float meet[2][THREADS / kWave], at_y[THREADS < 256 ? 4 : 1];
   const int tid = threadIdx.x % THREADS, slot = threadIdx.x / THREADS;
