@@ -144,45 +144,58 @@ __device__ inline u32x4 drop(u32x4 v, int s) {
 }
 
 // One operand's loads through registers, for rows of any alignment.  A chunk that passes the end of its row is read
-// from further back, so that it ends there, and shifted: every load is 16 bytes and inside the matrix, none is
-// behind a branch.  Rows shorter than 8 elements are read one by one.
+// from further back, so that it ends there, and shifted when it is stored: every load is 16 bytes and inside the
+// matrix, none waits for another or is behind a branch of its own.  Rows shorter than 8 elements are read one by one.
 template <class T, class Ti, int R, bool KC, int THREADS>
 struct Staged {
   static constexpr int kLoads = Ti::kChunks / THREADS;
   u32x4 v[kLoads];
+  int past[kLoads];  // elements of a chunk that its row does not have
+  bool whole;
 
   __device__ void load(int tid, const T* p, int64_t ld, int64_t r0, int64_t rows, int t, int ks) {
-    const int64_t k0 = int64_t(t) * kBK;
-    const int64_t length = KC ? ks : rows;  // of the contiguous side
-    const bool inside = r0 + R <= rows && k0 + kBK <= ks;
+    const int64_t k0 = int64_t(t) * kBK, length = KC ? ks : rows;  // of the contiguous side
+    whole = r0 + R <= rows && k0 + kBK <= ks;
+    if (whole) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        int row, k;
+        Ti::at(j * THREADS + tid, row, k);
+        __builtin_memcpy(&v[j], KC ? p + (r0 + row) * ld + k0 + k : p + (k0 + k) * ld + r0 + row, 16);
+      }
+      return;
+    }
+    const T* from[kLoads];
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       int row, k;
       Ti::at(j * THREADS + tid, row, k);
-      const int64_t gr = r0 + row, gk = k0 + k;
-      if (inside) {
-        __builtin_memcpy(&v[j], KC ? p + gr * ld + gk : p + gk * ld + gr, 16);
-        continue;
-      }
-      const int64_t along = KC ? gk : gr, across = KC ? gr : gk, last = (KC ? rows : int64_t(ks)) - 1;
+      const int64_t along = KC ? k0 + k : r0 + row, across = KC ? r0 + row : k0 + k, last = (KC ? rows : int64_t(ks)) - 1;
       const int64_t valid = across <= last ? length - along : 0;
-      const T* line = p + (across <= last ? across : last) * ld;
-      if (length >= 8) {
-        const int s = valid >= 8 ? 0 : valid <= 0 ? 8 : int(8 - valid);
-        u32x4 e;
-        __builtin_memcpy(&e, line + (s == 8 ? 0 : along - s), 16);
-        v[j] = drop(e, s);
-      } else {
+      past[j] = valid >= 8 ? 0 : valid <= 0 ? 8 : int(8 - valid);
+      from[j] = p + (across <= last ? across : last) * ld + (past[j] == 8 ? 0 : along - past[j]);
+    }
+    if (length >= 8) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) __builtin_memcpy(&v[j], from[j], 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {  // from[j] + past[j] is the chunk's first element; what is read ends its 8
         T e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i < valid ? line[along + i] : T(0.0f);
+        for (int i = 0; i < 8; ++i) e[i] = i >= past[j] ? from[j][i] : T(0.0f);
         __builtin_memcpy(&v[j], e, 16);
       }
     }
   }
   __device__ void store(int tid, char* lds) const {
+    if (whole) {
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(lds + (j * THREADS + tid) * 16) = v[j];
+      for (int j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(lds + (j * THREADS + tid) * 16) = v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(lds + (j * THREADS + tid) * 16) = drop(v[j], past[j]);
+    }
   }
 };
 
@@ -594,8 +607,9 @@ inline void pack(const Pack& a, const Pack& b, hipStream_t st) {
   if (blocks > 0) k_pack<T><<<dim3(unsigned(blocks < 8192 ? blocks : 8192), both ? 2 : 1), 256, 0, st>>>(first, b);
 }
 
+constexpr int64_t kMostDirectLd = int64_t(1) << 21;
 inline bool direct_ok(const void* p, int64_t ld, int64_t stride, int64_t contiguous, bool padded) {
-  return aligned(p, 16) && ld % 8 == 0 && stride % 8 == 0 && ld < (int64_t(1) << 21) && (contiguous % 8 == 0 || padded);
+  return aligned(p, 16) && ld % 8 == 0 && stride % 8 == 0 && ld < kMostDirectLd && (contiguous % 8 == 0 || padded);
 }
 
 template <class T, class C, bool AKC, bool BKC, class Epi>
@@ -612,6 +626,8 @@ int launch(GemmArgs g, const Epi& epi, hipStream_t st) {
     }
   if (direct)
     k_gemm<T, C, AKC, BKC, true, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
+  else if constexpr (!Epi::kAnyRows)
+    return XMEM_EINVAL;  // operands of the library's own workspace, aligned by construction
   else if constexpr (C::STAGED)
     k_gemm<T, C, AKC, BKC, false, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
   else

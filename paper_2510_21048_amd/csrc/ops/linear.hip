@@ -35,7 +35,7 @@ __device__ inline float slope(float z, int act) {
 // ACT < 0: the activation is `act`.
 template <class T, int ACT = -1>
 struct LinearEpilogue {
-  static constexpr bool kSymmetric = false, kPastL2 = true;
+  static constexpr bool kSymmetric = false, kPastL2 = true, kAnyRows = true;
   const float* bias;
   const T* r;
   T* y;
@@ -94,7 +94,7 @@ struct LinearEpilogue {
 
 template <class T>
 struct StoreEpilogue {
-  static constexpr bool kSymmetric = false, kPastL2 = true;
+  static constexpr bool kSymmetric = false, kPastL2 = true, kAnyRows = true;
   T* y;
   int64_t ldy;
 

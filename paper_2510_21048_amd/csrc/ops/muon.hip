@@ -27,7 +27,7 @@ constexpr int kThreads = 256;
 // 16 strong directions over weak ones the error goes from 4e-4 to 1.3e-3; each such step moves 4 of 8 bytes less.
 constexpr int kOneHalf = 2;
 constexpr int kNormParts = 256;  // workgroups whose sums make one matrix's norm
-constexpr int64_t kMostCount = 65535, kMostSide = int64_t(1) << 24;
+constexpr int64_t kMostCount = 65535, kMostSide = kMostDirectLd - 64;
 
 struct Shape {
   int64_t count, rows, cols, s, l;  // s <= l
@@ -148,7 +148,7 @@ __device__ inline int diagonal(int64_t m, int64_t n) {
 // P = X X^T without its diagonal, which goes to d.  Only tiles on or below the diagonal are computed; the tiles below it
 // are written to their mirrored places too.
 struct GramEpilogue {
-  static constexpr bool kSymmetric = true, kPastL2 = false;  // what it writes is read next
+  static constexpr bool kSymmetric = true, kPastL2 = false, kAnyRows = false;  // what it writes is read next
   f16* p;
   float* d;
   int64_t ld;
@@ -178,7 +178,7 @@ struct GramEpilogue {
 
 // Q = b P + c P P without its diagonal.
 struct PolyEpilogue {
-  static constexpr bool kSymmetric = true, kPastL2 = false;
+  static constexpr bool kSymmetric = true, kPastL2 = false, kAnyRows = false;
   const f16* p;
   const float* dp;
   f16* q;
@@ -227,7 +227,7 @@ struct PolyEpilogue {
 // X <- (a + q_ii) X_i + (Q X)_i.  The diagonal's index is the row where X lies as [s, l], the column else.
 template <bool TALL>
 struct StepEpilogue {
-  static constexpr bool kSymmetric = false, kPastL2 = true;
+  static constexpr bool kSymmetric = false, kPastL2 = true, kAnyRows = false;
   bool lines() const { return out ? whole_lines(out, cols) : whole_lines(nx, ld) && whole_lines(nlo, ld); }
   template <class F>
   __device__ __attribute__((always_inline)) void chosen(F f) const { f(*this); }
