@@ -91,6 +91,9 @@ __device__ inline f32x4 mfma(Vec<f16>::x8 a, Vec<f16>::x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
+// Row lengths for which a tile's bytes fit 31 bits.
+constexpr int64_t kMostDirectLd = int64_t(1) << 21;
+
 // A buffer load past num_records gives zeros, whose LDS place is written all the same.
 constexpr unsigned kNowhere = 0x80000000u;
 
@@ -145,26 +148,45 @@ __device__ inline u32x4 drop(u32x4 v, int s) {
 
 // One operand's loads through registers, for rows of any alignment.  A chunk that passes the end of its row is read
 // from further back, so that it ends there, and shifted when it is stored: every load is 16 bytes and inside the
-// matrix, none waits for another or is behind a branch of its own.  Rows shorter than 8 elements are read one by one.
+// matrix, none waits for another or is behind a branch of its own.  But for the last k tile a chunk's place in the
+// tile does not change, so a load costs no address arithmetic (which took longer than the loads).
 template <class T, class Ti, int R, bool KC, int THREADS>
 struct Staged {
   static constexpr int kLoads = Ti::kChunks / THREADS;
   u32x4 v[kLoads];
+  unsigned off[kLoads];
   int past[kLoads];  // elements of a chunk that its row does not have
-  bool whole;
+  bool plain;        // rows of 8 elements and more, near enough for 32-bit offsets
+  bool cut;          // some chunk passes its row's end
 
-  __device__ void load(int tid, const T* p, int64_t ld, int64_t r0, int64_t rows, int t, int ks) {
-    const int64_t k0 = int64_t(t) * kBK, length = KC ? ks : rows;  // of the contiguous side
-    whole = r0 + R <= rows && k0 + kBK <= ks;
-    if (whole) {
+  __device__ void init(int tid, int64_t ld, int64_t r0, int64_t rows, int ks) {
+    plain = (KC ? ks : rows) >= 8 && ld < kMostDirectLd;
+    cut = !KC && r0 + R > rows;
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        int row, k;
-        Ti::at(j * THREADS + tid, row, k);
-        __builtin_memcpy(&v[j], KC ? p + (r0 + row) * ld + k0 + k : p + (k0 + k) * ld + r0 + row, 16);
+    for (int j = 0; j < kLoads; ++j) {
+      int row, k;
+      Ti::at(j * THREADS + tid, row, k);
+      if (KC) {  // a row past the last one is read as the last: what comes of it is not written
+        const int left = int(rows - r0 < R ? rows - r0 : R) - 1;
+        past[j] = 0;
+        off[j] = unsigned(row < left ? row : left) * unsigned(ld * 2) + k * 2;
+      } else {
+        const int64_t valid = rows - (r0 + row);
+        past[j] = valid >= 8 ? 0 : valid <= 0 ? 8 : int(8 - valid);
+        off[j] = unsigned(k) * unsigned(ld * 2) + (past[j] == 8 ? 0 : row - past[j]) * 2;
       }
+    }
+  }
+  __device__ void load(int tid, const T* p, int64_t ld, int64_t r0, int64_t rows, int t, int ks) {
+    const int64_t k0 = int64_t(t) * kBK;
+    if (plain && k0 + kBK <= ks) {
+      const char* base = reinterpret_cast<const char*>(KC ? p + r0 * ld + k0 : p + k0 * ld + r0);
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) __builtin_memcpy(&v[j], base + int(off[j]), 16);
       return;
     }
+    cut = true;
+    const int64_t length = KC ? ks : rows;  // of the contiguous side
     const T* from[kLoads];
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
@@ -189,7 +211,7 @@ struct Staged {
     }
   }
   __device__ void store(int tid, char* lds) const {
-    if (whole) {
+    if (!cut) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(lds + (j * THREADS + tid) * 16) = v[j];
     } else {
@@ -436,6 +458,8 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
   } else {
     Staged<T, TA, C::BM, AKC, C::GROUP> la;
     Staged<T, TB, C::BN, BKC, C::GROUP> lb;
+    la.init(tid, g.lda, m0, g.m, ks);
+    lb.init(tid, g.ldb, n0, g.n, ks);
     const auto load = [&](int t) {
       la.load(tid, a, g.lda, m0, g.m, tile_at(t), ks);
       lb.load(tid, b, g.ldb, n0, g.n, tile_at(t), ks);
@@ -607,7 +631,6 @@ inline void pack(const Pack& a, const Pack& b, hipStream_t st) {
   if (blocks > 0) k_pack<T><<<dim3(unsigned(blocks < 8192 ? blocks : 8192), both ? 2 : 1), 256, 0, st>>>(first, b);
 }
 
-constexpr int64_t kMostDirectLd = int64_t(1) << 21;
 inline bool direct_ok(const void* p, int64_t ld, int64_t stride, int64_t contiguous, bool padded) {
   return aligned(p, 16) && ld % 8 == 0 && stride % 8 == 0 && ld < kMostDirectLd && (contiguous % 8 == 0 || padded);
 }
