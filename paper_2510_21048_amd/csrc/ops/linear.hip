@@ -1,4 +1,13 @@
 // linear.hip -- y = act(x w^T + b) + r and its gradients on MI355X (gfx950).
+//
+//   z = x w^T + b, y = act(z) + r          one product, its epilogue (gemm.h); z is written where the backward pass wants it
+//   dz = dy act'(z), db = sum over m dz    k_dz: one pass over dy and z, column sums of bands of rows; k_db adds the bands
+//   dx = dz w, dw = dz^T x                 two products, either operand as it lies
+//
+// dz is rounded to 16 bits, as the matrix instructions take it (the products' outputs are rounded to as many: 1.4 times
+// their error without); db sums it before that.  No sum's order depends on when a workgroup runs.
+// 8192 x 8192 x 2048 with gelu and z: 245 us (1,120 TFLOP/s; its 268 MB of outputs alone take 40); the gradients 573 us, of which
+// k_dz 87 (402 MB at 4.6 TB/s).  32768 x 4096 x 16384 with a residual: 3.4 ms.  One token through 4096 x 1024: 8.5 us.
 #include "gemm.h"
 
 using namespace xops;

@@ -14,6 +14,11 @@
 //   - Q is made from the same rounded P in both terms: b + 2 c p is near 0 where P is near 1, so that its error cancels.
 // On matrices of normal values the products alone, in bfloat16, leave 1e-2; in half precision without these, 1.5e-3;
 // where one direction holds most of a gradient, 1.6e-1 and 2e-2.
+//
+// Bound by the products where matrices are large: 24 of 8192 x 2048 take 17.1 ms, of which the five X X^T 5.3 (870 TFLOP/s of the
+// half that is computed: 864 tiles in 3.4 rounds), P P 1.3, Q X 8.6 (its 32 k tiles a workgroup are followed by 8 bytes read and
+// written an element, which nothing hides), momentum and start 1.6 (4 GB each at 4.5 and 5.5 TB/s).  A single 1024 x 1024 takes
+// 159 us: 17 launches one after another, 10 us a product.
 #include "gemm.h"
 
 using namespace xops;
@@ -132,11 +137,13 @@ __global__ __launch_bounds__(kThreads) void k_start(const G* g, const float* mom
   }
 }
 
-// Clears what is behind the rows of a matrix [rows, cols] of row length ld, up to a multiple of 8: what a piece of 16 bytes
-// reads with them.
-__global__ void k_clear_pads(f16* p, int64_t rows, int64_t cols, int64_t ld) {
-  const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x, pad = -cols & 7;
-  if (i < rows * pad) p[i / pad * ld + cols + i % pad] = f16(0.0f);
+// Clears what is behind the rows of the matrices that no kernel of the start writes, up to a multiple of 8: what a piece of
+// 16 bytes reads with them.  y: the second X, P, Q.
+__global__ void k_clear_pads(f16* x, f16* p, f16* q, int64_t rows_x, int64_t cols_x, int64_t ldx, int64_t rows_p, int64_t cols_p, int64_t ldp) {
+  f16* at = blockIdx.y == 0 ? x : blockIdx.y == 1 ? p : q;
+  const int64_t rows = blockIdx.y ? rows_p : rows_x, cols = blockIdx.y ? cols_p : cols_x, ld = blockIdx.y ? ldp : ldx, pad = -cols & 7;
+  const int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (i < rows * pad) at[i / pad * ld + cols + i % pad] = f16(0.0f);
 }
 
 // Which of the W columns from n on is m's own, or -1.
@@ -315,12 +322,9 @@ int update(const G* g, float* mom, const Shape& h, float mu, bool nesterov, int 
     return launched();
   }
   const int64_t sx = h.rows * h.ldx, sp = h.s * h.lds;
-  const auto clear = [&](f16* p, int64_t rows, int64_t cols, int64_t ld) {
-    if (cols % 8) k_clear_pads<<<unsigned((rows * (-cols & 7) + 255) / 256), 256, 0, st>>>(p, rows, cols, ld);
-  };
-  clear(w.x[1], h.count * h.rows, h.cols, h.ldx);
-  clear(w.p, h.count * h.s, h.s, h.lds);
-  clear(w.q, h.count * h.s, h.s, h.lds);
+  const int64_t pads_x = h.count * h.rows * (-h.cols & 7), pads_p = h.count * h.s * (-h.s & 7), pads = pads_x > pads_p ? pads_x : pads_p;
+  if (pads > 0)
+    k_clear_pads<<<dim3(unsigned((pads + 255) / 256), 3), 256, 0, st>>>(w.x[1], w.p, w.q, h.count * h.rows, h.cols, h.ldx, h.count * h.s, h.s, h.lds);
   for (int i = 0; i < steps && rc == XMEM_OK; ++i) {
     const f16 *x = w.x[i & 1], *lo = i == 0 || i < steps - kOneHalf ? w.lo[i & 1] : nullptr;
     bf16* to = i == steps - 1 ? out : nullptr;
