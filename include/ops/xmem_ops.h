@@ -143,7 +143,8 @@ size_t xmem_muon_update_workspace_bytes(int64_t count, int64_t rows, int64_t col
  *   d_momentum: float32 [count, rows, cols], read and written
  *   d_update  : bfloat16 [count, rows, cols], written
  *   d_workspace: >= xmem_muon_update_workspace_bytes(count, rows, cols), 256-byte aligned
- * Returns XMEM_OK, XMEM_EINVAL (null pointer, negative or too large size, steps
+ * Returns XMEM_OK, XMEM_EINVAL (null pointer, negative or too large size (rows or
+ * cols of 2^21 - 64 or more, count past 65,535, rows cols of 2^40 or more, 2^28 tiles of 64 x 64 or more in all), steps
  * outside 0..XMEM_NS_MAX_STEPS, unknown type), XMEM_EWORKSPACE or XMEM_EHIP. */
 int xmem_muon_update(const void* d_grad, int grad_dtype, float* d_momentum, int64_t count, int64_t rows, int64_t cols,
                      float mu, int nesterov, int steps, float scale, void* d_update, void* d_workspace,

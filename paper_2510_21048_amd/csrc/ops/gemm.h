@@ -8,7 +8,7 @@
 // its LDS reads take 1,536 of them without a bank conflict.  On values of 0 (no power limit) 8192 x 8192 x 8192 runs at 1,480
 // TFLOP/s, and at 1,770 where every k tile's loads come from the same place: the loads that miss the L2 (19%) hold it back.
 // On random values the clock falls: 1,270 to 1,440 TFLOP/s for x w^T, 1,050 to 1,200 for dz w, 1,120 to 1,290 for dz^T x, where the
-// library's products take 1,400 to 1,600, 1,210 to 1,300 and 1,070 to 1,240.  Small ones are bound by their latency: a launch
+// library's products reach 1,370 to 1,580, 1,210 to 1,370 and 1,070 to 1,210.  Small ones are bound by their latency: a launch
 // (2.1 us), the first loads, one reduction and the writes take 6.5 us for one k tile, each further group of four 0.8.
 #pragma once
 #include "common.h"

@@ -6,8 +6,8 @@
 //
 // dz is rounded to 16 bits, as the matrix instructions take it (the products' outputs are rounded to as many: 1.4 times
 // their error without); db sums it before that.  No sum's order depends on when a workgroup runs.
-// 8192 x 8192 x 2048 with gelu and z: 245 us (1,120 TFLOP/s; its 268 MB of outputs alone take 40); the gradients 573 us, of which
-// k_dz 87 (402 MB at 4.6 TB/s).  32768 x 4096 x 16384 with a residual: 3.4 ms.  One token through 4096 x 1024: 8.5 us.
+// 8192 x 8192 x 2048 with gelu and z: 242 to 272 us (1,010 to 1,140 TFLOP/s; its 268 MB of outputs alone take 40); the gradients 572 us, of which
+// k_dz 88 (402 MB at 4.6 TB/s).  32768 x 4096 x 16384 with a residual: 3.4 ms.  One token through 4096 x 1024: 8.6 us.
 #include "gemm.h"
 
 using namespace xops;
@@ -128,8 +128,8 @@ inline int64_t band_rows(int64_t m, int64_t n) { return (m + 63) / 64 * ((n + kB
 inline int64_t bands(int64_t m, int64_t n) { return (m + band_rows(m, n) - 1) / band_rows(m, n); }
 
 // Whether a matrix of `cols` columns is copied to rows of 16 bytes' alignment before a product of m n k multiplications: the
-// copy costs a launch and a pass over it.  1003 x 2047 x 1021 (2.1e9): 21 us with the copies and without; 4099 x 4097 x 4095: 210
-// against 365; 501 x 1023 x 511: 15 against 11.
+// copy costs a launch and a pass over it.  float16, with the copies and without: 501 x 1023 x 511 13.6 and 9.0 us,
+// 1003 x 2047 x 1021 (2.1e9) 21.1 and 17.2, 1601 x 1603 x 1605 (4.1e9) 30.1 and 30.8, 4099 x 4097 x 4095 221 and 303.
 constexpr double kPackFrom = 4.0e9;
 inline bool packs(int64_t cols, int64_t ld, int64_t m, int64_t n, int64_t k) {
   return (cols % 8 || ld % 8) && double(m) * double(n) * double(k) >= kPackFrom;
