@@ -57,9 +57,9 @@ struct Tile {
   static constexpr int kBytes = R * kBK * 2;
   static constexpr int kChunks = R * kBK / 8;
 
-  __device__ static int pair_hash(int k) { return ((k & 3) | ((k >> 1) & 4)) & (R / 16 - 1); }
+  __host__ __device__ static int pair_hash(int k) { return ((k & 3) | ((k >> 1) & 4)) & (R / 16 - 1); }
   // the row (or first of eight rows) and the k (or first of eight) of the chunk kept at place i
-  __device__ static void at(int i, int& row, int& k) {
+  __host__ __device__ static void at(int i, int& row, int& k) {
     if constexpr (KC) {
       row = i >> 3;
       k = ((i & 7) ^ ((row >> 1) & 7)) * 8;
@@ -140,7 +140,7 @@ struct Direct {
 };
 
 // v >> 16 s bits as one number of 128 bits, s = 0..8: the elements past the end of a row, dropped.
-__device__ inline u32x4 drop(u32x4 v, int s) {
+__host__ __device__ inline u32x4 drop(u32x4 v, int s) {
   if (s & 1) {
     v[0] = (v[0] >> 16) | (v[1] << 16);
     v[1] = (v[1] >> 16) | (v[2] << 16);
@@ -166,7 +166,7 @@ struct Staged {
   bool plain;        // rows of 8 elements and more, near enough for 32-bit offsets
   bool cut;          // some chunk passes its row's end
 
-  __device__ void init(int tid, int64_t ld, int64_t r0, int64_t rows, int ks) {
+  __host__ __device__ void init(int tid, int64_t ld, int64_t r0, int64_t rows, int ks) {
     plain = (KC ? ks : rows) >= 8 && ld < kMostDirectLd;
     cut = !KC && r0 + R > rows;
 #pragma unroll
@@ -180,11 +180,12 @@ struct Staged {
       } else {
         const int64_t valid = rows - (r0 + row);
         past[j] = valid >= 8 ? 0 : valid <= 0 ? 8 : int(8 - valid);
-        off[j] = unsigned(k) * unsigned(ld * 2) + (past[j] == 8 ? 0 : row - past[j]) * 2;
+        // a chunk wholly past the row's end reads the tile's first eight rows or, where there are fewer, the last eight of all
+        off[j] = unsigned(k) * unsigned(ld * 2) + (past[j] < 8 ? row - past[j] : rows - r0 < 8 ? int(rows - r0) - 8 : 0) * 2;
       }
     }
   }
-  __device__ void load(int tid, const T* p, int64_t ld, int64_t r0, int64_t rows, int t, int ks) {
+  __host__ __device__ void load(int tid, const T* p, int64_t ld, int64_t r0, int64_t rows, int t, int ks) {
     const int64_t k0 = int64_t(t) * kBK;
     if (plain && k0 + kBK <= ks) {
       const char* base = reinterpret_cast<const char*>(KC ? p + r0 * ld + k0 : p + k0 * ld + r0);
@@ -217,7 +218,7 @@ struct Staged {
       }
     }
   }
-  __device__ void store(int tid, char* lds) const {
+  __host__ __device__ void store(int tid, char* lds) const {
     if (!cut) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(lds + (j * THREADS + tid) * 16) = v[j];
