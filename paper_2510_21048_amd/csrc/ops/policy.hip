@@ -94,7 +94,7 @@ __device__ inline float over_row(float v, float* meet) {
 template <class T, int THREADS, int NCH>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS == 1024 ? 4 : THREADS == 64 ? 5 : 6) void k_policy(Policy p) {
   constexpr int E = kPer<T>;
-  __shared__ float meet[2][THREADS / kWave], at_y[THREADS < 256 ? 4 : 1];
+  __shared__ float meet[2][THREADS / kWave], at_y;  // neither where a row is a wavefront
   const int tid = threadIdx.x % THREADS, slot = threadIdx.x / THREADS;
   const int64_t t = THREADS < 256 ? int64_t(blockIdx.x) * (256 / THREADS) + slot : blockIdx.x;
   if (t >= p.tokens) return;  // a whole wavefront, of those that do not meet others
@@ -118,14 +118,14 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS == 1024 ? 4 
   }
   const bool in = y >= 0 && y < vocab;
   const int64_t cy = in ? y / E : -1;
-  if (!in && tid == 0) at_y[THREADS < 256 ? slot : 0] = NAN;
-  float m = -INFINITY, s = 0.0f, v[E];
+  if (THREADS > kWave && !in && tid == 0) at_y = NAN;
+  float m = -INFINITY, s = 0.0f, xy = NAN, v[E];
   // the sampled token's logit, from the thread that has it: the row may be overwritten
   const auto note = [&](int64_t i) {
     if (i == cy)
 #pragma unroll
       for (int k = 0; k < E; ++k)
-        if (i * E + k == y) at_y[THREADS < 256 ? slot : 0] = v[k];
+        if (i * E + k == y) (THREADS > kWave ? at_y : xy) = v[k];
   };
   u32x4 c[NCH > 0 ? NCH : 1];
   if constexpr (NCH > 0) {
@@ -176,8 +176,9 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS == 1024 ? 4 
     m = top;
     s = over_row<Sum, THREADS>(s, meet[1]);
   }
-  if constexpr (THREADS == kWave) __builtin_amdgcn_wave_barrier();
-  const float lp = (at_y[THREADS < 256 ? slot : 0] - m) - logf(s);
+  // a row's own wavefront passes it between lanes (chunk i is lane i % 64's); a workgroup's has met the others' since
+  xy = THREADS > kWave ? at_y : __shfl(xy, int(cy & (kWave - 1)));
+  const float lp = (xy - m) - logf(s);
   float grad = 0.0f;
   if (loss) {
     const float rho = expf(lp - old_lp);
