@@ -4,7 +4,9 @@ training step that allocate nothing by themselves (include/ops/xmem_ops.h).
 The functions named ``xmem_*`` mirror the C ABI one to one and take raw device
 pointers (ints) or torch CUDA tensors; ``linear_forward``, ``linear_backward``,
 ``policy_loss``, ``token_logp`` and ``muon_update`` check their tensors, allocate
-outputs and workspace with torch and run on the current torch stream.
+outputs and workspace with torch and run on the current torch stream, or on the
+raw ``stream`` given (then nothing waits for the current one by itself: the inputs
+have to be ready on it).
 """
 from __future__ import annotations
 
@@ -156,13 +158,61 @@ def _workspace(workspace, need: int, device):
     return workspace, workspace.numel()
 
 
-def _raw_stream(device, stream) -> int:
-    if stream is not None:
-        return stream
+def _raw_stream(device) -> int:
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # what current_stream() wraps, at a tenth of its time
     index = device.index
     return raw(index) if raw is not None and index is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+class _Here:
+    """A call on the current stream: torch's allocator orders what it takes by that stream already."""
+
+    def __init__(self, raw):
+        self.raw = raw
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *_):
+        return False
+
+    @staticmethod
+    def out(*tensors):
+        return tensors if len(tensors) > 1 else tensors[0]
+
+
+class _There:
+    """A call on another stream: its outputs and workspace are taken from that stream's memory, which the allocator gives to
+    nothing else before what the stream has been asked for, and what both streams see is kept until both are done with it."""
+
+    def __init__(self, device, raw, given):
+        import torch
+        self.raw, self.stream = raw, torch.cuda.ExternalStream(raw, device=device)
+        self.before = torch.cuda.current_stream(device)
+        for t in given:
+            if t is not None:
+                t.record_stream(self.stream)
+        self.context = torch.cuda.stream(self.stream)
+
+    def __enter__(self):
+        self.context.__enter__()
+        return self
+
+    def __exit__(self, *raised):
+        return self.context.__exit__(*raised)
+
+    def out(self, *tensors):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.before)
+        return tensors if len(tensors) > 1 else tensors[0]
+
+
+def _on(device, stream, *given):
+    """Where a call on checked tensors (the workspace among them) runs."""
+    here = _raw_stream(device)
+    return _Here(here) if stream is None or stream == here else _There(device, stream, given)
 
 
 def _activation(name: str) -> int:
@@ -182,12 +232,13 @@ def linear_forward(x, w, bias=None, residual=None, activation: str = "none", sav
     (m, k), n = x.shape, w.shape[0]
     ldr = 0 if residual is None else _matrix(residual, "residual", m, n, x.dtype, dev)
     _vector(bias, "bias", n, torch.float32, dev)
-    y = torch.empty((m, n), dtype=x.dtype, device=dev)
-    z = torch.empty((m, n), dtype=x.dtype, device=dev) if save_z else None
-    workspace, size = _workspace(workspace, lib.xmem_linear_forward_workspace_bytes(m, n, k, ldx, ldw), dev)
-    _check(xmem_linear_forward(x, ldx, w, ldw, bias, residual, ldr, m, n, k, code, act, y, n, z, n, workspace, size,
-                               _raw_stream(dev, stream)), "xmem_linear_forward")
-    return y, z
+    with _on(dev, stream, x, w, bias, residual, workspace) as on:
+        y = torch.empty((m, n), dtype=x.dtype, device=dev)
+        z = torch.empty((m, n), dtype=x.dtype, device=dev) if save_z else None
+        workspace, size = _workspace(workspace, lib.xmem_linear_forward_workspace_bytes(m, n, k, ldx, ldw), dev)
+        _check(xmem_linear_forward(x, ldx, w, ldw, bias, residual, ldr, m, n, k, code, act, y, n, z, n, workspace, size, on.raw),
+               "xmem_linear_forward")
+        return on.out(y, z)
 
 
 def linear_backward(dy, x, w, z=None, activation: str = "none", need_dx: bool = True, need_dw: bool = True, need_db: bool = True,
@@ -205,13 +256,14 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", need_dx: bool = 
     if z is None and act != ACTIVATIONS["none"]:
         raise XmemError("z: wanted with an activation (linear_forward's save_z)")
     ldz = 0 if z is None else _matrix(z, "z", m, n, dy.dtype, dev)
-    dx = torch.empty((m, k), dtype=dy.dtype, device=dev) if need_dx else None
-    dw = torch.empty((n, k), dtype=dy.dtype, device=dev) if need_dw else None
-    db = torch.empty(n, dtype=torch.float32, device=dev) if need_db else None
-    workspace, size = _workspace(workspace, xmem_linear_backward_workspace_bytes(m, n, k, lddy, ldx, ldw, act), dev)
-    _check(xmem_linear_backward(dy, lddy, z, ldz, x, ldx, w, ldw, m, n, k, code, act, dx, k, dw, k, db, workspace, size,
-                                _raw_stream(dev, stream)), "xmem_linear_backward")
-    return dx, dw, db
+    with _on(dev, stream, dy, x, w, z, workspace) as on:
+        dx = torch.empty((m, k), dtype=dy.dtype, device=dev) if need_dx else None
+        dw = torch.empty((n, k), dtype=dy.dtype, device=dev) if need_dw else None
+        db = torch.empty(n, dtype=torch.float32, device=dev) if need_db else None
+        workspace, size = _workspace(workspace, xmem_linear_backward_workspace_bytes(m, n, k, lddy, ldx, ldw, act), dev)
+        _check(xmem_linear_backward(dy, lddy, z, ldz, x, ldx, w, ldw, m, n, k, code, act, dx, k, dw, k, db, workspace, size, on.raw),
+               "xmem_linear_backward")
+        return on.out(dx, dw, db)
 
 
 _ANY = (XMEM_BF16, XMEM_F16, XMEM_F32)
@@ -226,10 +278,11 @@ def token_logp(logits, tokens, weights=None, stream=None):
     t, v = logits.shape
     _vector(tokens, "tokens", t, torch.int64, dev)
     _vector(weights, "weights", t, torch.float32, dev)
-    logp = torch.empty(t, dtype=torch.float32, device=dev)
-    _check(xmem_policy_loss(logits, ldl, tokens, weights, None, None, None, t, v, code, 0.0, 0.0, 0.0, 1.0, None, logp, None, 0,
-                            None, 0, _raw_stream(dev, stream)), "xmem_policy_loss")
-    return logp
+    with _on(dev, stream, logits, tokens, weights) as on:
+        logp = torch.empty(t, dtype=torch.float32, device=dev)
+        _check(xmem_policy_loss(logits, ldl, tokens, weights, None, None, None, t, v, code, 0.0, 0.0, 0.0, 1.0, None, logp, None, 0,
+                                None, 0, on.raw), "xmem_policy_loss")
+        return on.out(logp)
 
 
 def policy_loss(logits, tokens, weights, old_logp, advantages, ref_logp=None, clip_low: float = 0.2, clip_high: float = 0.2,
@@ -248,16 +301,16 @@ def policy_loss(logits, tokens, weights, old_logp, advantages, ref_logp=None, cl
         raise XmemError("old_logp and advantages are wanted (token_logp needs neither)")
     for a, name in ((weights, "weights"), (old_logp, "old_logp"), (advantages, "advantages"), (ref_logp, "ref_logp")):
         _vector(a, name, t, torch.float32, dev)
-    stats = torch.empty(4, dtype=torch.float32, device=dev)
-    logp = torch.empty(t, dtype=torch.float32, device=dev)
-    dlogits, ldd = None, 0
-    if need_dlogits:
-        dlogits, ldd = (logits, ldl) if in_place else (torch.empty((t, v), dtype=logits.dtype, device=dev), v)
-    workspace, size = _workspace(workspace, xmem_policy_loss_workspace_bytes(t, v), dev)
-    _check(xmem_policy_loss(logits, ldl, tokens, weights, old_logp, advantages, ref_logp, t, v, code, clip_low, clip_high,
-                            kl_coef, grad_scale, stats, logp, dlogits, ldd, workspace, size, _raw_stream(dev, stream)),
-           "xmem_policy_loss")
-    return stats, logp, dlogits
+    with _on(dev, stream, logits, tokens, weights, old_logp, advantages, ref_logp, workspace) as on:
+        stats = torch.empty(4, dtype=torch.float32, device=dev)
+        logp = torch.empty(t, dtype=torch.float32, device=dev)
+        dlogits, ldd = None, 0
+        if need_dlogits:
+            dlogits, ldd = (logits, ldl) if in_place else (torch.empty((t, v), dtype=logits.dtype, device=dev), v)
+        workspace, size = _workspace(workspace, xmem_policy_loss_workspace_bytes(t, v), dev)
+        _check(xmem_policy_loss(logits, ldl, tokens, weights, old_logp, advantages, ref_logp, t, v, code, clip_low, clip_high,
+                                kl_coef, grad_scale, stats, logp, dlogits, ldd, workspace, size, on.raw), "xmem_policy_loss")
+        return on.out(stats, logp, dlogits)
 
 
 def muon_update(grad, momentum, mu: float = 0.95, nesterov: bool = True, steps: int = 5, scale: float = 1.0, workspace=None,
@@ -272,8 +325,9 @@ def muon_update(grad, momentum, mu: float = 0.95, nesterov: bool = True, steps: 
     if momentum.shape != grad.shape or momentum.dtype != torch.float32 or momentum.device != dev or not momentum.is_contiguous():
         raise XmemError("momentum: a contiguous float32 tensor shaped as grad is wanted")
     count, (rows, cols) = (1 if grad.dim() == 2 else grad.shape[0]), grad.shape[-2:]
-    update = torch.empty(grad.shape, dtype=torch.bfloat16, device=dev)
-    workspace, size = _workspace(workspace, xmem_muon_update_workspace_bytes(count, rows, cols), dev)
-    _check(xmem_muon_update(grad, code, momentum, count, rows, cols, mu, nesterov, steps, scale, update, workspace, size,
-                            _raw_stream(dev, stream)), "xmem_muon_update")
-    return update
+    with _on(dev, stream, grad, momentum, workspace) as on:
+        update = torch.empty(grad.shape, dtype=torch.bfloat16, device=dev)
+        workspace, size = _workspace(workspace, xmem_muon_update_workspace_bytes(count, rows, cols), dev)
+        _check(xmem_muon_update(grad, code, momentum, count, rows, cols, mu, nesterov, steps, scale, update, workspace, size, on.raw),
+               "xmem_muon_update")
+        return on.out(update)

@@ -27,3 +27,74 @@ def test_linear_backward_last_tile_of_few_rows(size, dtype):
     want, bound = ref.backward(dyc, xc, wc, dyc, "none")
     for name, a, v, b in zip(("dx", "dw", "db"), got, want, bound):
         within(a, v, b, f"{name} {size}")
+
+
+def calls():
+    """Each operator as a call of a stream, on inputs of the current one, with sizes that need a workspace."""
+    g = torch.Generator().manual_seed(77)
+    new = lambda *s: torch.randn(*s, generator=g).to(BF).cuda()
+    x, w, dy, z = new(512, 4096), new(256, 4096), new(512, 256), new(512, 256)
+    logits, tokens = new(300, 999), torch.randint(0, 999, (300,), generator=g).cuda()
+    f = [torch.randn(300, generator=g).cuda() for _ in range(4)]
+    grad, mom = new(2, 512, 300), torch.randn(2, 512, 300, generator=g).cuda()
+    return {
+        "xmem_linear_forward": lambda s: xm.linear_forward(x[:128], w, activation="gelu", save_z=True, stream=s),
+        "xmem_linear_backward": lambda s: xm.linear_backward(dy, x, w, z, "silu", stream=s),
+        "xmem_policy_loss": lambda s: xm.policy_loss(logits, tokens, f[0].abs(), f[1] - 7, f[2], f[3] - 7, kl_coef=0.1, stream=s),
+        "xmem_muon_update": lambda s: (xm.muon_update(grad, mom.clone() if s is None else mom, stream=s),),
+    }
+
+
+@pytest.mark.parametrize("name", ["xmem_linear_forward", "xmem_linear_backward", "xmem_policy_loss", "xmem_muon_update"])
+def test_workspace_of_a_given_stream_stays_its_own(name, monkeypatch):
+    """What a call on another stream took is not handed to the current one while the call may still run."""
+    from paper_2510_21048_amd import ops
+    seen = []
+    real = getattr(ops, name)
+
+    def spy(*args):
+        seen.extend((t.data_ptr(), t.untyped_storage().nbytes()) for t in args if isinstance(t, torch.Tensor) and t.dtype == torch.uint8)
+        return real(*args)
+
+    monkeypatch.setattr(ops, name, spy)
+    call = calls()[name]
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    log(f"[ops] {name} on a stream of its own")
+    call(s.cuda_stream)
+    assert len(seen) == 1
+    at, size = seen[0]
+    for _ in range(3):
+        taken = torch.empty(size, dtype=torch.uint8, device="cuda")
+        assert taken.data_ptr() + size <= at or at + size <= taken.data_ptr()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("name", ["xmem_linear_forward", "xmem_linear_backward", "xmem_policy_loss", "xmem_muon_update"])
+def test_given_stream_beside_the_current_one(name):
+    """The same bits on a stream that runs late while the current one takes and writes blocks of the same sizes, before and after."""
+    call = calls()[name]
+    want = call(None)
+    torch.cuda.synchronize()
+    sizes = [t.nbytes for t in want if t is not None] + [1 << 16, 1 << 20, 1 << 22]
+    s = torch.cuda.Stream()
+
+    def flood():
+        for size in sizes:
+            for _ in range(3):
+                torch.empty(size, dtype=torch.uint8, device="cuda").fill_(255)
+
+    flood()
+    s.wait_stream(torch.cuda.current_stream())
+    torch.cuda._sleep(20_000_000)  # the blocks are written late ...
+    flood()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(10_000_000)
+    log(f"[ops] {name} beside writes")
+    got = call(s.cuda_stream)  # ... and the call runs late
+    flood()
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
