@@ -12,8 +12,8 @@
  *   xmem_muon_update               momentum and an update orthogonalised by
  *                                  Newton-Schulz products
  *
- * All calls run on the caller's stream, allocate nothing, keep nothing and do
- * not synchronise.  Pointers named d_* are device memory owned by the caller.
+ * All calls run on the caller's stream, which has to be one of the current device,
+ * allocate nothing, keep nothing and do not synchronise.  Pointers named d_* are device memory owned by the caller.
  * Matrices are row-major; ld* is the distance between rows in elements and at
  * least the row's length.  Rows need no more than their elements' alignment;
  * the fast loads want 16-byte aligned pointers and ld a multiple of 8 (and k a

@@ -183,17 +183,22 @@ class _Here:
 
 
 class _There:
-    """A call on another stream: its outputs and workspace are taken from that stream's memory, which the allocator gives to
-    nothing else before what the stream has been asked for, and what both streams see is kept until both are done with it."""
+    """A call on another stream or device than the current one.  Launches go to the current device, so the tensors' own is
+    made current.  Outputs and workspace are taken from the stream's memory, which the allocator gives to nothing else before
+    what the stream has been asked for, and what both streams see is kept until both are done with it."""
 
     def __init__(self, device, raw, given):
         import torch
-        self.raw, self.stream = raw, torch.cuda.ExternalStream(raw, device=device)
+        self.raw = raw
         self.before = torch.cuda.current_stream(device)
+        if raw == self.before.cuda_stream:
+            self.context = torch.cuda.device(device)
+            return
+        stream = torch.cuda.ExternalStream(raw, device=device)
         for t in given:
             if t is not None:
-                t.record_stream(self.stream)
-        self.context = torch.cuda.stream(self.stream)
+                t.record_stream(stream)
+        self.context = torch.cuda.stream(stream)
 
     def __enter__(self):
         self.context.__enter__()
@@ -211,8 +216,10 @@ class _There:
 
 def _on(device, stream, *given):
     """Where a call on checked tensors (the workspace among them) runs."""
+    import torch
     here = _raw_stream(device)
-    return _Here(here) if stream is None or stream == here else _There(device, stream, given)
+    raw = here if stream is None else stream
+    return _Here(here) if raw == here and torch.cuda.current_device() == device.index else _There(device, raw, given)
 
 
 def _activation(name: str) -> int:

@@ -131,3 +131,39 @@ def test_missing_library_fails_loudly(monkeypatch, tmp_path):
     monkeypatch.setattr(ops, "_LIB_PATH", tmp_path / "absent.so")
     with pytest.raises(xm.XmemError):
         ops.load_ops()
+
+
+def test_calls_run_on_the_device_of_their_tensors(monkeypatch):
+    """A tensor's device that is not the current one is made current for the call, on its own current stream; where it is
+    current already nothing is switched."""
+    entered, now = [], [0]
+
+    class Device:
+        def __init__(self, d):
+            self.to = torch.device(d).index
+
+        def __enter__(self):
+            entered.append(self.to)
+            self.back, now[0] = now[0], self.to
+
+        def __exit__(self, *_):
+            now[0] = self.back
+            return False
+
+    class Stream:
+        cuda_stream = 4096
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: Stream())
+    monkeypatch.setattr(ops, "_raw_stream", lambda d: 4096)
+    with ops._on(torch.device("cuda", 1), None) as on:
+        assert now[0] == 1 and on.raw == 4096
+    assert now[0] == 0 and entered == [1]
+    for stream in (None, 4096):
+        with ops._on(torch.device("cuda", 0), stream) as on:
+            assert now[0] == 0 and on.raw == 4096
+    assert entered == [1]
+    with ops._on(torch.device("cuda", 1), 4096):
+        assert now[0] == 1
+    assert now[0] == 0
