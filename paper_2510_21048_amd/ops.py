@@ -150,12 +150,15 @@ def _vector(t, what: str, n: int, dtype, device):
 
 
 def _workspace(workspace, need: int, device):
+    """The caller's workspace where it is large enough, else one of torch's."""
+    if workspace is not None and (workspace.device != device or not workspace.is_contiguous()):
+        raise XmemError(f"workspace: a contiguous tensor on {device} is wanted, got strides {workspace.stride()} on {workspace.device}")
     if need == 0:
         return None, 0
-    if workspace is None or workspace.numel() < need:
-        import torch
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    return workspace, workspace.numel()
+    if workspace is not None and workspace.nbytes >= need:
+        return workspace, workspace.nbytes
+    import torch
+    return torch.empty(need, dtype=torch.uint8, device=device), need
 
 
 def _raw_stream(device) -> int:
@@ -196,7 +199,7 @@ class _There:
             return
         stream = torch.cuda.ExternalStream(raw, device=device)
         for t in given:
-            if t is not None:
+            if t is not None and t.is_cuda:
                 t.record_stream(stream)
         self.context = torch.cuda.stream(stream)
 

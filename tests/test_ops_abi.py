@@ -167,3 +167,19 @@ def test_calls_run_on_the_device_of_their_tensors(monkeypatch):
     with ops._on(torch.device("cuda", 1), 4096):
         assert now[0] == 1
     assert now[0] == 0
+
+
+def test_workspace_is_checked():
+    """A caller's workspace has to be contiguous memory of the tensors' device; its bytes count, not its elements."""
+    cpu, meta = torch.device("cpu"), torch.device("meta")
+    space = torch.empty(1024, dtype=torch.uint8, device=meta)
+    for bad, dev in ((space, cpu), (space[::2], meta), (space.view(32, 32).T, meta)):
+        for need in (0, 16):
+            with pytest.raises(xm.XmemError):
+                ops._workspace(bad, need, dev)
+    assert ops._workspace(space, 1024, meta) == (space, 1024)
+    floats = torch.empty(256, device=meta)
+    assert ops._workspace(floats, 1024, meta) == (floats, 1024)
+    own, size = ops._workspace(space, 1025, meta)
+    assert own is not space and size == own.numel() == 1025
+    assert ops._workspace(None, 0, meta) == (None, 0)
