@@ -6,7 +6,10 @@ pointers (ints) or torch CUDA tensors; ``linear_forward``, ``linear_backward``,
 ``policy_loss``, ``token_logp`` and ``muon_update`` check their tensors, allocate
 outputs and workspace with torch and run on the current torch stream, or on the
 raw ``stream`` given (then nothing waits for the current one by itself: the inputs
-have to be ready on it).
+have to be ready on it).  They are no part of autograd's graph (the gradients are
+calls of their own): inputs that require one are refused while it is recorded, so
+call them on detached tensors, under ``torch.no_grad()`` or in a
+``torch.autograd.Function``.
 """
 from __future__ import annotations
 
@@ -220,6 +223,8 @@ class _There:
 def _on(device, stream, *given):
     """Where a call on checked tensors (the workspace among them) runs."""
     import torch
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given):
+        raise XmemError("an input requires a gradient, which is not recorded here: detach it or call under torch.no_grad()")
     here = _raw_stream(device)
     raw = here if stream is None else stream
     return _Here(here) if raw == here and torch.cuda.current_device() == device.index else _There(device, raw, given)

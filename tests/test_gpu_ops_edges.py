@@ -98,3 +98,23 @@ def test_given_stream_beside_the_current_one(name):
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
+
+
+def test_no_call_drops_a_gradient():
+    """Whichever input requires a gradient, each call says so instead of returning results without one."""
+    g = torch.Generator().manual_seed(4)
+    new = lambda *s: torch.randn(*s, generator=g).to(BF).cuda()
+    x, w, r, dy = new(8, 16), new(24, 16), new(8, 24), new(8, 24)
+    b, y = torch.randn(24, generator=g).cuda(), torch.randint(0, 24, (8,), generator=g).cuda()
+    f = [torch.randn(8, generator=g).cuda() for _ in range(4)]
+    for call, args in ((lambda *a: xm.linear_forward(*a), [x, w, b, r]), (lambda *a: xm.linear_backward(*a, "silu"), [dy, x, w, r]),
+                       (lambda lg, *a: xm.policy_loss(lg, y, *a), [dy, *f]), (lambda lg, a: xm.token_logp(lg, y, a), [dy, f[0]]),
+                       (lambda *a: xm.muon_update(*a), [dy, torch.zeros(8, 24, device="cuda")])):
+        call(*args)
+        for i in range(len(args)):
+            mine = [a.clone().requires_grad_() if i == j else a for j, a in enumerate(args)]
+            with pytest.raises(xm.XmemError, match="gradient"):
+                call(*mine)
+            with torch.no_grad():
+                call(*mine)
+    torch.cuda.synchronize()

@@ -183,3 +183,17 @@ def test_workspace_is_checked():
     own, size = ops._workspace(space, 1025, meta)
     assert own is not space and size == own.numel() == 1025
     assert ops._workspace(None, 0, meta) == (None, 0)
+
+
+def test_inputs_that_require_a_gradient_are_refused(monkeypatch):
+    """The calls record nothing for autograd: while it records, an input that requires a gradient is an error, not a result
+    without one; under no_grad it is taken."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(ops, "_raw_stream", lambda d: 4096)
+    plain, leaf = torch.zeros(3), torch.zeros(3, requires_grad=True)
+    for given in ((leaf,), (plain, None, leaf), (plain, leaf * 2)):
+        with pytest.raises(xm.XmemError, match="gradient"):
+            ops._on(torch.device("cuda", 0), None, *given)
+        with torch.no_grad():
+            assert ops._on(torch.device("cuda", 0), None, *given).raw == 4096
+        assert ops._on(torch.device("cuda", 0), None, *(None if t is None else t.detach() for t in given)).raw == 4096
