@@ -230,6 +230,12 @@ def _on(device, stream, *given):
     return _Here(here) if raw == here and torch.cuda.current_device() == device.index else _There(device, raw, given)
 
 
+def _written(tensor) -> None:
+    """An input was overwritten: a graph that saved it has to see that, as after torch's own in-place operations."""
+    import torch
+    torch.autograd.graph.increment_version(tensor)
+
+
 def _activation(name: str) -> int:
     if name not in ACTIVATIONS:
         raise XmemError(f"activation {name!r}: one of {', '.join(ACTIVATIONS)} is wanted")
@@ -325,6 +331,8 @@ def policy_loss(logits, tokens, weights, old_logp, advantages, ref_logp=None, cl
         workspace, size = _workspace(workspace, xmem_policy_loss_workspace_bytes(t, v), dev)
         _check(xmem_policy_loss(logits, ldl, tokens, weights, old_logp, advantages, ref_logp, t, v, code, clip_low, clip_high,
                                 kl_coef, grad_scale, stats, logp, dlogits, ldd, workspace, size, on.raw), "xmem_policy_loss")
+        if dlogits is logits:
+            _written(logits)
         return on.out(stats, logp, dlogits)
 
 
@@ -345,4 +353,5 @@ def muon_update(grad, momentum, mu: float = 0.95, nesterov: bool = True, steps: 
         workspace, size = _workspace(workspace, xmem_muon_update_workspace_bytes(count, rows, cols), dev)
         _check(xmem_muon_update(grad, code, momentum, count, rows, cols, mu, nesterov, steps, scale, update, workspace, size, on.raw),
                "xmem_muon_update")
+        _written(momentum)
         return on.out(update)

@@ -118,3 +118,25 @@ def test_no_call_drops_a_gradient():
             with torch.no_grad():
                 call(*mine)
     torch.cuda.synchronize()
+
+
+def test_overwritten_inputs_are_seen_by_autograd():
+    """A graph that saved the logits, or the momentum, before a call overwrote them raises instead of using the new values."""
+    g = torch.Generator().manual_seed(5)
+    y = torch.randint(0, 24, (8,), generator=g).cuda()
+    f = [torch.randn(8, generator=g).cuda() for _ in range(3)]
+    for write, kept in ((lambda t: xm.policy_loss(t, y, *f, in_place=True), False), (lambda t: xm.policy_loss(t, y, *f), True),
+                        (lambda t: xm.muon_update(torch.ones(8, 24, device="cuda"), t), False)):
+        leaf = torch.randn(8, 24, generator=g).cuda().requires_grad_()
+        logits = leaf * 2
+        out = logits.square().sum()  # saves logits
+        write(logits.detach())
+        if kept:
+            out.backward()
+            assert torch.equal(leaf.grad, 8 * leaf.detach())
+        else:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                out.backward()
+    with torch.inference_mode():
+        xm.muon_update(torch.ones(8, 24, device="cuda"), torch.zeros(8, 24, device="cuda"))
+    torch.cuda.synchronize()
