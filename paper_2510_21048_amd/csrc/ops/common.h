@@ -26,6 +26,8 @@ template <> struct Vec<f16> {
 constexpr int kWave = 64;
 constexpr int kCus = 256;
 constexpr int kXcds = 8;
+// Threads of one launch: a grid of 2^32 and more is refused, or run without its upper bits.
+constexpr int64_t kMostThreads = int64_t(1) << 31;
 
 inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 inline size_t up256(size_t b) { return (b + 255) & ~size_t(255); }

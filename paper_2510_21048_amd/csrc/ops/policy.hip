@@ -24,6 +24,7 @@ struct Policy {
   void* dx;
   int64_t ldd;
   float* part;  // [3][tokens]
+  int64_t first = 0;  // row of the launch
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS == 1024 ? 4 
   constexpr int E = kPer<T>;
   __shared__ float meet[2][THREADS / kWave], at_y;  // neither where a row is a wavefront
   const int tid = threadIdx.x % THREADS, slot = threadIdx.x / THREADS;
-  const int64_t t = THREADS < 256 ? int64_t(blockIdx.x) * (256 / THREADS) + slot : blockIdx.x;
+  const int64_t t = p.first + (THREADS < 256 ? int64_t(blockIdx.x) * (256 / THREADS) + slot : int64_t(blockIdx.x));
   if (t >= p.tokens) return;  // a whole wavefront, of those that do not meet others
   const int64_t vocab = p.vocab, chunks = (vocab + E - 1) / E;
   // the token's scalars, asked for together
@@ -245,20 +246,25 @@ __global__ __launch_bounds__(1024) void k_policy_sums(const float* part, int64_t
   }
 }
 
+template <class T, int THREADS, int NCH>
+int launch_rows(Policy p, hipStream_t st) {
+  constexpr int per = THREADS < 256 ? 256 / THREADS : 1, block = per * THREADS;
+  constexpr int64_t most = kMostThreads / block * per;
+  for (; p.first < p.tokens; p.first += most) {
+    const int64_t rows = p.tokens - p.first < most ? p.tokens - p.first : most;
+    k_policy<T, THREADS, NCH><<<unsigned((rows + per - 1) / per), block, 0, st>>>(p);
+  }
+  return launched();
+}
+
 template <class T>
-void launch_policy(const Policy& p, hipStream_t st) {
+int launch_policy(const Policy& p, hipStream_t st) {
   const int64_t chunks = (p.vocab + kPer<T> - 1) / kPer<T>;
-  const unsigned rows = unsigned(p.tokens);
-  if (chunks <= 64 * 4)
-    k_policy<T, 64, 4><<<(rows + 3) / 4, 256, 0, st>>>(p);
-  else if (chunks <= 256 * 8)
-    k_policy<T, 256, 8><<<rows, 256, 0, st>>>(p);
-  else if (chunks <= 512 * 13)
-    k_policy<T, 512, 13><<<rows, 512, 0, st>>>(p);
-  else if (chunks <= 1024 * 16 && p.dx)
-    k_policy<T, 1024, 16><<<rows, 1024, 0, st>>>(p);
-  else
-    k_policy<T, 1024, 0><<<rows, 1024, 0, st>>>(p);
+  if (chunks <= 64 * 4) return launch_rows<T, 64, 4>(p, st);
+  if (chunks <= 256 * 8) return launch_rows<T, 256, 8>(p, st);
+  if (chunks <= 512 * 13) return launch_rows<T, 512, 13>(p, st);
+  if (chunks <= 1024 * 16 && p.dx) return launch_rows<T, 1024, 16>(p, st);
+  return launch_rows<T, 1024, 0>(p, st);
 }
 
 constexpr int64_t kMost = int64_t(1) << 31;
@@ -290,7 +296,10 @@ int xmem_policy_loss(const void* d_logits, int64_t ldl, const int64_t* d_tokens,
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   Policy p{d_logits, ldl, d_tokens, d_weights, d_old_logp, d_advantages, d_ref_logp, tokens, vocab, clip_low, clip_high, kl_coef,
            grad_scale, d_logp, d_dlogits, ldd, loss ? static_cast<float*>(d_workspace) : nullptr};
-  if (tokens > 0) (dtype == XMEM_BF16 ? launch_policy<bf16> : dtype == XMEM_F16 ? launch_policy<f16> : launch_policy<float>)(p, st);
+  if (tokens > 0) {
+    const int rc = (dtype == XMEM_BF16 ? launch_policy<bf16> : dtype == XMEM_F16 ? launch_policy<f16> : launch_policy<float>)(p, st);
+    if (rc != XMEM_OK) return rc;
+  }
   if (loss) k_policy_sums<<<1, 1024, 0, st>>>(p.part, tokens, d_ref_logp ? kl_coef : 0.0f, d_stats);
   return launched();
 }

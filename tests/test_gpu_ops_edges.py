@@ -140,3 +140,24 @@ def test_overwritten_inputs_are_seen_by_autograd():
     with torch.inference_mode():
         xm.muon_update(torch.ones(8, 24, device="cuda"), torch.zeros(8, 24, device="cuda"))
     torch.cuda.synchronize()
+
+
+def test_policy_of_more_rows_than_a_launch():
+    """2^26 rows and a few: four a workgroup of 256 threads, which is a grid of 2^32 threads, past what one launch may have."""
+    t = 2 ** 26 + 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(t, 2, generator=g, device="cuda", dtype=HF)
+    y = torch.randint(0, 2, (t,), generator=g, device="cuda")
+    log("[ops] policy_loss of 2^26 + 5 rows")
+    want = torch.nn.functional.logsigmoid((x[:, 0].float() - x[:, 1].float()) * (1 - 2 * y))
+    adv = torch.randn(t, generator=g, device="cuda")
+    stats, lp, dx = xm.policy_loss(x, y, None, want, adv)
+    torch.cuda.synchronize()
+    # each value: a few roundings of 32 bits of numbers below 16
+    assert float((lp - want).abs().max()) < 16 * 8 * ref.E
+    # the ratio is 1 to 1e-5: the loss is minus the mean advantage, and dx = -adv / t (1[j = y] - p_j)
+    assert abs(float(stats[0]) + float(adv.double().mean())) < 1e-5 and float(stats[3]) == 0.0
+    hit = torch.stack([y == 0, y == 1], 1).float()
+    slope = -adv[:, None] / t * (hit - torch.softmax(x.float(), 1))
+    # half a unit of float16's subnormals (all of dx are), and 1e-4 of the value
+    assert float((dx.float() - slope).abs().max()) <= 2.0 ** -25 + 1e-4 * float(slope.abs().max())
