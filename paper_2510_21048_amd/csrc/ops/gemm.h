@@ -28,6 +28,7 @@ struct GemmArgs {
   int64_t count = 1;
   // set by the launch
   int tiles_m = 0, tiles_n = 0, tiles = 0, splits = 1, span = 0;  // span: k tiles of a split
+  int first = 0;  // workgroup of the launch
   float* part = nullptr;
 };
 
@@ -397,7 +398,7 @@ __global__ __launch_bounds__(C::THREADS) void k_gemm(GemmArgs g, Epi epi) {
   constexpr int SUMS = C::WK > 1 ? FM * FN * 16 * C::THREADS : 0, BYTES = C::WK * 2 * BUF;
   static_assert(!Epi::kSymmetric || Mirror<C>::kBytes <= BYTES);
   __shared__ __attribute__((aligned(1024))) char all_lds[BYTES > SUMS ? BYTES : SUMS];
-  int id = run_of(blockIdx.x, gridDim.x), tm, tn;
+  int id = g.first + run_of(blockIdx.x, gridDim.x), tm, tn;
   const int z = id / (g.tiles * g.splits);
   id -= z * g.tiles * g.splits;
   const int split = id / g.tiles, tile = id % g.tiles;
@@ -643,28 +644,36 @@ inline bool direct_ok(const void* p, int64_t ld, int64_t stride, int64_t contigu
   return aligned(p, 16) && ld % 8 == 0 && stride % 8 == 0 && ld < kMostDirectLd && (contiguous % 8 == 0 || padded);
 }
 
+template <class T, class C, bool AKC, bool BKC, bool DIRECT, bool PAST_L2, class Epi>
+void launch_tiles(GemmArgs g, const Epi& epi, hipStream_t st) {
+  const int64_t all = int64_t(g.tiles) * g.count * g.splits, most = kMostThreads / C::THREADS;
+  for (int64_t first = 0; first < all; first += most) {
+    g.first = int(first);
+    k_gemm<T, C, AKC, BKC, DIRECT, PAST_L2, Epi><<<unsigned(all - first < most ? all - first : most), C::THREADS, 0, st>>>(g, epi);
+  }
+}
+
 template <class T, class C, bool AKC, bool BKC, class Epi>
 int launch(GemmArgs g, const Epi& epi, hipStream_t st) {
   g.tiles_m = int((g.m + C::BM - 1) / C::BM);
   g.tiles_n = int((g.n + C::BN - 1) / C::BN);
   g.tiles = int(tiles_of(g.m, g.n, C::BM, C::BN, Epi::kSymmetric));
-  const unsigned blocks = unsigned(g.tiles * g.count);
   const bool direct = direct_ok(g.a, g.lda, g.stride_a, AKC ? g.k : g.m, g.pad_a) && direct_ok(g.b, g.ldb, g.stride_b, BKC ? g.k : g.n, g.pad_b);
   if constexpr (C::BM == 256 && Epi::kPastL2)
     if (direct && epi.lines()) {
-      k_gemm<T, C, AKC, BKC, true, true, Epi><<<blocks, C::THREADS, 0, st>>>(g, epi);
+      launch_tiles<T, C, AKC, BKC, true, true>(g, epi, st);
       return launched();
     }
   if (direct)
-    k_gemm<T, C, AKC, BKC, true, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
+    launch_tiles<T, C, AKC, BKC, true, false>(g, epi, st);
   else if constexpr (!Epi::kAnyRows)
     return XMEM_EINVAL;  // operands of the library's own workspace, aligned by construction
   else if constexpr (C::STAGED)
-    k_gemm<T, C, AKC, BKC, false, false, Epi><<<blocks * g.splits, C::THREADS, 0, st>>>(g, epi);
+    launch_tiles<T, C, AKC, BKC, false, false>(g, epi, st);
   else
     return launch<T, Medium, AKC, BKC>(g, epi, st);  // a tile's registers would not fit
   if constexpr (C::BM == 64)
-    if (g.splits > 1) k_join<C, Epi><<<blocks, C::GROUP, 0, st>>>(g, epi);
+    if (g.splits > 1) k_join<C, Epi><<<unsigned(g.tiles * g.count), C::GROUP, 0, st>>>(g, epi);
   return launched();
 }
 

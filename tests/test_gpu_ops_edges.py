@@ -161,3 +161,14 @@ def test_policy_of_more_rows_than_a_launch():
     slope = -adv[:, None] / t * (hit - torch.softmax(x.float(), 1))
     # half a unit of float16's subnormals (all of dx are), and 1e-4 of the value
     assert float((dx.float() - slope).abs().max()) <= 2.0 ** -25 + 1e-4 * float(slope.abs().max())
+
+
+def test_linear_of_more_tiles_than_a_launch():
+    """2^30 - 1 rows of one element: tiles of 128 rows in 512 threads are a grid of 2^32 threads, past what one launch may have."""
+    m = 2 ** 30 - 1
+    x = torch.randn(m, 1, device="cuda", dtype=BF)
+    w = torch.randn(1, 1, device="cuda", dtype=BF)
+    log("[ops] linear_forward of 2^30 - 1 rows")
+    y = xm.linear_forward(x, w)[0]
+    torch.cuda.synchronize()
+    assert torch.equal(y, x * w)
