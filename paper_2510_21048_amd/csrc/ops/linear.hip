@@ -182,11 +182,11 @@ __global__ __launch_bounds__(256) void k_dz(const T* dy, int64_t lddy, const T* 
     }
 }
 
-// The bands' sums, 16 runs of bands to a column and those in order.
-__global__ __launch_bounds__(1024) void k_db(const float* part, int64_t nb, int64_t n, float* db) {
+// The bands' sums of the columns from `first` on, 16 runs of bands to a column and those in order.
+__global__ __launch_bounds__(1024) void k_db(const float* part, int64_t nb, int64_t first, int64_t n, float* db) {
   __shared__ float sums[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = int64_t(blockIdx.x) * 64 + lane;
+  const int64_t c = first + int64_t(blockIdx.x) * 64 + lane;
   float sum = 0.0f;
   if (c < n)
 #pragma unroll 8
@@ -277,7 +277,9 @@ int backward(const void* dy, int64_t lddy, const void* z, int64_t ldz, const voi
           static_cast<const T*>(dy) + r0 * lddy, lddy, z ? static_cast<const T*>(z) + r0 * ldz : nullptr, ldz, m - r0, n,
           dz ? dz + r0 * ldd : nullptr, ldd, sums, int(band_rows(m, n)));
     }
-  if (db && n > 0 && bands(m, n) != 1) k_db<<<unsigned((n + 63) / 64), 1024, 0, st>>>(part, bands(m, n), n, db);
+  if (db && bands(m, n) != 1)
+    for (int64_t c = 0; c < n; c += kMostThreads / 1024 * 64)
+      k_db<<<unsigned((n - c < kMostThreads / 1024 * 64 ? n - c + 63 : kMostThreads / 1024 * 64) / 64), 1024, 0, st>>>(part, bands(m, n), c, n, db);
   GemmArgs gx{d, w, ldd, ldw, 0, 0, m, k, n, dz != nullptr}, gw{d, x, ldd, ldx, 0, 0, n, k, m, dz != nullptr};
   Pack px{}, pw{};
   if (packs(k, ldx, m, n, k)) {

@@ -172,3 +172,18 @@ def test_linear_of_more_tiles_than_a_launch():
     y = xm.linear_forward(x, w)[0]
     torch.cuda.synchronize()
     assert torch.equal(y, x * w)
+
+
+def test_linear_gradients_of_more_columns_than_a_launch():
+    """2^28 columns: their sums take 64 a workgroup of 1024 threads, a grid of 2^32 threads, past what one launch may have."""
+    n = 2 ** 28 + 7
+    log("[ops] linear_backward of 2^28 + 7 columns")
+    dy, x, w = (torch.zeros(*size, device="cuda", dtype=BF) for size in ((0, n), (0, 1), (n, 1)))
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    held = torch.full((n,), math.nan, device="cuda")  # what the memory that db gets holds
+    at = held.data_ptr()
+    del held
+    db = xm.linear_backward(dy, x, w, need_dx=False, need_dw=False)[2]
+    torch.cuda.synchronize()
+    assert db.data_ptr() == at and db.shape == (n,) and bool((db == 0).all())
