@@ -102,7 +102,8 @@ size_t xmem_policy_loss_workspace_bytes(int64_t tokens, int64_t vocab);
  * over each sequence first).  A token with weight 0 is not looked at, whatever
  * its logits hold: its lp is 0 and its gradient 0.  Logits of -inf are entries the
  * vocabulary does not offer.  A row without one finite or +inf logit, a row with NaN or
- * +inf, and a token outside [0, vocab) give NaN for that row (and the sums).
+ * +inf, and a token outside [0, vocab) give NaN for that row (and the sums).  A ratio
+ * that overflows times an advantage of 0 is 0; with kl_coef 0 the KL term is reported and nothing else.
  *   d_logits  : [tokens, vocab] of dtype (XMEM_BF16, XMEM_F16 or XMEM_F32), rows ldl apart
  *   d_tokens  : int64 [tokens]
  *   d_weights : float32 [tokens], or NULL for 1/tokens each

@@ -183,14 +183,15 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS == 1024 ? 4 
   float grad = 0.0f;
   if (loss) {
     const float rho = expf(lp - old_lp);
-    const float free = rho * adv, held = fminf(fmaxf(rho, 1.0f - p.low), 1.0f + p.high) * adv;
+    // a ratio past 32 bits times 0 is 0, and so is a KL term past them whose coefficient is 0
+    const float free = adv == 0.0f && rho == INFINITY ? 0.0f : rho * adv, held = fminf(fmaxf(rho, 1.0f - p.low), 1.0f + p.high) * adv;
     const bool clipped = held < free;
     float kl = 0.0f;
     grad = clipped ? 0.0f : -free;
     if (p.ref) {
       const float d = ref - lp, e = expm1f(d);
       kl = e - d;
-      grad -= p.kl_coef * e;
+      if (p.kl_coef != 0.0f) grad -= p.kl_coef * e;
     }
     grad *= wt;
     if (tid == 0) {
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(1024) void k_policy_sums(const float* part, int64_t
       v[q] = 0.0;
       for (int i = 0; i < 16; ++i) v[q] += sums[q][i];
     }
-    stats[0] = float(v[0] + double(kl_coef) * v[1]);
+    stats[0] = float(kl_coef != 0.0f ? v[0] + double(kl_coef) * v[1] : v[0]);
     stats[1] = float(v[0]), stats[2] = float(v[1]), stats[3] = float(v[2]);
   }
 }

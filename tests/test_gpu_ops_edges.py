@@ -187,3 +187,30 @@ def test_linear_gradients_of_more_columns_than_a_launch():
     db = xm.linear_backward(dy, x, w, need_dx=False, need_dw=False)[2]
     torch.cuda.synchronize()
     assert db.data_ptr() == at and db.shape == (n,) and bool((db == 0).all())
+
+
+@pytest.mark.parametrize("v", [33, 600, 4100, 60000, 140000])
+def test_policy_terms_of_weight_nothing(v):
+    """What is multiplied by 0 adds 0, however large: a ratio past 32 bits times an advantage of 0, and a KL term past 32 bits
+    whose coefficient is 0 (it is still reported)."""
+    from test_gpu_ops import policy_check, policy_inputs
+    x, y, wt, old, adv, refp = policy_inputs(6, v, torch.float32, 40 + v)
+    wt[:] = 0.25
+    lp = (x.double()[torch.arange(6), y] - torch.logsumexp(x.double(), 1)).float()
+    old[1], adv[1] = lp[1] - 100, 0.0  # exp(100) is past 32 bits
+    old[2], adv[2] = -math.inf, 0.0
+    log(f"[ops] policy_loss, terms of weight 0, v={v}")
+    # 64 bits hold exp(100) 0 = 0; exp(inf) 0 counts as the same
+    finite = old.clone()
+    finite[2] = lp[2]
+    got = xm.policy_loss(x.cuda(), *[a.cuda() for a in (y, wt, old, adv)], clip_low=0.2, clip_high=0.28)
+    policy_check(got, x, y, wt, finite, adv, None, 0.0)
+    far = refp.clone()
+    far[3] = lp[3] + 100
+    stats, lp2, dx = xm.policy_loss(x.cuda(), *[a.cuda() for a in (y, wt, old, adv, far)], clip_low=0.2, clip_high=0.28, kl_coef=0.0)
+    assert torch.equal(stats[:2], got[0][:2]) and float(stats[2]) == math.inf and torch.equal(stats[3], got[0][3])
+    assert torch.equal(lp2, got[1]) and torch.equal(dx, got[2])
+    # NaN is none of these
+    old[1] = math.nan
+    stats, _, dx = xm.policy_loss(x.cuda(), *[a.cuda() for a in (y, wt, old, adv)], clip_low=0.2, clip_high=0.28)
+    assert bool(stats[0].isnan()) and bool(dx[1].isnan().all()) and not bool(dx[2].isnan().any())
