@@ -167,12 +167,13 @@ def _workspace(workspace, need: int, device):
 def _raw_stream(device) -> int:
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # what current_stream() wraps, at a tenth of its time
-    index = device.index
-    return raw(index) if raw is not None and index is not None else torch.cuda.current_stream(device).cuda_stream
+    return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 class _Here:
     """A call on the current stream: torch's allocator orders what it takes by that stream already."""
+
+    __slots__ = ("raw",)
 
     def __init__(self, raw):
         self.raw = raw
@@ -180,11 +181,10 @@ class _Here:
     def __enter__(self):
         return self
 
-    def __exit__(self, *_):
+    def __exit__(self, kind, value, trace):
         return False
 
-    @staticmethod
-    def out(*tensors):
+    def out(self, *tensors):
         return tensors if len(tensors) > 1 else tensors[0]
 
 
@@ -223,8 +223,10 @@ class _There:
 def _on(device, stream, *given):
     """Where a call on checked tensors (the workspace among them) runs."""
     import torch
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given):
-        raise XmemError("an input requires a gradient, which is not recorded here: detach it or call under torch.no_grad()")
+    if torch.is_grad_enabled():
+        for t in given:
+            if t is not None and t.requires_grad:
+                raise XmemError("an input requires a gradient, which is not recorded here: detach it or call under torch.no_grad()")
     here = _raw_stream(device)
     raw = here if stream is None else stream
     return _Here(here) if raw == here and torch.cuda.current_device() == device.index else _There(device, raw, given)
@@ -248,14 +250,14 @@ def linear_forward(x, w, bias=None, residual=None, activation: str = "none", sav
     ``linear_backward`` needs of an activation), else None."""
     import torch
     lib = load_ops()
-    act, code, dev = _activation(activation), _dtype(x, "x"), x.device
-    ldx, ldw = _matrix(x, "x"), _matrix(w, "w", None, x.shape[1], x.dtype, x.device)
-    (m, k), n = x.shape, w.shape[0]
-    ldr = 0 if residual is None else _matrix(residual, "residual", m, n, x.dtype, dev)
+    act, code, dt, dev = _activation(activation), _dtype(x, "x"), x.dtype, x.device
+    ldx, (m, k) = _matrix(x, "x"), x.shape
+    ldw, n = _matrix(w, "w", None, k, dt, dev), w.shape[0]
+    ldr = 0 if residual is None else _matrix(residual, "residual", m, n, dt, dev)
     _vector(bias, "bias", n, torch.float32, dev)
     with _on(dev, stream, x, w, bias, residual, workspace) as on:
-        y = torch.empty((m, n), dtype=x.dtype, device=dev)
-        z = torch.empty((m, n), dtype=x.dtype, device=dev) if save_z else None
+        y = x.new_empty((m, n))
+        z = x.new_empty((m, n)) if save_z else None
         workspace, size = _workspace(workspace, lib.xmem_linear_forward_workspace_bytes(m, n, k, ldx, ldw), dev)
         _check(xmem_linear_forward(x, ldx, w, ldw, bias, residual, ldr, m, n, k, code, act, y, n, z, n, workspace, size, on.raw),
                "xmem_linear_forward")
@@ -278,8 +280,8 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", need_dx: bool = 
         raise XmemError("z: wanted with an activation (linear_forward's save_z)")
     ldz = 0 if z is None else _matrix(z, "z", m, n, dy.dtype, dev)
     with _on(dev, stream, dy, x, w, z, workspace) as on:
-        dx = torch.empty((m, k), dtype=dy.dtype, device=dev) if need_dx else None
-        dw = torch.empty((n, k), dtype=dy.dtype, device=dev) if need_dw else None
+        dx = dy.new_empty((m, k)) if need_dx else None
+        dw = dy.new_empty((n, k)) if need_dw else None
         db = torch.empty(n, dtype=torch.float32, device=dev) if need_db else None
         workspace, size = _workspace(workspace, xmem_linear_backward_workspace_bytes(m, n, k, lddy, ldx, ldw, act), dev)
         _check(xmem_linear_backward(dy, lddy, z, ldz, x, ldx, w, ldw, m, n, k, code, act, dx, k, dw, k, db, workspace, size, on.raw),
@@ -327,7 +329,7 @@ def policy_loss(logits, tokens, weights, old_logp, advantages, ref_logp=None, cl
         logp = torch.empty(t, dtype=torch.float32, device=dev)
         dlogits, ldd = None, 0
         if need_dlogits:
-            dlogits, ldd = (logits, ldl) if in_place else (torch.empty((t, v), dtype=logits.dtype, device=dev), v)
+            dlogits, ldd = (logits, ldl) if in_place else (logits.new_empty((t, v)), v)
         workspace, size = _workspace(workspace, xmem_policy_loss_workspace_bytes(t, v), dev)
         _check(xmem_policy_loss(logits, ldl, tokens, weights, old_logp, advantages, ref_logp, t, v, code, clip_low, clip_high,
                                 kl_coef, grad_scale, stats, logp, dlogits, ldd, workspace, size, on.raw), "xmem_policy_loss")
