@@ -13,14 +13,12 @@ typedef _Float16 f16;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-template <class T> struct Vec;  // eight 16-bit elements: what a lane holds of an operand; four: of a result
+template <class T> struct Vec;  // eight 16-bit elements: what a lane holds of an operand
 template <> struct Vec<bf16> {
   typedef bf16 x8 __attribute__((ext_vector_type(8)));
-  typedef bf16 x4 __attribute__((ext_vector_type(4)));
 };
 template <> struct Vec<f16> {
   typedef f16 x8 __attribute__((ext_vector_type(8)));
-  typedef f16 x4 __attribute__((ext_vector_type(4)));
 };
 
 constexpr int kWave = 64;
@@ -34,11 +32,6 @@ inline size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
 inline int launched() { return hipGetLastError() == hipSuccess ? XMEM_OK : XMEM_EHIP; }
 
 // Sums over the wavefront, every lane getting the result.  The order is fixed.
-__device__ inline float wave_sum(float v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
-}
 __device__ inline double wave_sum(double v) {
 #pragma unroll
   for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
