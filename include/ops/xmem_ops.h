@@ -3,8 +3,7 @@
  *
  * The estimator of xmem.h says what a recorded step needs; these operators are
  * the parts of a step that allocate nothing by themselves: every output and
- * every workspace is the caller's, sized by a function of the shapes, so the
- * step's allocation trace can be written down without running it.
+ * every workspace is the caller's, and its size a function of the shapes.
  *
  *   xmem_linear_forward/_backward  y = act(x w^T + b) + r and its gradients
  *   xmem_policy_loss               clipped policy loss with a KL term over a
@@ -17,7 +16,9 @@
  * Matrices are row-major; ld* is the distance between rows in elements and at
  * least the row's length.  Rows need no more than their elements' alignment;
  * the fast loads want 16-byte aligned pointers and ld a multiple of 8 (and k a
- * multiple of 8 where rows are summed along).  Errors are the XMEM_E* codes of xmem.h. */
+ * multiple of 8 where rows are summed along).  Rows that are not are copied where
+ * the product is large; an operand whose pointer alone is not aligned is read
+ * through registers, at less than half the speed of a large product.  Errors are the XMEM_E* codes of xmem.h. */
 #ifndef XMEM_OPS_H
 #define XMEM_OPS_H
 
@@ -72,7 +73,7 @@ size_t xmem_linear_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int
 /* The gradients of xmem_linear_forward for an output gradient dy:
  *   dz = dy act'(z);  dx = dz w;  dw = dz^T x;  db = sum over rows of dz.
  * The residual's gradient is dy itself.  dz is rounded to dtype for the two
- * products (db sums it before that).
+ * products (db sums it before that): a float16 dz past 65,504 becomes infinite.
  *   d_dy : [m, n] of dtype
  *   d_z  : [m, n] of dtype as xmem_linear_forward wrote it; not looked at (and
  *          NULL allowed) where activation is XMEM_ACT_NONE

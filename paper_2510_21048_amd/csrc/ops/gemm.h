@@ -6,7 +6,7 @@
 //
 // What bounds it.  A tile of 256 x 256 reads 64 KiB an operand pair for 64 k, which its matrix instructions use for 2,048 cycles;
 // its LDS reads take 1,536 of them without a bank conflict.  On values of 0 (no power limit) 8192 x 8192 x 8192 runs at 1,480
-// TFLOP/s, and at 1,770 where every k tile's loads come from the same place: the loads that miss the L2 (19%) hold it back.
+// TFLOP/s, and at 1,770 where every k tile's loads come from the same place: the loads that miss the L2 (21%) hold it back.
 // On random values the clock falls: 1,270 to 1,440 TFLOP/s for x w^T, 1,050 to 1,200 for dz w, 1,120 to 1,290 for dz^T x, where the
 // library's products reach 1,370 to 1,580, 1,210 to 1,370 and 1,070 to 1,210.  Small ones are bound by their latency: a launch
 // (2.1 us), the first loads, one reduction and the writes take 6.5 us for one k tile, each further group of four 0.8.
@@ -284,10 +284,6 @@ __device__ inline void tile_of(int id, const GemmArgs& g, int& tm, int& tn) {
   }
 }
 
-// What a lane has of a tile: FN products' four neighbours each, of FM rows.  Two products' fours, exchanged between the
-// lanes 16 apart, are eight neighbours of one or the other: the epilogue takes these, 16 bytes at a time and 64 next to
-// each other, from row i0 on every STEP-th; what it reads of memory is asked for four rows at a time, before anything
-// of them is written.  The Q-th eight of a lane; recursive, so that acc is indexed by constants however long the epilogue is.
 // The mirrored block of a symmetric product's tile: the epilogue's values as they were written, kept in LDS row by row in
 // the layout of an operand with its rows contiguous, whose transposing reads give a lane eight neighbours of a column.
 // 5 of 4096 x 4096 x 4096: 345 us; written entry by entry from the lanes' accumulators 372.
@@ -329,6 +325,10 @@ template <bool WHOLE_, bool PAST_L2_>
 struct How {
   static constexpr bool WHOLE = WHOLE_, PAST_L2 = PAST_L2_;
 };
+// What a lane has of a tile: FN products' four neighbours each, of FM rows.  Two products' fours, exchanged between the
+// lanes 16 apart, are eight neighbours of one or the other: the epilogue takes these, 16 bytes at a time and 64 next to
+// each other, from row i0 on every STEP-th; what it reads of memory is asked for four rows at a time, before anything
+// of them is written.  The Q-th eight of a lane; recursive, so that acc is indexed by constants however long the epilogue is.
 template <class C, int STEP, int Q, class HOW, class Epi>
 __device__ __attribute__((always_inline)) inline void finish(const f32x4 (&acc)[C::FM][C::FN], int i0, const Epi& epi, int64_t m0,
                                                              int64_t n0, int z, const GemmArgs& g, char* lds) {

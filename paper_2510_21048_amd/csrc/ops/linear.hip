@@ -6,8 +6,9 @@
 //
 // dz is rounded to 16 bits, as the matrix instructions take it (the products' outputs are rounded to as many: 1.4 times
 // their error without); db sums it before that.  No sum's order depends on when a workgroup runs.
-// 8192 x 8192 x 2048 with gelu and z: 242 to 272 us (1,010 to 1,140 TFLOP/s; its 268 MB of outputs alone take 40); the gradients 572 us, of which
-// k_dz 88 (402 MB at 4.6 TB/s).  32768 x 4096 x 16384 with a residual: 3.4 ms.  One token through 4096 x 1024: 8.6 us.
+// 8192 x 8192 x 2048 with gelu and z: 262 to 282 us by the card (975 to 1,050 TFLOP/s; its 268 MB of outputs alone take 55 at a
+// large copy's rate); the gradients 572 to 615 us, of which k_dz 88 (402 MB at 4.6 TB/s).  32768 x 4096 x 16384 with a residual: 3.4 ms.
+// One token through 4096 x 1024: 8.5 us.
 #include "gemm.h"
 
 using namespace xops;
@@ -17,7 +18,8 @@ namespace {
 constexpr float kGelu = 0.7978845608028654f, kCube = 0.044715f;  // sqrt(2 / pi)
 
 // (1 + tanh(u)) / 2 is the logistic function of 2u, without a difference of near numbers: gelu(z) = z s(2u), as
-// silu(z) = z s(z).  exp and 1/x are the hardware's, good to 2^-22 of their values.
+// silu(z) = z s(z).  exp and 1/x are the hardware's; 1/x is good to 2^-22 of its value, exp(v) to |v| 2^-24 more, since
+// v log2(e) is rounded before the power of two (2^-18 at v = 80, where the logistic function is next to nothing).
 __device__ inline float logistic(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
 __device__ inline float gelu_argument(float z) { return z * (2.0f * kGelu + (2.0f * kGelu * kCube) * (z * z)); }
 
@@ -123,7 +125,9 @@ struct StoreEpilogue {
 
 constexpr int kBandCols = 512;  // columns of a workgroup of k_dz, eight a lane
 
-// Rows whose column sums one workgroup of k_dz takes: 64, or 16 where that would leave most CUs without one.
+// Rows whose column sums one workgroup of k_dz takes: 64, or 16 where that makes fewer than four workgroups a CU (128 does not
+// pay anywhere near).  us with db and, with gelu, dw of 8 columns, 16 rows and 64: 128 x 4096 21.4 and 24.9, 2048 x 4096 29.3 and
+// 41.3, 4096 x 4096 38.6 and 50.4, 8192 x 4096 (1,024 workgroups of 64) 61.2 and 61.5, 8192 x 8192 130.5 and 122.8.
 inline int64_t band_rows(int64_t m, int64_t n) { return (m + 63) / 64 * ((n + kBandCols - 1) / kBandCols) < 4 * kCus ? 16 : 64; }
 inline int64_t bands(int64_t m, int64_t n) { return (m + band_rows(m, n) - 1) / band_rows(m, n); }
 

@@ -15,8 +15,11 @@
 // On matrices of normal values the products alone, in bfloat16, leave 1e-2; in half precision without these, 1.5e-3;
 // where one direction holds most of a gradient, 1.6e-1 and 2e-2.
 //
-// Bound by the products where matrices are large: 24 of 8192 x 2048 take 17.0 ms, of which the five X X^T 5.1 (800 TFLOP/s of the
-// half that is computed: 864 tiles in 3.4 rounds), P P 1.3, Q X 7.6 to 9.3 (its 32 k tiles a workgroup are followed by 8 bytes read and
+// A |u| far below the 1e-7 added to it makes X as small, and its entries lose bits past half precision's range: of an update below
+// a hundredth of a usual one.
+//
+// Bound by the products where matrices are large: 24 of 8192 x 2048 take 17.0 to 17.3 ms, of which the five X X^T 5.1 to 5.4 (800 TFLOP/s of
+// the half that is computed: 864 tiles in 3.4 rounds), P P 1.3, Q X 7.6 to 9.3 (its 32 k tiles a workgroup are followed by 8 bytes read and
 // written an element, which nothing hides), momentum and start 1.6 (4 GB each at 4.5 and 5.5 TB/s).  A single 1024 x 1024 takes
 // 159 us: 17 launches one after another, 10 us a product.
 #include "gemm.h"

@@ -3,10 +3,12 @@
 // With m the row's largest logit and s = sum_j exp(x_j - m), the token's log-probability is (x_y - m) - log s, every other
 // number of a row follows from it and four scalars, and dx_j = c (1[j = y] - exp(x_j - m) / s) with one c a row.  So a row is
 // read once and its gradient written once: a workgroup keeps it in registers between the two (52 a thread for 50,304 logits of
-// 16 bits in 512 threads).  Exponentials and sums are in 32 bits, the batch's sums in 64 and in a fixed order (k_policy_sums).
+// 16 bits in 512 threads).  Rows past 16,384 pieces of 16 bytes (131,072 logits of 16 bits, 65,536 of 32) do not fit there: those are
+// read twice where a gradient is wanted, 2048 x 131072 in float32 in 583 us.
+// Exponentials and sums are in 32 bits, the batch's sums in 64 and in a fixed order (k_policy_sums).  exp(x - m) is a power of two of
+// (x - m) log2(e), whose rounding adds |x - m| 2^-24 to a term's relative error: terms that count are near m.
 // Bound by memory: 32768 x 50304 in bfloat16, 30% of the rows masked, 5.6 GB in 1.08 ms (5.2 TB/s; a large copy reaches 4.9);
-// log-probabilities of 2048 x 50304 42 us (4.9 TB/s).  Rows past 16,384 pieces of 16 bytes are read again for the gradient: 2048 x 131072
-// in float32 583 us.  A row and its sums take 8 us at least: two launches.
+// log-probabilities of 2048 x 50304 42 us (4.9 TB/s).  A row and its sums take 8 us at least: two launches.
 #include "common.h"
 
 using namespace xops;
@@ -258,6 +260,11 @@ int launch_rows(Policy p, hipStream_t st) {
   return launched();
 }
 
+// The fewest threads whose registers hold a row: 4 pieces of 16 bytes a thread where a row is a wavefront; 8 of 256 threads; 13 of
+// 512, the most that leave six wavefronts a SIMD their registers (80); 16 of 1024.  Measured in us at each limit, 16 bits, with a gradient and
+// without: 32768 rows of 2048 52 and 28, in 256 threads 72 and 46; 4096 rows of 16,384 48 and 24, in 512 threads 51 and 30; of 50,304 168 and
+// 77, in 1024 threads 239 and 145 (in 512 with 16 pieces and four wavefronts a SIMD 159 and 87); of 131,072 545 and 281, read again
+// 563 and 266.  So without a gradient, where nothing is read again, a row past 512 x 13 pieces is not kept either (100,000: 209, kept 237).
 template <class T>
 int launch_policy(const Policy& p, hipStream_t st) {
   const int64_t chunks = (p.vocab + kPer<T> - 1) / kPer<T>;
