@@ -125,8 +125,8 @@ struct StoreEpilogue {
 
 constexpr int kBandCols = 512;  // columns of a workgroup of k_dz, eight a lane
 
-// Rows whose column sums one workgroup of k_dz takes: 64, or 16 where that makes fewer than four workgroups a CU (128 does not
-// pay anywhere near).  us with db and, with gelu, dw of 8 columns, 16 rows and 64: 128 x 4096 21.4 and 24.9, 2048 x 4096 29.3 and
+// Rows whose column sums one workgroup of k_dz takes: 64, or 16 where that makes fewer than four workgroups a CU (128 are a third
+// slower there, and 2 to 8% faster only from 4,096 workgroups of 64 on).  us with db and, with gelu, dw of 8 columns, 16 rows and 64: 128 x 4096 21.4 and 24.9, 2048 x 4096 29.3 and
 // 41.3, 4096 x 4096 38.6 and 50.4, 8192 x 4096 (1,024 workgroups of 64) 61.2 and 61.5, 8192 x 8192 130.5 and 122.8.
 inline int64_t band_rows(int64_t m, int64_t n) { return (m + 63) / 64 * ((n + kBandCols - 1) / kBandCols) < 4 * kCus ? 16 : 64; }
 inline int64_t bands(int64_t m, int64_t n) { return (m + band_rows(m, n) - 1) / band_rows(m, n); }
