@@ -30,17 +30,18 @@ def test_linear_backward_last_tile_of_few_rows(size, dtype):
 
 
 def calls():
-    """Each operator as a call of a stream, on inputs of the current one, with sizes that need a workspace."""
+    """Each operator as a call of a stream, on inputs made beforehand on the current one, with sizes that need a workspace."""
     g = torch.Generator().manual_seed(77)
     new = lambda *s: torch.randn(*s, generator=g).to(BF).cuda()
     x, w, dy, z = new(512, 4096), new(256, 4096), new(512, 256), new(512, 256)
     logits, tokens = new(300, 999), torch.randint(0, 999, (300,), generator=g).cuda()
     f = [torch.randn(300, generator=g).cuda() for _ in range(4)]
+    weights, old, refp = f[0].abs(), f[1] - 7, f[3] - 7
     grad, mom = new(2, 512, 300), torch.randn(2, 512, 300, generator=g).cuda()
     return {
         "xmem_linear_forward": lambda s: xm.linear_forward(x[:128], w, activation="gelu", save_z=True, stream=s),
         "xmem_linear_backward": lambda s: xm.linear_backward(dy, x, w, z, "silu", stream=s),
-        "xmem_policy_loss": lambda s: xm.policy_loss(logits, tokens, f[0].abs(), f[1] - 7, f[2], f[3] - 7, kl_coef=0.1, stream=s),
+        "xmem_policy_loss": lambda s: xm.policy_loss(logits, tokens, weights, old, f[2], refp, kl_coef=0.1, stream=s),
         "xmem_muon_update": lambda s: (xm.muon_update(grad, mom.clone() if s is None else mom, stream=s),),
     }
 
