@@ -215,3 +215,39 @@ def test_policy_terms_of_weight_nothing(v):
     old[1] = math.nan
     stats, _, dx = xm.policy_loss(x.cuda(), *[a.cuda() for a in (y, wt, old, adv)], clip_low=0.2, clip_high=0.28)
     assert bool(stats[0].isnan()) and bool(dx[1].isnan().all()) and not bool(dx[2].isnan().any())
+
+
+def test_operators_in_a_graph():
+    """A captured step of every operator, replayed on new inputs with eager work and synchronizations between: each replay is the
+    eager result, bit for bit."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    new = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    x, w, dy = new(200, 1000).to(BF), (new(300, 1000) / 30).to(BF), new(200, 300).to(BF)
+    y, f = torch.randint(0, 300, (200,), generator=g, device="cuda"), [new(200) for _ in range(3)]
+    mom = new(300, 1000)
+
+    def step(m):
+        out, z = xm.linear_forward(x, w, activation="gelu", save_z=True)
+        dx, dw, db = xm.linear_backward(dy, x, w, z, "gelu")
+        stats, lp, dlogits = xm.policy_loss(out, y, None, f[0] - 6, f[1], f[2] - 6, kl_coef=0.1)
+        return out, z, dx, dw, db, stats, lp, dlogits, xm.muon_update(dw, m), xm.token_logp(out, y), m
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(mom.clone())
+    torch.cuda.current_stream().wait_stream(side)
+    graph, held = torch.cuda.CUDAGraph(), mom.clone()
+    with torch.cuda.graph(graph):
+        got = step(held)
+    for i in range(4):
+        x.copy_(new(200, 1000))
+        dy.copy_(new(200, 300))
+        held.copy_(mom)
+        want = step(mom.clone())
+        torch.cuda.synchronize()
+        log(f"[ops] graph replay {i}")
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a, b)
