@@ -22,3 +22,8 @@ from .ops import (  # noqa: F401
     xmem_linear_backward, xmem_linear_backward_workspace_bytes, xmem_linear_forward, xmem_linear_forward_workspace_bytes,
     xmem_muon_update, xmem_muon_update_workspace_bytes, xmem_policy_loss, xmem_policy_loss_workspace_bytes,
 )
+from .ops_step import (  # noqa: F401
+    GATES, NORMS, XMEM_NO_PADDING, clip_grad_norm, embedding_backward, embedding_forward, residual_norm_backward, residual_norm_forward,
+    xmem_clip_grad_norm, xmem_clip_grad_norm_workspace_bytes, xmem_embedding_backward, xmem_embedding_backward_workspace_bytes,
+    xmem_embedding_forward, xmem_residual_norm_backward, xmem_residual_norm_backward_workspace_bytes, xmem_residual_norm_forward,
+)

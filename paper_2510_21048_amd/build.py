@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
@@ -13,7 +14,7 @@ LIB = PKG / "libxmem_replay.so"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # no packed fp32 instructions anywhere (none are needed: the path is integer-only)
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # the row tables order their integer keys as doubles, none of them a NaN: min and max need no quieting
@@ -31,32 +32,36 @@ FLAGS = [
 OPS_SRCS = sorted((PKG / "csrc" / "ops").glob("*.hip"))
 OPS_LIB = PKG / "libxmem_ops.so"
 OPS_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # no packed fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
 
 
-def _start(flags, srcs, out: Path):
-    return subprocess.Popen([HIPCC, *flags, f"-I{ROOT / 'include'}", *map(str, srcs), "-o", str(out)],
-                            stderr=subprocess.PIPE)
+def _run(cmd):
+    return subprocess.Popen([HIPCC, *map(str, cmd)], stderr=subprocess.PIPE)
 
 
-def _finish(proc, tmp: Path, lib: Path) -> None:
+def _wait(proc) -> None:
     err = proc.communicate()[1]
     if proc.returncode:
         raise subprocess.CalledProcessError(proc.returncode, proc.args, stderr=err)
-    os.replace(tmp, lib)
 
 
 def build() -> Path:
-    """Compile both libraries every time it is called, side by side (under a minute)."""
-    started = []
-    for flags, srcs, lib in ((FLAGS, SRCS, LIB), (OPS_FLAGS, OPS_SRCS, OPS_LIB)):
-        tmp = lib.with_suffix(".so.tmp")
-        started.append((_start(flags, srcs, tmp), tmp, lib))
-    for proc, tmp, lib in started:
-        _finish(proc, tmp, lib)
+    """Compile both libraries every time it is called, all sources side by side (about a minute)."""
+    with tempfile.TemporaryDirectory() as at:
+        started = []
+        for flags, srcs, lib in ((FLAGS, SRCS, LIB), (OPS_FLAGS, OPS_SRCS, OPS_LIB)):
+            objects = [Path(at) / f"{lib.stem}_{src.stem}.o" for src in srcs]
+            compiling = [_run([*flags, f"-I{ROOT / 'include'}", "-c", src, "-o", obj]) for src, obj in zip(srcs, objects)]
+            started.append((flags, lib, objects, compiling))
+        for flags, lib, objects, compiling in started:
+            for proc in compiling:
+                _wait(proc)
+            tmp = lib.with_suffix(".so.tmp")
+            _wait(_run([*flags, "-shared", *objects, "-o", tmp]))
+            os.replace(tmp, lib)
     return LIB
 
 

@@ -49,6 +49,15 @@ def load_ops():
             ("xmem_policy_loss", [vp, i64] + [vp] * 5 + [i64] * 2 + [i32] + [f32] * 4 + [vp] * 3 + [i64, vp, size, vp], i32),
             ("xmem_muon_update_workspace_bytes", [i64] * 3, size),
             ("xmem_muon_update", [vp, i32, vp] + [i64] * 3 + [f32, i32, i32, f32, vp, vp, size, vp], i32),
+            ("xmem_residual_norm_forward", [vp, i64] * 3 + [vp, f32, i32, vp, vp, i32, vp, vp, i32, f32, i64, i64, i32, vp, i64, vp, i64, vp, vp], i32),
+            ("xmem_residual_norm_backward_workspace_bytes", [i64, i64, i32], size),
+            ("xmem_residual_norm_backward", [vp, i64] * 3 + [vp] + [vp, i64] * 2 + [vp, f32, i32, vp, vp, i32, vp, i32, i64, i64, i32] + [vp, i64] * 3
+             + [vp] * 6 + [size, vp], i32),
+            ("xmem_embedding_forward", [vp, i64, vp] + [i64] * 3 + [i32, f32, i64, vp, i64, vp], i32),
+            ("xmem_embedding_backward_workspace_bytes", [i64] * 3, size),
+            ("xmem_embedding_backward", [vp, i64, vp] + [i64] * 3 + [i32, f32, i64, i32, i32, vp, i64, vp, size, vp], i32),
+            ("xmem_clip_grad_norm_workspace_bytes", [], size),
+            ("xmem_clip_grad_norm", [vp, vp, vp, i64, f32, f32, vp, vp, size, vp], i32),
         ):
             f = getattr(lib, name)
             f.argtypes, f.restype = args, res
