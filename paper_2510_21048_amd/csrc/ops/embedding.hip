@@ -134,16 +134,19 @@ __global__ __launch_bounds__(256) void k_scan(TableGrad p) {
 
 // Rows are spread over groups of kKeys or fewer by a multiplication: key = id * mul mod 2^bits, of which the upper bits are
 // the group, so that frequent tokens (whose numbers are often neighbours) do not meet in one.
-constexpr int kGroups = 256, kKeys = 1024, kWaves = 16;
-constexpr int kRun = 32;  // entries of the sorted list that one wavefront adds up
+constexpr int kMostBits = 22;  // of a key: products of 24 bits
+constexpr int kGroups = 256, kKeyBits = 10, kKeys = 1 << kKeyBits, kWaves = 16;
+constexpr int kNotes = 1024;  // of a wavefront
+constexpr int kRun = 16;  // entries of the sorted list that one wavefront adds up
 
 struct Groups {
   int bits, low;  // of a key, and of its place in the group
   unsigned mul, inverse;
   int64_t count() const { return int64_t(1) << (bits - low); }
-  __host__ __device__ unsigned key(unsigned id) const { return (id * mul) & mask(); }
-  __host__ __device__ unsigned id(unsigned key) const { return (key * inverse) & mask(); }
+  __host__ __device__ int words() const { return low > 6 ? 1 << (low - 6) : 1; }  // of 64 keys, in a group
   __host__ __device__ unsigned mask() const { return (1u << bits) - 1; }
+  __device__ unsigned key(unsigned id) const { return __umul24(id, mul) & mask(); }
+  __device__ unsigned id(unsigned key) const { return __umul24(key, inverse) & mask(); }
 };
 Groups groups_of(int64_t vocab) {
   Groups g{0, 0, 0, 0};
@@ -151,18 +154,21 @@ Groups groups_of(int64_t vocab) {
   g.mul = unsigned(0.6180339887 * double(int64_t(1) << g.bits)) | 1;
   g.inverse = 1;
   for (int i = 0; i < 5; ++i) g.inverse *= 2 - g.mul * g.inverse;  // twice the bits a step
+  g.inverse &= g.mask();
   while ((int64_t(1) << (g.bits - g.low)) > kGroups && (1 << g.low) < kKeys) ++g.low;
   return g;
 }
 
 struct Lists {
   int *token, *row;  // sorted: tokens of one row together and in their order
-  int* count;        // entries
-  int* state;        // of a run of kRun entries, see k_sum
+  int* count;        // entries, and rows that go past two runs of kRun entries
+  int* state;        // of a run, see k_sum
+  int* begin;        // the runs in which those rows begin, in any order
+  uint64_t* empty;   // a bit for each key whose row is in the table and has no token
   float* part;       // two rows a run
   size_t bytes;
 };
-Lists carve(void* base, int64_t t, int64_t n) {
+Lists carve(void* base, int64_t t, const Groups& groups, int64_t n) {
   Lists w;
   char* at = static_cast<char*>(base);
   const auto take = [&](size_t b) {
@@ -173,71 +179,95 @@ Lists carve(void* base, int64_t t, int64_t n) {
   const int64_t runs = (t + kRun - 1) / kRun;
   w.token = reinterpret_cast<int*>(take(size_t(t) * 4));
   w.row = reinterpret_cast<int*>(take(size_t(t) * 4));
-  w.count = reinterpret_cast<int*>(take(4));
+  w.count = reinterpret_cast<int*>(take(8));
   w.state = reinterpret_cast<int*>(take(size_t(runs) * 4));
+  w.begin = reinterpret_cast<int*>(take(size_t(runs) * 4));
+  w.empty = reinterpret_cast<uint64_t*>(take(size_t(groups.count()) * groups.words() * 8));
   w.part = reinterpret_cast<float*>(take(size_t(runs) * 2 * size_t(n) * 4));
   w.bytes = size_t(at - static_cast<char*>(base));
   return w;
 }
 
-// A workgroup has the rows of one group.  It looks at every token twice, each wavefront at a sixteenth of them in order: first it
-// counts its own rows' and those of the groups before, then it puts its own where these counts say.  Rows without a token are cleared.
-template <class O>
-__global__ __launch_bounds__(kWaves * 64) void k_group(TableGrad p, Groups groups, Lists lists) {
-  __shared__ int hist[kWaves][kKeys], meet[kWaves][2];
+// A workgroup has the rows of one group.  It looks at every token, each wavefront at a sixteenth of them in order, counts those of the
+// groups before and notes its own in LDS; then it counts its rows' tokens and puts them where these counts say.  Where a wavefront has
+// more than kNotes of its own, its workgroup reads the tokens again for each of the two.
+__global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64_t t, unsigned vocab, unsigned padding, Groups groups, Lists lists) {
+  __shared__ int hist[kWaves][kKeys], meet[kWaves][2], sums[kWaves];
+  __shared__ unsigned notes[kWaves][kNotes];  // place in the group, and the token's number in the wavefront's share
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int keys = 1 << groups.low;
-  const unsigned mine = blockIdx.x;
-  for (int i = threadIdx.x; i < kWaves * keys; i += kWaves * 64) hist[i / keys][i % keys] = 0;
-  __syncthreads();
-  const int64_t share = ((p.t + kWaves - 1) / kWaves + 63) / 64 * 64, from = wave * share, to = from + share < p.t ? from + share : p.t;
-  // the key, or all bits where the token adds nothing
-  const auto key_at = [&](int64_t i) {
-    const int64_t id = i < to ? p.ids[i] : -1;
-    return id >= 0 && id < p.vocab && id != p.padding ? groups.key(unsigned(id)) : ~0u;
-  };
-  int before = 0, all = 0;
-#pragma unroll 8
-  for (int64_t i = from + lane; i < to; i += 64) {
-    const unsigned key = key_at(i);
-    const unsigned group = key == ~0u ? ~0u : key >> groups.low;
-    before += group < mine;
-    all += key != ~0u;
-    if (group == mine) atomicAdd(&hist[wave][key & (keys - 1)], 1);
-  }
+  const unsigned mine = blockIdx.x, mask = groups.mask(), width = groups.bits - groups.low;
+  for (int i = threadIdx.x; i < kWaves * keys; i += kWaves * 64) hist[i >> groups.low][i & (keys - 1)] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) lists.count[1] = 0;
+  const int64_t share = ((t + kWaves - 1) / kWaves + 63) / 64 * 64, from = wave * share < t ? wave * share : t;
+  const int n = int(from + share < t ? share : t - from);
+  ids += from;
+  int before = 0, own = 0;
+  // calls f(the lanes whose token is of this group, a lane's place in it, the first lane's token) for 64 tokens at a time
+  const auto each = [&](const auto& f) {
+    constexpr int kBatch = 8;
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += kBatch * 64) {
+      uint64_t id[kBatch];
 #pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    before += __shfl_xor(before, d);
-    all += __shfl_xor(all, d);
-  }
+      for (int j = 0; j < kBatch; ++j) id[j] = ids[i0 + j * 64 + lane < n ? i0 + j * 64 + lane : 0];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const unsigned low = unsigned(id[j]), high = unsigned(id[j] >> 32), key = __umul24(low, groups.mul) & mask;
+        const uint64_t there = __ballot(high == 0) & __ballot(low < vocab) & __ballot(low != padding) & __ballot(i0 + j * 64 + lane < n);
+        const unsigned group = __builtin_amdgcn_ubfe(key, groups.low, width);
+        f(there & __ballot(group == mine), there & __ballot(group < mine), int(key & (keys - 1)), i0 + j * 64);
+      }
+    }
+  };
+  const bool noted = share < (int64_t(1) << (32 - kKeyBits));
+  each([&](uint64_t hit, uint64_t less, int local, int i0) {
+    before += __popcll(less);
+    if (hit) {
+      const int at = own + __popcll(hit & ((uint64_t(1) << lane) - 1));
+      if (hit >> lane & 1 && at < kNotes) notes[wave][at] = unsigned(i0 + lane) << kKeyBits | unsigned(local);
+      own += __popcll(hit);
+    }
+  });
   if (lane == 0) {
     meet[wave][0] = before;
-    meet[wave][1] = all;
+    meet[wave][1] = own;
   }
   __syncthreads();
-  int base = 0, count = 0;
+  int base = 0;
+  bool fits = noted;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     base += meet[w][0];
-    count += meet[w][1];
+    fits = fits && meet[w][1] <= kNotes;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) *lists.count = count;
+  if (fits) {
+    for (int i = lane; i < own; i += 64) atomicAdd(&hist[wave][notes[wave][i] & (kKeys - 1)], 1);
+  } else {
+    each([&](uint64_t hit, uint64_t, int local, int) {
+      if (hit >> lane & 1) atomicAdd(&hist[wave][local], 1);
+    });
+  }
+  __syncthreads();
   // the places of a row's tokens: behind those of the group's rows before it, a wavefront's behind the earlier ones'
-  __shared__ int sums[kWaves];
-  int own = 0;
+  int here = 0;
   if (int(threadIdx.x) < keys)
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) own += hist[w][threadIdx.x];
-  int place = own;
+    for (int w = 0; w < kWaves; ++w) here += hist[w][threadIdx.x];
+  int place = here;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const int up = __shfl_up(place, d);
     if (lane >= d) place += up;
   }
+  const uint64_t empty = __ballot(int(threadIdx.x) < keys && here == 0 && groups.id((mine << groups.low) + threadIdx.x) < vocab);
+  if (lane == 0 && wave < groups.words()) lists.empty[mine * groups.words() + wave] = empty;
   if (lane == 63) sums[wave] = place;
   __syncthreads();
   for (int w = 0; w < wave; ++w) place += sums[w];
-  place += base - own;
+  place += base;
+  if (mine + 1 == gridDim.x && int(threadIdx.x) == keys - 1) *lists.count = place;  // all of them
+  place -= here;
   if (int(threadIdx.x) < keys)
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
@@ -245,199 +275,232 @@ __global__ __launch_bounds__(kWaves * 64) void k_group(TableGrad p, Groups group
       hist[w][threadIdx.x] = place;
       place += c;
     }
-  const bool empty = int(threadIdx.x) < keys && own == 0;
   __syncthreads();
-#pragma unroll 4
-  for (int64_t i0 = from; i0 < to; i0 += 64) {
-    const unsigned key = key_at(i0 + lane);
-    const int local = int(key & (keys - 1));
-    uint64_t left = __ballot(key != ~0u && (key >> groups.low) == mine);
+  // up to 64 tokens in their order, those of one row at a time
+  const auto put = [&](uint64_t left, int local, int token) {
+    volatile int* next = hist[wave];
     while (left) {
-      const int leader = __builtin_ctzll(left);
-      const uint64_t same = left & __ballot(local == __shfl(local, leader));
-      int at = 0;
-      if (lane == leader) at = atomicAdd(&hist[wave][local], __popcll(same));
-      at = __shfl(at, leader) + __popcll(same & ((uint64_t(1) << lane) - 1));
+      const int leader = __builtin_ctzll(left), which = __builtin_amdgcn_readlane(local, leader);
+      const uint64_t same = left & __ballot(local == which);
+      const int first = next[which];
+      if (lane == leader) next[which] = first + __popcll(same);
       if (same >> lane & 1) {
-        lists.token[at] = int(i0 + lane);
-        lists.row[at] = int(groups.id(key));
+        const int at = first + __popcll(same & ((uint64_t(1) << lane) - 1));
+        lists.token[at] = int(from) + token;
+        lists.row[at] = int(groups.id((mine << groups.low) + unsigned(which)));
       }
       left &= ~same;
     }
-  }
-  if (p.add) return;
-  // a wavefront clears the rows of its 64 threads' keys
-  uint64_t clear = __ballot(empty && groups.id((mine << groups.low) + threadIdx.x) < unsigned(p.vocab));
-  __shared__ uint64_t cleared[kWaves];
-  if (lane == 0) cleared[wave] = clear;
-  __syncthreads();
-  int turn = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    clear = cleared[w];
-    while (clear) {
-      const int k = __builtin_ctzll(clear);
-      clear &= clear - 1;
-      if (turn++ % kWaves != wave) continue;
-      O* out = static_cast<O*>(p.out) + int64_t(groups.id((mine << groups.low) + w * 64 + k)) * p.ldd;
-      const float zero[kPiece<O>] = {};
-      for (int64_t i = lane; i * kPiece<O> < p.n; i += 64) put_piece(out, i, p.n, zero);
+  };
+  if (fits) {
+#pragma unroll 1
+    for (int i = 0; i < own; i += 64) {
+      const unsigned note = notes[wave][i + lane < own ? i + lane : i];
+      put(__ballot(i + lane < own), int(note & (kKeys - 1)), int(note >> kKeyBits));
     }
+  } else {
+    each([&](uint64_t hit, uint64_t, int local, int i0) { put(hit, local, i0 + lane); });
   }
 }
 
-// scale times a row's sum, added to what is there or not
-template <class O, int E>
-__device__ inline void put_sum(const TableGrad& p, int64_t row, int64_t c, int valid, const float (&sum)[E]) {
-  O* out = static_cast<O*>(p.out) + row * p.ldd + c;
-  O e[E];
-  if (p.add) {
-    if (valid >= E) {
-      __builtin_memcpy(e, out, sizeof(e));
-    } else {
-#pragma unroll
-      for (int k = 0; k < E; ++k) e[k] = k < valid ? out[k] : O(0.0f);
+// What a run leaves: its last row begins in it and ends past the next run; all of it is one row that began before and goes on.
+constexpr int kBegins = 1, kPasses = 2;
+
+// W columns of a row of n >= W from c on: the last place is moved so far down that it ends with the row.  Two lanes of a wavefront have
+// its columns twice then, and write the same values to them.
+__device__ inline int64_t place_of(int64_t c, int64_t n, int w) { return c < n - w ? c : n - w; }
+
+// A wavefront adds up the entries of a run over 64 pieces of their rows, as many of them alike as slabs come to.  A row that begins in
+// the run and ends in the next is finished here, and left out there.  A longer one leaves its part in part row 2 r + 1 where it
+// begins and in 2 r where it goes on or ends.  The next entries' loads are on their way while a batch is added up.
+// Workgroups past the launch's `runs` clear the rows without a token, those of 64 keys each.
+template <class T, class O, bool ADD>
+__global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists lists, int64_t first_run, unsigned runs) {
+  constexpr int E = kPiece<T>, U = ADD ? 4 : 8, Q = E * int(sizeof(O)) / 16;
+  if (!ADD && blockIdx.x >= runs) {
+    const unsigned word = (blockIdx.x - runs) * gridDim.y + blockIdx.y, words = unsigned(groups.words());
+    if (word >= words << (groups.bits - groups.low)) return;
+    uint64_t left = lists.empty[word];
+    const unsigned key = (word / words << groups.low) + word % words * 64;
+    for (int turn = 0; left; ++turn) {
+      const int k = __builtin_ctzll(left);
+      left &= left - 1;
+      if (turn % 4 != __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) continue;
+      O* out = static_cast<O*>(p.out) + int64_t(groups.id(key + k)) * p.ldd;
+      constexpr int Z = kPiece<O>;
+      const int64_t pieces = (p.n + Z - 1) / Z;
+#pragma unroll 4
+      for (int64_t i = threadIdx.x & 63; i < pieces; i += 64) {
+        const u32x4 zero = {};
+        __builtin_memcpy(out + place_of(i * Z, p.n, Z), &zero, 16);
+      }
     }
-#pragma unroll
-    for (int k = 0; k < E; ++k) e[k] = O(float(e[k]) + p.scale * sum[k]);
-  } else {
-#pragma unroll
-    for (int k = 0; k < E; ++k) e[k] = O(p.scale * sum[k]);
+    return;
   }
-  if (valid >= E) {
-    __builtin_memcpy(out, e, sizeof(e));
-  } else {
-#pragma unroll
-    for (int k = 0; k < E; ++k)
-      if (k < valid) out[k] = e[k];
-  }
-}
-
-constexpr int kBegins = 1, kPasses = 2;  // state of a run: its last row goes on in the next run; all of it is one row that does and has begun before
-
-// A wavefront adds up kRun entries of the list over 64 pieces of their rows.  A row all of whose entries it has is done; one that
-// goes on leaves a part: where the run begins in part row 2 r, else in 2 r + 1.
-template <class T, class O>
-__global__ __launch_bounds__(256) void k_sum(TableGrad p, Lists lists, int64_t first) {
-  constexpr int E = kPiece<T>, U = 8;
   const int lane = threadIdx.x & 63;
-  const int64_t run = first + blockIdx.x, start = run * kRun, count = *lists.count;
+  const int64_t run = first_run + blockIdx.x, start = run * kRun, count = *lists.count;
   if (start >= count) return;
-  const int mine = int(count - start < kRun ? count - start : kRun);
-  const int row = lane < mine ? lists.row[start + lane] : -1, token = lane < mine ? lists.token[start + lane] : 0;
-  const int before = start > 0 ? lists.row[start - 1] : -1, after = start + kRun < count ? lists.row[start + kRun] : -1;
-  for (int64_t c0 = (int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 64 * E; c0 < p.n; c0 += int64_t(gridDim.y) * 4 * 64 * E) {
-    const int n = int(p.n - c0 < 64 * E ? p.n - c0 : 64 * E), valid = n - lane * E;
+  const int row = start + lane < count ? lists.row[start + lane] : -1, token = start + lane < count ? lists.token[start + lane] : 0;
+  const int before = start > 0 ? lists.row[start - 1] : -1, earlier = start > kRun ? lists.row[start - kRun - 1] : -1;
+  const int after = start + 2 * kRun < count ? lists.row[start + 2 * kRun] : -1;
+  const auto row_at = [&](int e) { return __builtin_amdgcn_readlane(row, e); };
+  const int head = row_at(0), tail = row_at(kRun - 1);
+  const bool on = tail >= 0 && tail == row_at(kRun);  // the run's last row goes on
+  const bool open = head == before, passes = open && on && head == tail, part = open && (passes || head == earlier);
+  int begin = 0, end = int(count - start < kRun ? count - start : kRun);
+  if (open && !part) begin = __builtin_ctzll(__ballot(row != head));
+  int state = passes ? kPasses : 0;
+  if (on && !passes) {
+    if (tail == row_at(2 * kRun - 1) && tail == after) {
+      state = kBegins;
+    } else {
+      const uint64_t other = __ballot(row != tail) >> kRun;
+      end = other ? kRun + __builtin_ctzll(other) : 2 * kRun;
+    }
+  }
+  // entries that are their row's last here
+  const uint64_t last = __ballot(row != __shfl_down(row, 1)) | uint64_t(1) << (end - 1);
+  if (blockIdx.y == 0 && threadIdx.x == 0) {
+    lists.state[run] = state;
+    if (state == kBegins) lists.begin[atomicAdd(lists.count + 1, 1)] = int(run);
+  }
+  const int64_t pieces = (p.n + E - 1) / E, slabs = (pieces + 63) / 64;
+  for (int64_t slab = int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); slab < slabs; slab += int64_t(gridDim.y) * 4) {
+    const int64_t p0 = pieces * slab / slabs, c0 = p0 * E;
+    const int wide = int(pieces * (slab + 1) / slabs - p0);
+    const int off = int(place_of(c0 + (lane < wide ? lane : wide - 1) * E, p.n, E) - c0);
     const T* dy = static_cast<const T*>(p.dy) + c0;
-    u32x4 c[2][U];
-    const auto load = [&](int g, u32x4 (&to)[U]) {
+    O* out = static_cast<O*>(p.out) + c0;
+    struct Batch {
+      u32x4 dy[U], old[ADD ? U : 1][Q];
+    };
+    const auto load = [&](int g, Batch& to) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (g + u < mine) to[u] = near_piece(dy + int64_t(__builtin_amdgcn_readlane(token, g + u)) * p.lddy, lane, n);
+        if (g + u < end) {
+          __builtin_memcpy(&to.dy[u], dy + int64_t(__builtin_amdgcn_readlane(token, g + u)) * p.lddy + unsigned(off), 16);
+          if constexpr (ADD)
+            if (last >> (g + u) & 1) __builtin_memcpy(to.old[u], out + int64_t(row_at(g + u)) * p.ldd + unsigned(off), sizeof(to.old[u]));
+        }
     };
     float sum[E] = {};
-    bool open = __builtin_amdgcn_readlane(row, 0) == before;
-    int state = 0;
-    const auto add = [&](int g, const u32x4 (&from)[U]) {
+    Batch now, next;
+    load(begin, now);
+#pragma unroll 1
+    for (int g = begin; g < end; g += U) {
+      load(g + U, next);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (g + u >= mine) break;
+        const int e = g + u;
+        if (e >= end) break;
         float v[E];
-        unpack<T>(from[u], v);
+        unpack<T>(now.dy[u], v);
 #pragma unroll
         for (int k = 0; k < E; ++k) sum[k] += v[k];
-        const int e = g + u, id = __builtin_amdgcn_readlane(row, e), next = e + 1 < kRun ? __builtin_amdgcn_readlane(row, e + 1) : after;
-        if (id == next) {
-          if (e + 1 < kRun) continue;
-          state = open ? kPasses : kBegins;
+        if (!(last >> e & 1)) continue;
+        const int id = row_at(e);
+        const bool to_part = (part && id == head) || (state == kBegins && e == end - 1);
+        if (lane < wide) {
+          if (to_part) {
+            __builtin_memcpy(lists.part + (2 * run + (part && id == head ? 0 : 1)) * p.n + c0 + off, sum, sizeof(sum));
+          } else {
+            O o[E];
+            if constexpr (ADD) __builtin_memcpy(o, now.old[u], sizeof(o));
+#pragma unroll
+            for (int k = 0; k < E; ++k) o[k] = O(ADD ? float(o[k]) + p.scale * sum[k] : p.scale * sum[k]);
+            __builtin_memcpy(out + int64_t(id) * p.ldd + unsigned(off), o, sizeof(o));
+          }
         }
-        if (open || state) {
-          if (valid > 0) put_vector(lists.part + (2 * run + (open ? 0 : 1)) * p.n + c0, lane, n, sum);
-        } else if (valid > 0) {
-          put_sum<O>(p, id, c0 + lane * E, valid, sum);
-        }
-        open = false;
 #pragma unroll
         for (int k = 0; k < E; ++k) sum[k] = 0.0f;
       }
-    };
-    load(0, c[0]);
-#pragma unroll
-    for (int g = 0; g < kRun; g += 2 * U) {
-      load(g + U, c[1]);
-      add(g, c[0]);
-      load(g + 2 * U, c[0]);
-      add(g + U, c[1]);
+      now = next;
     }
-    if (c0 == 0 && lane == 0) lists.state[run] = state;
   }
 }
 
-// The parts of a row that went on from run to run, added up in order: eight wavefronts a share of them each, then their sums.
+// The parts of the rows that went past two runs, added up in order: four wavefronts a share of them each, then their sums.
 template <class O>
-__global__ __launch_bounds__(512) void k_join(TableGrad p, Lists lists, int64_t first) {
-  __shared__ f32x4 sums[8][64];
+__global__ __launch_bounds__(256) void k_join(TableGrad p, Lists lists) {
+  constexpr int U = 8;
+  __shared__ f32x4 sums[3][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t run = first + blockIdx.x, count = *lists.count, runs = (count + kRun - 1) / kRun;
-  if (run >= runs || lists.state[run] != kBegins) return;
-  const int64_t row = lists.row[run * kRun + kRun - 1];
-  int64_t last = run + 1;  // the run in which the row ends
-  for (;;) {
-    const bool ends = last + lane >= runs || lists.state[last + lane] != kPasses;
-    const uint64_t which = __ballot(ends);
-    if (which) {
-      last += __builtin_ctzll(which);
-      break;
+  const int64_t runs = (*lists.count + kRun - 1) / kRun, rows = lists.count[1];
+  const int64_t pieces = (p.n + 3) / 4, slabs = (pieces + 63) / 64;
+  for (int64_t item = blockIdx.x; item < rows * slabs; item += gridDim.x) {
+    const int64_t run = lists.begin[item / slabs], slab = item % slabs, row = lists.row[run * kRun + kRun - 1];
+    int64_t last = run + 1;  // the run in which the row ends
+    for (;;) {
+      const uint64_t which = __ballot(last + lane >= runs || lists.state[last + lane] != kPasses);
+      if (which) {
+        last += __builtin_ctzll(which);
+        break;
+      }
+      last += 64;
     }
-    last += 64;
-  }
-  const int64_t parts = last - run + 1, share = (parts + 7) / 8, from = wave * share, to = from + share < parts ? from + share : parts;
-  for (int64_t c0 = int64_t(blockIdx.y) * 256; c0 < p.n; c0 += int64_t(gridDim.y) * 256) {
-    const int n = int(p.n - c0 < 256 ? p.n - c0 : 256), valid = n - lane * 4;
+    const int64_t parts = last - run + 1, share = (parts + 3) / 4, from = wave * share, to = from + share < parts ? from + share : parts;
+    const int64_t p0 = pieces * slab / slabs, wide = pieces * (slab + 1) / slabs - p0;
+    const int64_t c = place_of((p0 + (lane < wide ? lane : wide - 1)) * 4, p.n, 4);
     f32x4 sum = {};
-#pragma unroll 8
-    for (int64_t k = from; k < to; ++k) {
-      float v[4];
-      vector_of<4>(lists.part + (k == 0 ? 2 * run + 1 : 2 * (run + k)) * p.n + c0, lane, n, 0.0f, v);
+    for (int64_t k0 = from; k0 < to; k0 += U) {
+      f32x4 v[U];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sum[q] += v[q];
+      for (int u = 0; u < U; ++u)
+        if (k0 + u < to) __builtin_memcpy(&v[u], lists.part + (k0 + u == 0 ? 2 * run + 1 : 2 * (run + k0 + u)) * p.n + c, 16);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 + u < to) sum += v[u];
     }
-    sums[wave][lane] = sum;
+    if (wave > 0) sums[wave - 1][lane] = sum;
     __syncthreads();
-    if (wave == 0 && valid > 0) {
-      float v[4];
+    if (wave == 0) {
+      O* out = static_cast<O*>(p.out) + row * p.ldd + c;
+      O o[4];
+      if (p.add) __builtin_memcpy(o, out, sizeof(o));
 #pragma unroll
-      for (int w = 1; w < 8; ++w) sum += sums[w][lane];
+      for (int w = 0; w < 3; ++w) sum += sums[w][lane];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = sum[q];
-      put_sum<O>(p, row, c0 + lane * 4, valid, v);
+      for (int k = 0; k < 4; ++k) o[k] = O(p.add ? float(o[k]) + p.scale * sum[k] : p.scale * sum[k]);
+      if (lane < wide) __builtin_memcpy(out, o, sizeof(o));
     }
     __syncthreads();
   }
 }
 
 constexpr int64_t kFewTokens = 256;
-inline bool scans(int64_t t, int64_t vocab) { return t <= kFewTokens || vocab > (int64_t(1) << 22); }
+inline bool scans(int64_t t, int64_t vocab, int64_t n) { return t <= kFewTokens || vocab > (int64_t(1) << kMostBits) || n < 8; }
+
+template <class T, class O, bool ADD>
+void launch_sums(const TableGrad& p, const Groups& groups, const Lists& lists, hipStream_t st) {
+  const int64_t runs = (p.t + kRun - 1) / kRun, most = int64_t(1) << 19;
+  const int64_t slabs = ((p.n + kPiece<T> - 1) / kPiece<T> + 63) / 64, four = (slabs + 3) / 4, high = four < 8 ? four : 8;
+  for (int64_t first = 0; first < runs; first += most) {
+    const int64_t here = runs - first < most ? runs - first : most;
+    const int64_t clear = ADD || first ? 0 : (groups.count() * groups.words() + high - 1) / high;
+    k_sum<T, O, ADD><<<dim3(unsigned(here + clear), unsigned(high)), 256, 0, st>>>(p, groups, lists, first, unsigned(here));
+  }
+  if (runs > 2) {
+    const int64_t items = (runs - 2) * ((p.n + 255) / 256);
+    k_join<O><<<unsigned(items < 2048 ? items : 2048), 256, 0, st>>>(p, lists);
+  }
+}
 
 template <class T, class O>
 int launch_grad(const TableGrad& p, void* workspace, hipStream_t st) {
-  if (scans(p.t, p.vocab)) {
+  if (scans(p.t, p.vocab, p.n)) {
     const int64_t items = (p.vocab + 3) / 4 * ((p.n + 64 * kPiece<T> - 1) / (64 * kPiece<T>)), most = 1 << 20;
     k_scan<T, O><<<unsigned(items < most ? items : most), 256, 0, st>>>(p);
     return launched();
   }
-  const Lists lists = carve(workspace, p.t, p.n);
   const Groups groups = groups_of(p.vocab);
-  k_group<O><<<unsigned(groups.count()), kWaves * 64, 0, st>>>(p, groups, lists);
-  const int64_t runs = (p.t + kRun - 1) / kRun, wide = int64_t(1) << 20;
-  const auto slabs = [&](int64_t of, int64_t most) {
-    const int64_t all = (p.n + of - 1) / of;
-    return unsigned(all < most ? all : most);
-  };
-  const unsigned y = slabs(4 * 64 * kPiece<T>, 8), z = slabs(256, 8);
-  for (int64_t first = 0; first < runs; first += wide)
-    k_sum<T, O><<<dim3(unsigned(runs - first < wide ? runs - first : wide), y), 256, 0, st>>>(p, lists, first);
-  for (int64_t first = 0; first < runs - 1; first += wide / 2)
-    k_join<O><<<dim3(unsigned(runs - first < wide / 2 ? runs - first : wide / 2), z), 512, 0, st>>>(p, lists, first);
+  const Lists lists = carve(workspace, p.t, groups, p.n);
+  const unsigned vocab = unsigned(p.vocab), padding = p.padding >= 0 && p.padding < p.vocab ? unsigned(p.padding) : ~0u;
+  const unsigned grid = unsigned(groups.count());
+  k_group<<<grid, kWaves * 64, 0, st>>>(p.ids, p.t, vocab, padding, groups, lists);
+  if (p.add)
+    launch_sums<T, O, true>(p, groups, lists, st);
+  else
+    launch_sums<T, O, false>(p, groups, lists, st);
   return launched();
 }
 
@@ -460,8 +523,8 @@ int xmem_embedding_forward(const void* d_table, int64_t ldt, const int64_t* d_id
 }
 
 size_t xmem_embedding_backward_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width) {
-  if (!sizes_ok(tokens, vocab, width) || scans(tokens, vocab)) return 0;
-  return carve(nullptr, tokens, width).bytes;
+  if (!sizes_ok(tokens, vocab, width) || scans(tokens, vocab, width)) return 0;
+  return carve(nullptr, tokens, groups_of(vocab), width).bytes;
 }
 
 int xmem_embedding_backward(const void* d_dy, int64_t lddy, const int64_t* d_ids, int64_t tokens, int64_t vocab, int64_t width,
