@@ -30,22 +30,23 @@ __device__ inline float gate_of(float g, int act) {
   return act == XMEM_GATE_NONE ? g : act == XMEM_GATE_SIGMOID ? logistic(g) : g * logistic(g);
 }
 
-// alpha s a(g) ((h - mu) rho w + b), piece by piece.
+// alpha s a(g) ((h - mu) rho w + b) of a piece; `vector` reads a vector's part of it.
 template <class T>
 struct Branch {
   static constexpr int E = kPiece<T>;
   const Norms& p;
   float mu, rho;
-  __device__ void of(u32x4 h, u32x4 g, int64_t i, float (&v)[E]) const {
+  template <class Vector>
+  __device__ void of(u32x4 h, u32x4 g, const Vector& vector, float (&v)[E]) const {
     float w[E], b[E], s[E];
     unpack<T>(h, v);
     if (p.post != XMEM_NORM_NONE) {
-      vector_of<E>(p.w1, i, p.n, 1.0f, w);
-      vector_of<E>(p.b1, i, p.n, 0.0f, b);
+      vector(p.w1, 1.0f, w);
+      vector(p.b1, 0.0f, b);
 #pragma unroll
       for (int k = 0; k < E; ++k) v[k] = (v[k] - mu) * rho * w[k] + b[k];
     }
-    vector_of<E>(p.s, i, p.n, 1.0f, s);
+    vector(p.s, 1.0f, s);
 #pragma unroll
     for (int k = 0; k < E; ++k) v[k] *= p.alpha * s[k];
     if (p.gate) {
@@ -57,118 +58,98 @@ struct Branch {
   }
 };
 
-template <int E>
-__device__ inline float squares(const float (&v)[E], float mu, int64_t valid) {
-  float s = 0.0f;
-  if (valid >= E) {
-#pragma unroll
-    for (int k = 0; k < E; ++k) s += (v[k] - mu) * (v[k] - mu);
-  } else {
-#pragma unroll
-    for (int k = 0; k < E; ++k) s += k < valid ? (v[k] - mu) * (v[k] - mu) : 0.0f;
-  }
-  return s;
-}
-template <int E>
-__device__ inline float total(const float (&v)[E]) {
-  float s = v[0];
-#pragma unroll
-  for (int k = 1; k < E; ++k) s += v[k];
-  return s;
-}
-
-// Mean and reciprocal deviation of a row: `each(f)` calls f with every piece of the thread and the row's elements from it on.
-template <int THREADS, class Each>
-__device__ inline void moments(RowSums<THREADS>& sums, const Each& each, int kind, int64_t n, float eps, float& mu, float& rho) {
+// Mean and reciprocal deviation of a row: `each(f)` gives the sum of f(x) over the thread's elements of it.
+template <class Sums, class Each>
+__device__ inline void moments(Sums& sums, const Each& each, int kind, int64_t n, float eps, float& mu, float& rho) {
   mu = 0.0f;
   rho = 0.0f;
   if (kind == XMEM_NORM_NONE) return;
-  float s = 0.0f;
-  if (kind == XMEM_NORM_LAYER) {
-    each([&](const auto& v, int64_t) { s += total(v); });
-    mu = sums.one(s) / float(n);
-    s = 0.0f;
-  }
-  each([&](const auto& v, int64_t valid) { s += squares(v, mu, valid); });
-  rho = 1.0f / sqrtf(sums.one(s) / float(n) + eps);
+  if (kind == XMEM_NORM_LAYER) mu = sums.one(each([](float x) { return x; })) / float(n);
+  rho = 1.0f / sqrtf(sums.one(each([&](float x) { return (x - mu) * (x - mu); })) / float(n) + eps);
 }
 
-template <int THREADS>
-constexpr int kBlock = THREADS < 256 ? 256 : THREADS;
-
-// THREADS of a row (64: four rows a workgroup), NCH pieces of it in each thread's registers.
-template <class T, int THREADS, int NCH>
-__global__ __launch_bounds__(kBlock<THREADS>) void k_norm(Norms p) {
-  constexpr int E = kPiece<T>;
-  __shared__ typename RowSums<THREADS>::Meet meet;
-  RowSums<THREADS> sums(meet);
-  const int tid = threadIdx.x % THREADS;
-  const int64_t t = p.first + (THREADS < 256 ? int64_t(blockIdx.x) * (256 / THREADS) + threadIdx.x / THREADS : int64_t(blockIdx.x));
-  if (t >= p.t) return;  // a whole wavefront, of those that do not meet others
-  const int64_t n = p.n;
-  const int pieces = int((n + E - 1) / E);
-  const T* r = static_cast<const T*>(p.r) + t * p.ldr;
+// W threads of a row, with NCH pieces of it in each thread's registers; as many rows a workgroup as make 256 threads.
+template <class T, int W, int NCH>
+__global__ __launch_bounds__(W < 256 ? 256 : W) void k_norm(Norms p) {
+  constexpr int E = kPiece<T>, R = W < 256 ? 256 / W : 1;
+  __shared__ typename RowSums<W, R>::Meet meet;
+  const int slot = W < kWave ? threadIdx.x / W : __builtin_amdgcn_readfirstlane(threadIdx.x / W), tid = threadIdx.x % W;
+  RowSums<W, R> sums(meet, slot);
+  const int64_t t = p.first + int64_t(blockIdx.x) * R + slot, at = t < p.t ? t : p.t - 1;
+  const bool here = t < p.t;  // a row that is not there is the last one again, and not written
+  const int n = int(p.n), pieces = (n + E - 1) / E;
+  const auto place = [&](int j) { return Place<E>(j * W + tid, n); };
+  const auto row = [&](const void* x, int64_t ld, int j) { return piece_at(static_cast<const T*>(x) + at * ld, place(j).at); };
+  const auto put = [&](void* x, int64_t ld, int j, const float (&v)[E]) {
+    if (here) put_piece_at(static_cast<T*>(x) + at * ld, place(j).at, v);
+  };
+  // over the thread's elements of pieces that `piece` gives
+  const auto total = [&](const auto& piece, const auto& f) {
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j)
+      if (j * W < pieces) {
+        float v[E];
+        piece(j, v);
+#pragma unroll
+        for (int k = 0; k < E; ++k) v[k] = f(v[k]);
+        place(j).counted(v);
+#pragma unroll
+        for (int k = 0; k < E; ++k) s += v[k];
+      }
+    return s;
+  };
   float x[NCH][E], mu1 = 0.0f, rho1 = 0.0f, mu2, rho2;
   u32x4 cr[NCH];
 #pragma unroll
   for (int j = 0; j < NCH; ++j)
-    if (j * THREADS < pieces) cr[j] = piece_of(r, j * THREADS + tid, n);
+    if (j * W < pieces) cr[j] = row(p.r, p.ldr, j);
   if (p.h) {
-    const T* h = static_cast<const T*>(p.h) + t * p.ldh;
-    const T* g = p.gate ? static_cast<const T*>(p.gate) + t * p.ldg : nullptr;
     u32x4 ch[NCH], cg[NCH];
 #pragma unroll
     for (int j = 0; j < NCH; ++j)
-      if (j * THREADS < pieces) {
-        ch[j] = piece_of(h, j * THREADS + tid, n);
-        if (g) cg[j] = piece_of(g, j * THREADS + tid, n);
+      if (j * W < pieces) {
+        ch[j] = row(p.h, p.ldh, j);
+        if (p.gate) cg[j] = row(p.gate, p.ldg, j);
       }
-    moments<THREADS>(sums, [&](const auto& f) {
-#pragma unroll
-      for (int j = 0; j < NCH; ++j)
-        if (j * THREADS < pieces) {
-          float v[E];
-          unpack<T>(ch[j], v);
-          f(v, n - int64_t(j * THREADS + tid) * E);
-        }
-    }, p.post, n, p.eps, mu1, rho1);
+    const auto piece = [&](int j, float (&v)[E]) { unpack<T>(ch[j], v); };
+    moments(sums, [&](const auto& f) { return total(piece, f); }, p.post, n, p.eps, mu1, rho1);
+    // elements that two wavefronts have are read by both before one writes them
+    if (W > kWave && p.post == XMEM_NORM_NONE && p.out == p.r) __syncthreads();
     const Branch<T> branch{p, mu1, rho1};
-    T* out = static_cast<T*>(p.out) + t * p.ldo;
 #pragma unroll
     for (int j = 0; j < NCH; ++j)
-      if (j * THREADS < pieces) {
+      if (j * W < pieces) {
         float v[E];
-        branch.of(ch[j], cg[j], j * THREADS + tid, v);
+        branch.of(ch[j], cg[j], [&](const float* w, float without, float (&to)[E]) { vector_at(w, place(j).at, without, to); }, v);
         unpack<T>(cr[j], x[j]);
-        const int64_t valid = n - int64_t(j * THREADS + tid) * E;
 #pragma unroll
-        for (int k = 0; k < E; ++k) x[j][k] = k < valid ? x[j][k] + v[k] : 0.0f;
-        put_piece(out, j * THREADS + tid, n, x[j]);
+        for (int k = 0; k < E; ++k) x[j][k] += v[k];
+        put(p.out, p.ldo, j, x[j]);
       }
   } else {
 #pragma unroll
     for (int j = 0; j < NCH; ++j)
-      if (j * THREADS < pieces) unpack<T>(cr[j], x[j]);
+      if (j * W < pieces) unpack<T>(cr[j], x[j]);
   }
-  moments<THREADS>(sums, [&](const auto& f) {
+  const auto piece = [&](int j, float (&v)[E]) {
 #pragma unroll
-    for (int j = 0; j < NCH; ++j)
-      if (j * THREADS < pieces) f(x[j], n - int64_t(j * THREADS + tid) * E);
-  }, p.pre, n, p.eps, mu2, rho2);
+    for (int k = 0; k < E; ++k) v[k] = x[j][k];
+  };
+  moments(sums, [&](const auto& f) { return total(piece, f); }, p.pre, n, p.eps, mu2, rho2);
   if (p.y) {
-    T* y = static_cast<T*>(p.y) + t * p.ldy;
 #pragma unroll
     for (int j = 0; j < NCH; ++j)
-      if (j * THREADS < pieces) {
+      if (j * W < pieces) {
         float w[E], b[E];
-        vector_of<E>(p.w2, j * THREADS + tid, n, 1.0f, w);
-        vector_of<E>(p.b2, j * THREADS + tid, n, 0.0f, b);
+        vector_at(p.w2, place(j).at, 1.0f, w);
+        vector_at(p.b2, place(j).at, 0.0f, b);
 #pragma unroll
         for (int k = 0; k < E; ++k) x[j][k] = (x[j][k] - mu2) * rho2 * w[k] + b[k];
-        put_piece(y, j * THREADS + tid, n, x[j]);
+        put(p.y, p.ldy, j, x[j]);
       }
   }
-  if (p.stats && tid == 0) {
+  if (p.stats && tid == 0 && here) {
     p.stats[t] = mu1;
     p.stats[p.t + t] = rho1;
     p.stats[2 * p.t + t] = mu2;
@@ -176,9 +157,9 @@ __global__ __launch_bounds__(kBlock<THREADS>) void k_norm(Norms p) {
   }
 }
 
-// A row that no registers hold: its inputs are read again for each sum, and outputs written last (out may be r).
+// A row that no registers hold, or of less than a piece: its inputs are read again for each sum, and outputs written last (out may be r).
 template <class T>
-__global__ __launch_bounds__(1024) void k_norm_long(Norms p) {
+__global__ __launch_bounds__(1024) void k_norm_any(Norms p) {
   constexpr int E = kPiece<T>, THREADS = 1024;
   __shared__ typename RowSums<THREADS>::Meet meet;
   RowSums<THREADS> sums(meet);
@@ -187,30 +168,30 @@ __global__ __launch_bounds__(1024) void k_norm_long(Norms p) {
   const T* h = p.h ? static_cast<const T*>(p.h) + t * p.ldh : nullptr;
   const T* g = p.gate ? static_cast<const T*>(p.gate) + t * p.ldg : nullptr;
   float mu1, rho1, mu2, rho2;
-  moments<THREADS>(sums, [&](const auto& f) {
+  const auto total = [&](const auto& piece, const auto& f) {
+    float s = 0.0f;
     for (int64_t i = threadIdx.x; i < pieces; i += THREADS) {
       float v[E];
-      unpack<T>(piece_of(h, i, n), v);
-      f(v, n - i * E);
+      piece(i, v);
+#pragma unroll
+      for (int k = 0; k < E; ++k) s += i * E + k < n ? f(v[k]) : 0.0f;
     }
-  }, h ? p.post : XMEM_NORM_NONE, n, p.eps, mu1, rho1);
+    return s;
+  };
+  const auto block = [&](int64_t i, float (&v)[E]) { unpack<T>(piece_of(h, i, n), v); };
+  moments(sums, [&](const auto& f) { return total(block, f); }, h ? p.post : XMEM_NORM_NONE, n, p.eps, mu1, rho1);
   const Branch<T> branch{p, mu1, rho1};
   const auto sum = [&](int64_t i, float (&x)[E]) {
     unpack<T>(piece_of(r, i, n), x);
     if (h) {
       float v[E];
-      branch.of(piece_of(h, i, n), g ? piece_of(g, i, n) : u32x4{}, i, v);
+      branch.of(piece_of(h, i, n), g ? piece_of(g, i, n) : u32x4{},
+                [&](const float* w, float without, float (&to)[E]) { vector_of<E>(w, i, n, without, to); }, v);
 #pragma unroll
-      for (int k = 0; k < E; ++k) x[k] = i * E + k < n ? x[k] + v[k] : 0.0f;
+      for (int k = 0; k < E; ++k) x[k] += v[k];
     }
   };
-  moments<THREADS>(sums, [&](const auto& f) {
-    for (int64_t i = threadIdx.x; i < pieces; i += THREADS) {
-      float x[E];
-      sum(i, x);
-      f(x, n - i * E);
-    }
-  }, p.pre, n, p.eps, mu2, rho2);
+  moments(sums, [&](const auto& f) { return total(sum, f); }, p.pre, n, p.eps, mu2, rho2);
   for (int64_t i = threadIdx.x; i < pieces; i += THREADS) {
     float x[E], w[E], b[E];
     sum(i, x);
@@ -241,17 +222,25 @@ int launch_rows(Kernel kernel, Norms p, int per, int block, hipStream_t st) {
   return launched();
 }
 
+template <class T, int W, int NCH>
+int launch_norm(const Norms& p, hipStream_t st) {
+  return launch_rows(k_norm<T, W, NCH>, p, W < 256 ? 256 / W : 1, W < 256 ? 256 : W, st);
+}
 template <class T>
 int launch_norm(const Norms& p, hipStream_t st) {
   const int64_t pieces = (p.n + kPiece<T> - 1) / kPiece<T>;
-  if (pieces <= 64) return launch_rows(k_norm<T, 64, 1>, p, 4, 256, st);
-  if (pieces <= 64 * 2) return launch_rows(k_norm<T, 64, 2>, p, 4, 256, st);
-  if (pieces <= 64 * 4) return launch_rows(k_norm<T, 64, 4>, p, 4, 256, st);
-  if (pieces <= 256 * 2) return launch_rows(k_norm<T, 256, 2>, p, 1, 256, st);
-  if (pieces <= 256 * 4) return launch_rows(k_norm<T, 256, 4>, p, 1, 256, st);
-  if (pieces <= 1024 * 2) return launch_rows(k_norm<T, 1024, 2>, p, 1, 1024, st);
-  if (pieces <= 1024 * 4) return launch_rows(k_norm<T, 1024, 4>, p, 1, 1024, st);
-  return launch_rows(k_norm_long<T>, p, 1, 1024, st);
+  if (p.n < kPiece<T>) return launch_rows(k_norm_any<T>, p, 1, 1024, st);
+  if (pieces <= 8) return launch_norm<T, 8, 1>(p, st);
+  if (pieces <= 16) return launch_norm<T, 16, 1>(p, st);
+  if (pieces <= 32) return launch_norm<T, 32, 1>(p, st);
+  if (pieces <= 64) return launch_norm<T, 64, 1>(p, st);
+  if (pieces <= 128) return launch_norm<T, 128, 1>(p, st);
+  if (pieces <= 256) return launch_norm<T, 256, 1>(p, st);
+  if (pieces <= 512) return launch_norm<T, 256, 2>(p, st);
+  if (pieces <= 1024) return launch_norm<T, 256, 4>(p, st);
+  if (pieces <= 2048) return launch_norm<T, 1024, 2>(p, st);
+  if (pieces <= 4096) return launch_norm<T, 1024, 4>(p, st);
+  return launch_rows(k_norm_any<T>, p, 1, 1024, st);
 }
 
 // ------------------------------------------------------------------ gradients
@@ -287,15 +276,11 @@ struct Piece {
       hat[k] = (hat[k] - mu2) * rho2;
     }
   }
-  // dr from dout, e, xhat2 and the means of e and e xhat2, where `valid` elements are the row's; 0 behind them
-  __device__ void grad(u32x4 cdout, const float (&e)[E], const float (&hat)[E], float mean_e, float mean_eh, int64_t valid,
-                       float (&d)[E]) const {
+  // dr from dout, e, xhat2 and the means of e and e xhat2
+  __device__ void grad(u32x4 cdout, const float (&e)[E], const float (&hat)[E], float mean_e, float mean_eh, float (&d)[E]) const {
     unpack<T>(cdout, d);
 #pragma unroll
     for (int k = 0; k < E; ++k) d[k] += rho2 * (e[k] - mean_e - hat[k] * mean_eh);
-    if (valid < E)
-#pragma unroll
-      for (int k = 0; k < E; ++k) d[k] = k < valid ? d[k] : 0.0f;
   }
   // from d = dr and s = alpha scale: b = d a(g), xhat1, f = s b w1 and dgate
   __device__ void second(u32x4 ch, u32x4 cg, const float (&d)[E], const float (&s)[E], const float (&w1)[E], const float (&b1)[E],
@@ -331,43 +316,46 @@ __device__ inline float column_of(const NormGrads& p, int q, int64_t c) {
   return q == 0 ? p.alpha * (p.s ? p.s[c] : 1.0f) : q == 1 ? (p.w1 ? p.w1[c] : 1.0f) : q == 2 ? (p.w2 ? p.w2[c] : 1.0f) : (p.b1 ? p.b1[c] : 0.0f);
 }
 
-// BLOCK / W rows at a time, W threads and NCH pieces a thread each, whose columns' sums over all of the workgroup's rows stay
-// in registers (with NCH of 2, those of B and D in LDS).
+// BLOCK / W rows at a time, W threads and NCH pieces a thread each, whose columns' sums over all of the workgroup's rows stay in
+// registers, half of them in LDS where they are four vectors', and all where a thread has more than eight columns of two.  The vectors are in LDS where they fit (VLDS).  With more than a piece a thread,
+// what the first norm does not need is loaded after its sums.
 template <class T, int W, int NCH, bool BIASES, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void k_norm_back(NormGrads p) {
-  constexpr int E = kPiece<T>, R = BLOCK / W, HELD = NCH == 1 && BIASES ? 4 : 2, VECTORS = BIASES ? 4 : 3;
-  constexpr bool APART = BIASES && HELD == 2;  // B and D in LDS
+  constexpr int E = kPiece<T>, R = BLOCK / W, VECTORS = BIASES ? 4 : 3;
+  constexpr bool VLDS = NCH == 1, LATE = NCH > 1, APART = BIASES ? W < 1024 || NCH > 1 : NCH * E > 8;
+  constexpr int HELD = BIASES ? APART ? 2 : 4 : APART ? 0 : 2;
+  constexpr int ROWS = BLOCK / kWave * (W < kWave ? W : kWave) * E, COLUMNS = VLDS ? VECTORS * W * E : 0;  // floats
   __shared__ typename RowSums<W, R>::Meet meet;
-  __shared__ float apart[APART ? 2 : 1][APART ? NCH * E : 1][APART ? BLOCK : 1], rows[R > 1 ? E : 1][R > 1 ? BLOCK : 1];
-  __shared__ f32x4 columns[NCH == 1 ? VECTORS : 1][NCH == 1 ? E / 4 : 1][NCH == 1 ? W : 1];
-  const int slot = __builtin_amdgcn_readfirstlane(threadIdx.x / W), tid = threadIdx.x % W;
+  __shared__ float apart[APART ? 2 : 1][APART ? NCH * E : 1][APART ? BLOCK : 1];
+  __shared__ __attribute__((aligned(16))) float shared[R > 1 && ROWS > COLUMNS ? ROWS : COLUMNS > 4 ? COLUMNS : 4];  // vectors, then rows' sums
+  const int slot = W < kWave ? threadIdx.x / W : __builtin_amdgcn_readfirstlane(threadIdx.x / W), tid = threadIdx.x % W;
   RowSums<W, R> sums(meet, slot);
   const int n = int(p.n), pieces = (n + E - 1) / E;
-  if constexpr (NCH == 1) {
-    for (int i = threadIdx.x; i < VECTORS * W * E; i += BLOCK) {
+  const auto place = [&](int j) { return Place<E>(j * W + tid, n); };
+  if constexpr (VLDS) {  // [vector][half of a piece][thread of the row][4]
+    for (int i = threadIdx.x; i < COLUMNS; i += BLOCK) {
       const int q = i / (W * E), c = i % (W * E);
-      reinterpret_cast<float*>(&columns[q][c % E / 4][c / E])[c % 4] = c < n ? column_of(p, q, c) : 0.0f;
+      shared[((q * (E / 4) + c % E / 4) * W + c / E) * 4 + c % 4] = column_of(p, q, Place<E>(c / E, n).at + c % E);
     }
     __syncthreads();
   }
   const auto vector = [&](int q, int j, float (&v)[E]) {
-    if constexpr (NCH == 1) {
-      if (q < VECTORS) {
+    if constexpr (VLDS) {
 #pragma unroll
-        for (int h = 0; h < E / 4; ++h) __builtin_memcpy(v + 4 * h, &columns[q][h][tid], 16);
-      } else {
+      for (int h = 0; h < E / 4; ++h) {
+        f32x4 part = {};
+        if (q < VECTORS) part = *reinterpret_cast<const f32x4*>(shared + ((q * (E / 4) + h) * W + tid) * 4);
 #pragma unroll
-        for (int k = 0; k < E; ++k) v[k] = 0.0f;
+        for (int k = 0; k < 4; ++k) v[4 * h + k] = part[k];
       }
     } else {
+      vector_at(q == 0 ? p.s : q == 1 ? p.w1 : q == 2 ? p.w2 : BIASES ? p.b1 : nullptr, place(j).at, q == 3 ? 0.0f : 1.0f, v);
+      if (q == 0)
 #pragma unroll
-      for (int k = 0; k < E; ++k) {
-        const int c = (j * W + tid) * E + k;
-        v[k] = q < VECTORS ? column_of(p, q, c < n ? c : n - 1) : 0.0f;
-      }
+        for (int k = 0; k < E; ++k) v[k] *= p.alpha;
     }
   };
-  float acc[HELD][NCH][E] = {};  // A, B, C, D or A, C
+  float acc[HELD ? HELD : 1][NCH][E] = {};  // A, B, C, D or A, C
   if constexpr (APART)
 #pragma unroll
     for (int q = 0; q < 2; ++q)
@@ -376,9 +364,9 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(NormGrads p) {
   const auto add = [&](int q, int j, int k, float v) {  // q: 0 to 3 for A to D
     if constexpr (HELD == 4)
       acc[q][j][k] += v;
-    else if constexpr (!BIASES)
+    else if constexpr (!APART)
       acc[q / 2][j][k] += v;
-    else if (q & 1)
+    else if (!BIASES || (q & 1))
       apart[q / 2][j * E + k][threadIdx.x] += v;
     else
       acc[q / 2][j][k] += v;
@@ -387,12 +375,16 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(NormGrads p) {
     const int64_t t = t0 + slot, at = t < p.t ? t : 0;
     const bool here = t < p.t;  // a row that is not there is one of 0, and not written
     const auto row = [&](const void* x, int64_t ld, int j) {
-      return here ? near_piece(static_cast<const T*>(x) + at * ld, j * W + tid, n) : u32x4{};
+      return here ? piece_at(static_cast<const T*>(x) + at * ld, place(j).at) : u32x4{};
     };
     const auto put = [&](void* x, int64_t ld, int j, const float (&v)[E]) {
-      if (here) put_piece(static_cast<T*>(x) + at * ld, j * W + tid, n, v);
+      if (here) put_piece_at(static_cast<T*>(x) + at * ld, place(j).at, v);
     };
     u32x4 cdy[NCH], cdo[NCH], co[NCH], ch[NCH], cg[NCH];
+    const auto rest = [&](int j) {
+      if (p.h) ch[j] = row(p.h, p.ldh, j);
+      if (p.gate) cg[j] = row(p.gate, p.ldg, j);
+    };
 #pragma unroll
     for (int j = 0; j < NCH; ++j)
       if (j * W < pieces) {
@@ -401,13 +393,14 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(NormGrads p) {
           co[j] = row(p.out, p.ldo, j);
         }
         cdo[j] = p.dout ? row(p.dout, p.lddo, j) : u32x4{};
-        if (p.h) ch[j] = row(p.h, p.ldh, j);
-        if (p.gate) cg[j] = row(p.gate, p.ldg, j);
+        if (!LATE) rest(j);
       }
+    // elements that two wavefronts have are read by both before one writes them
+    if (W > kWave && !p.dy && p.dr == p.dout) __syncthreads();
     const Piece<T> q{p, p.stats[at], p.stats[p.t + at], p.stats[2 * p.t + at], p.stats[3 * p.t + at]};
-    float d[NCH][E];
+    float s1 = 0.0f, s2 = 0.0f;
     if (p.dy) {
-      float s1 = 0.0f, s2 = 0.0f, e[E], hat[E], dy[E], w[E];
+      float e[E], hat[E], dy[E], w[E];
 #pragma unroll
       for (int j = 0; j < NCH; ++j)
         if (j * W < pieces) {
@@ -415,10 +408,14 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(NormGrads p) {
           q.first(cdy[j], co[j], w, e, hat, dy);
 #pragma unroll
           for (int k = 0; k < E; ++k) {
-            s1 += e[k] * hat[k];
-            s2 += e[k];
             add(2, j, k, dy[k] * hat[k]);
             if (BIASES) add(3, j, k, dy[k]);
+          }
+          place(j).counted(e);
+#pragma unroll
+          for (int k = 0; k < E; ++k) {
+            s1 += e[k] * hat[k];
+            s2 += e[k];
           }
         }
       if (p.pre == XMEM_NORM_LAYER)
@@ -427,61 +424,63 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(NormGrads p) {
         s1 = sums.one(s1), s2 = 0.0f;
       s1 /= float(n);
       s2 /= float(n);
-#pragma unroll
-      for (int j = 0; j < NCH; ++j)
-        if (j * W < pieces) {
-          vector(2, j, w);
-          q.first(cdy[j], co[j], w, e, hat, dy);
-          q.grad(cdo[j], e, hat, s2, s1, n - (j * W + tid) * E, d[j]);
-        }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NCH; ++j)
-        if (j * W < pieces) unpack<T>(cdo[j], d[j]);
     }
-#pragma unroll
-    for (int j = 0; j < NCH; ++j)
-      if (j * W < pieces) put(p.dr, p.lddr, j, d[j]);
-    if (!p.h) continue;
-    float s1 = 0.0f, s2 = 0.0f, b[E], hat[E], f[E], dg[E], s[E], w1[E], b1[E];
+    float f[NCH][E], s3 = 0.0f, s4 = 0.0f;
 #pragma unroll
     for (int j = 0; j < NCH; ++j)
       if (j * W < pieces) {
+        float e[E], hat[E], d[E], w[E], b[E], dg[E], s[E], w1[E], b1[E];
+        if (LATE) rest(j);
+        if (p.dy) {
+          vector(2, j, w);
+          q.first(cdy[j], co[j], w, e, hat, d);
+          q.grad(cdo[j], e, hat, s2, s1, d);
+        } else {
+          unpack<T>(cdo[j], d);
+        }
+        put(p.dr, p.lddr, j, d);
+        if (!p.h) continue;
         vector(0, j, s);
         vector(1, j, w1);
         vector(3, j, b1);
-        q.second(ch[j], cg[j], d[j], s, w1, b1, b, hat, f, dg);
+        q.second(ch[j], cg[j], d, s, w1, b1, b, hat, f[j], dg);
         if (p.dg) put(p.dg, p.lddg, j, dg);
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-          s1 += f[k] * hat[k];
-          s2 += f[k];
           add(0, j, k, b[k] * hat[k]);
           if (BIASES) add(1, j, k, b[k]);
-          d[j][k] = f[k];
+          b[k] = f[j][k];
+        }
+        place(j).counted(b);
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          s3 += b[k] * hat[k];
+          s4 += b[k];
         }
       }
+    if (!p.h) continue;
     if (p.post != XMEM_NORM_NONE) {
       if (p.post == XMEM_NORM_LAYER)
-        sums.two(s1, s2);
+        sums.two(s3, s4);
       else
-        s1 = sums.one(s1), s2 = 0.0f;
-      s1 /= float(n);
-      s2 /= float(n);
+        s3 = sums.one(s3), s4 = 0.0f;
+      s3 /= float(n);
+      s4 /= float(n);
     }
 #pragma unroll
     for (int j = 0; j < NCH; ++j)
       if (j * W < pieces) {
         if (p.post != XMEM_NORM_NONE) {
+          float hat[E];
           unpack<T>(ch[j], hat);
 #pragma unroll
-          for (int k = 0; k < E; ++k) d[j][k] = q.rho1 * (d[j][k] - s2 - (hat[k] - q.mu1) * q.rho1 * s1);
+          for (int k = 0; k < E; ++k) f[j][k] = q.rho1 * (f[j][k] - s4 - (hat[k] - q.mu1) * q.rho1 * s3);
         }
-        put(p.dh, p.lddh, j, d[j]);
+        put(p.dh, p.lddh, j, f[j]);
       }
   }
   if (!p.part) return;
-  // the workgroup's rows, then its part of each sum
+  // the rows' sums, then the workgroup's part of each
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     if (!BIASES && (q & 1)) continue;
@@ -491,29 +490,36 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(NormGrads p) {
 #pragma unroll
       for (int k = 0; k < E; ++k) {
         if constexpr (APART)
-          v[k] = q & 1 ? apart[q / 2][j * E + k][threadIdx.x] : acc[q / 2][j][k];
+          v[k] = !BIASES || (q & 1) ? apart[q / 2][j * E + k][threadIdx.x] : acc[HELD ? q / 2 : 0][j][k];
         else
           v[k] = acc[HELD == 4 ? q : q / 2][j][k];
       }
       if constexpr (R > 1) {
-        __syncthreads();
+        constexpr int V = W < kWave ? W : kWave, PARTS = BLOCK / (W < kWave ? kWave : W);  // lanes that meet, wavefronts of one column
 #pragma unroll
-        for (int k = 0; k < E; ++k) rows[k][threadIdx.x] = v[k];
+        for (int d = W; d < kWave; d *= 2)
+#pragma unroll
+          for (int k = 0; k < E; ++k) v[k] += __shfl_xor(v[k], d);
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         __syncthreads();
-        if (slot == 0)
+        if (lane < V)
+#pragma unroll
+          for (int k = 0; k < E; ++k) shared[(k * (BLOCK / kWave) + wave) * V + lane] = v[k];
+        __syncthreads();
+        if (threadIdx.x < W)
 #pragma unroll
           for (int k = 0; k < E; ++k)
 #pragma unroll
-            for (int w = 1; w < R; ++w) v[k] += rows[k][w * W + tid];
+            for (int w = 1; w < PARTS; ++w) v[k] += shared[(k * (BLOCK / kWave) + w * RowSums<W, R>::kParts + wave) * V + lane];
       }
-      if (slot == 0) put_vector(p.part + (int64_t(q) * gridDim.x + blockIdx.x) * n, j * W + tid, n, v);
+      if (threadIdx.x < W && j * W < pieces) __builtin_memcpy(p.part + (int64_t(q) * gridDim.x + blockIdx.x) * n + place(j).at, v, sizeof(v));
     }
   }
 }
 
-// Rows that no registers hold: each is read three times, and a workgroup's sums are kept where its parts go.
+// Rows that no registers hold, or of less than a piece: each is read three times, and a workgroup's sums are kept where its parts go.
 template <class T>
-__global__ __launch_bounds__(1024) void k_norm_back_long(NormGrads p) {
+__global__ __launch_bounds__(1024) void k_norm_back_any(NormGrads p) {
   constexpr int E = kPiece<T>, THREADS = 1024;
   __shared__ typename RowSums<THREADS>::Meet meet;
   RowSums<THREADS> sums(meet);
@@ -523,8 +529,10 @@ __global__ __launch_bounds__(1024) void k_norm_back_long(NormGrads p) {
       return x ? piece_of(static_cast<const T*>(x) + t * ld, i, n) : u32x4{};
     };
     const auto vector = [&](int q, int64_t i, float (&v)[E]) {
+      vector_of<E>(q == 0 ? p.s : q == 1 ? p.w1 : q == 2 ? p.w2 : p.b1, i, n, q == 3 ? 0.0f : 1.0f, v);
+      if (q == 0)
 #pragma unroll
-      for (int k = 0; k < E; ++k) v[k] = column_of(p, q, i * E + k < n ? i * E + k : n - 1);
+        for (int k = 0; k < E; ++k) v[k] *= p.alpha;
     };
     const Piece<T> q{p, p.stats[t], p.stats[p.t + t], p.stats[2 * p.t + t], p.stats[3 * p.t + t]};
     float s1 = 0.0f, s2 = 0.0f, s3 = 0.0f, s4 = 0.0f, e[E], hat[E], dy[E], d[E], b[E], f[E], dg[E], s[E], w[E], add[E];
@@ -546,7 +554,7 @@ __global__ __launch_bounds__(1024) void k_norm_back_long(NormGrads p) {
       if (p.dy) {
         vector(2, i, w);
         q.first(row(p.dy, p.lddy, i), row(p.out, p.ldo, i), w, e, hat, dy);
-        q.grad(row(p.dout, p.lddo, i), e, hat, s2, s1, n - i * E, d);
+        q.grad(row(p.dout, p.lddo, i), e, hat, s2, s1, d);
       } else {
         unpack<T>(row(p.dout, p.lddo, i), d);
       }
@@ -563,6 +571,7 @@ __global__ __launch_bounds__(1024) void k_norm_back_long(NormGrads p) {
         second(i);
 #pragma unroll
         for (int k = 0; k < E; ++k) {
+          if (i * E + k >= n) f[k] = 0.0f;
           s3 += f[k] * hat[k];
           s4 += f[k];
         }
@@ -612,26 +621,37 @@ struct VectorGrads {
   float *ds, *dw1, *db1, *dw2, *db2;
 };
 
-// The groups' parts added up in a fixed order: sixteen wavefronts a share of the groups each, then their sums.
+// The groups' parts added up in a fixed order: sixteen columns a workgroup, whose 64 shares take every 64th group each.
 __global__ __launch_bounds__(1024) void k_norm_sums(VectorGrads p) {
-  __shared__ float sums[16][4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ float sums[4][16][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = threadIdx.x & 15;
   const bool wanted[4] = {p.ds || p.dw1, p.db1 || (p.ds && p.b1), p.dw2 != nullptr, p.db2 != nullptr};
-  for (int64_t c = int64_t(blockIdx.x) * 64 + lane; c - lane < p.n; c += int64_t(gridDim.x) * 64) {
+  for (int64_t c0 = int64_t(blockIdx.x) * 16; c0 < p.n; c0 += int64_t(gridDim.x) * 16) {
+    const int64_t c = c0 + col < p.n ? c0 + col : p.n - 1;
     float v[4] = {};
-    if (c < p.n)
+    for (int64_t g0 = threadIdx.x >> 4; g0 < p.groups; g0 += 4 * 64) {
+      float x[4][4];
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (wanted[q])
-#pragma unroll 8
-          for (int64_t g = wave; g < p.groups; g += 16) v[q] += p.part[(q * p.groups + g) * p.n + c];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) sums[wave][q][lane] = v[q];
+        for (int u = 0; u < 4; ++u) x[q][u] = wanted[q] && g0 + 64 * u < p.groups ? p.part[(q * p.groups + g0 + 64 * u) * p.n + c] : 0.0f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[q] += x[q][u];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v[q] += __shfl_xor(v[q], 16);
+      v[q] += __shfl_xor(v[q], 32);
+      if (lane < 16) sums[q][wave][lane] = v[q];
+    }
     __syncthreads();
-    if (wave == 0 && c < p.n) {
+    if (threadIdx.x < 16 && c0 + col < p.n) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        for (int w = 1; w < 16; ++w) v[q] += sums[w][q][lane];
+#pragma unroll
+        for (int w = 1; w < 16; ++w) v[q] += sums[q][w][col];
       const float s = p.alpha * (p.s ? p.s[c] : 1.0f);
       if (p.ds) p.ds[c] = p.alpha * ((p.w1 ? p.w1[c] : 1.0f) * v[0] + (p.b1 ? p.b1[c] * v[1] : 0.0f));
       if (p.dw1) p.dw1[c] = s * v[0];
@@ -644,7 +664,7 @@ __global__ __launch_bounds__(1024) void k_norm_sums(VectorGrads p) {
 }
 
 // How rows are taken: threads of a row and pieces a thread (0: read again), and how many groups of sums there are.
-constexpr int kBackBlock = 1024;
+template <int W> constexpr int kBackBlock = W <= 512 ? 512 : 1024;
 struct Plan {
   int threads, nch;
   int64_t groups;
@@ -652,31 +672,40 @@ struct Plan {
 Plan plan_of(int64_t t, int64_t n, int dtype) {
   const int e = dtype == XMEM_F32 ? 4 : 8;
   const int64_t pieces = (n + e - 1) / e;
-  Plan q{64, 1, 0};
-  while (q.threads < kBackBlock && q.threads < pieces) q.threads *= 2;
-  if (pieces > kBackBlock) q.nch = pieces <= 2 * kBackBlock ? 2 : 0;
-  const int per = kBackBlock / q.threads;
+  Plan q{8, 1, 0};
+  while (q.threads < 1024 && q.threads < pieces) q.threads *= 2;
+  if (n < e)
+    q.threads = 1024, q.nch = 0;
+  else if (pieces > 1024)
+    q.nch = pieces <= 2 * 1024 ? 2 : e == 4 && pieces <= 4 * 1024 ? 4 : 0;
+  const int block = q.threads <= 512 ? 512 : 1024, per = block / q.threads;
   const int64_t rows = (t + per - 1) / per;
-  int64_t most = kCus;
+  int64_t most = kCus * 1024 / block;
   if (q.nch == 0) {  // parts of 256 MiB at most, or one group's
     const int64_t fit = (int64_t(1) << 24) / n;
     most = fit < 1 ? 1 : fit < most ? fit : most;
   }
-  q.groups = rows < most ? rows : most;
+  q.groups = rows < 2 * most ? (rows + 1) / 2 : most;  // two rounds at least: a part a round would be as much to write as the rows
   return q;
 }
 
 template <class T, int W, int NCH>
 void launch_back(const NormGrads& p, const Plan& q, hipStream_t st) {
   if (p.biases)
-    k_norm_back<T, W, NCH, true, kBackBlock><<<unsigned(q.groups), kBackBlock, 0, st>>>(p);
+    k_norm_back<T, W, NCH, true, kBackBlock<W>><<<unsigned(q.groups), kBackBlock<W>, 0, st>>>(p);
   else
-    k_norm_back<T, W, NCH, false, kBackBlock><<<unsigned(q.groups), kBackBlock, 0, st>>>(p);
+    k_norm_back<T, W, NCH, false, kBackBlock<W>><<<unsigned(q.groups), kBackBlock<W>, 0, st>>>(p);
 }
 template <class T>
 int launch_backward(const NormGrads& p, const Plan& q, hipStream_t st) {
   if (q.nch == 0)
-    k_norm_back_long<T><<<unsigned(q.groups), 1024, 0, st>>>(p);
+    k_norm_back_any<T><<<unsigned(q.groups), 1024, 0, st>>>(p);
+  else if (q.threads == 8)
+    launch_back<T, 8, 1>(p, q, st);
+  else if (q.threads == 16)
+    launch_back<T, 16, 1>(p, q, st);
+  else if (q.threads == 32)
+    launch_back<T, 32, 1>(p, q, st);
   else if (q.threads == 64)
     launch_back<T, 64, 1>(p, q, st);
   else if (q.threads == 128)
@@ -687,8 +716,10 @@ int launch_backward(const NormGrads& p, const Plan& q, hipStream_t st) {
     launch_back<T, 512, 1>(p, q, st);
   else if (q.nch == 1)
     launch_back<T, 1024, 1>(p, q, st);
-  else
+  else if (q.nch == 2)
     launch_back<T, 1024, 2>(p, q, st);
+  else if constexpr (sizeof(T) == 4)
+    launch_back<T, 1024, 4>(p, q, st);
   return launched();
 }
 
@@ -767,7 +798,7 @@ int xmem_residual_norm_backward(const void* d_dy, int64_t lddy, const void* d_do
   }
   if (sums) {
     const VectorGrads v{part, d_scale, d_w1, d_b1, tokens > 0 ? q.groups : 0, width, alpha, d_dscale, d_dw1, d_db1, d_dw2, d_db2};
-    const int64_t blocks = (width + 63) / 64;
+    const int64_t blocks = (width + 15) / 16;
     k_norm_sums<<<unsigned(blocks < 65536 ? blocks : 65536), 1024, 0, st>>>(v);
   }
   return launched();

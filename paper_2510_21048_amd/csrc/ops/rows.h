@@ -24,28 +24,39 @@ __device__ inline u32x4 piece_of(const T* x, int64_t i, int64_t n) {
   return c;
 }
 
-// The same for rows of less than 2^28 elements that begin at a place the wavefront shares: one load whatever the row's end is,
-// the last piece's from the row's last 16 bytes, moved down.
-template <class T>
-__device__ inline u32x4 near_piece(const T* x, int i, int n) {
-  constexpr int E = kPiece<T>;
-  u32x4 c;
-  if (n < E) {
-    T e[E];
+// Where piece i of a row of n >= E elements is read and written: at i * E, but not past n - E.  The first `over` of its elements (all,
+// where it is not smaller than E) are then other threads' too, which have the same values for them; they do not count in sums.
+template <int E>
+struct Place {
+  int at, over;
+  __device__ Place(int i, int n) : at(i * E < n - E ? i * E : n - E), over(i * E - at) {}
+  __device__ void counted(float (&v)[E]) const {
+    if (over > 0)
 #pragma unroll
-    for (int k = 0; k < E; ++k) e[k] = i == 0 && k < n ? x[k] : T(0.0f);
-    __builtin_memcpy(&c, e, 16);
-    return c;
+      for (int k = 0; k < E; ++k) v[k] = k < over ? 0.0f : v[k];
   }
-  const int from = i * E < n - E ? i * E : n - E, over = i * E - from;
-  __builtin_memcpy(&c, reinterpret_cast<const char*>(x) + unsigned(from) * unsigned(sizeof(T)), 16);
-  if (over > 0) {
-    unsigned __int128 all = 0;
-    __builtin_memcpy(&all, &c, 16);
-    all = over < E ? all >> (over * int(sizeof(T)) * 8) : 0;
-    __builtin_memcpy(&c, &all, 16);
-  }
+};
+template <class T>
+__device__ inline u32x4 piece_at(const T* x, int at) {
+  u32x4 c;
+  __builtin_memcpy(&c, reinterpret_cast<const char*>(x) + unsigned(at) * unsigned(sizeof(T)), 16);
   return c;
+}
+template <class T>
+__device__ inline void put_piece_at(T* x, int at, const float (&v)[kPiece<T>]) {
+  T e[kPiece<T>];
+#pragma unroll
+  for (int k = 0; k < kPiece<T>; ++k) e[k] = T(v[k]);
+  __builtin_memcpy(reinterpret_cast<char*>(x) + unsigned(at) * unsigned(sizeof(T)), e, 16);
+}
+template <int E>
+__device__ inline void vector_at(const float* w, int at, float without, float (&v)[E]) {
+  if (w) {
+    __builtin_memcpy(v, reinterpret_cast<const char*>(w) + unsigned(at) * 4u, sizeof(v));
+  } else {
+#pragma unroll
+    for (int k = 0; k < E; ++k) v[k] = without;
+  }
 }
 
 template <class T>
@@ -108,26 +119,45 @@ __device__ inline float wave_total(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
-// Sums over the W threads of a row, one of R rows of a workgroup: a wavefront by itself, or wavefronts whose sums meet in LDS.  Two
-// places take turns: who writes one again has passed the other's barrier, before which every wavefront has read it.
+// The sum over each W neighbouring lanes, in all of them.
+template <int W>
+__device__ inline float lanes_total(float v) {
+  if constexpr (W == kWave) {
+    return wave_total(v);
+  } else {
+    if constexpr (W > 1) v += from_lane<0xb1, 0xf>(v);   // the other of a pair
+    if constexpr (W > 2) v += from_lane<0x4e, 0xf>(v);   // the other pair of four
+    if constexpr (W > 4) v += from_lane<0x141, 0xf>(v);  // the other half of eight
+    if constexpr (W > 8) v += from_lane<0x140, 0xf>(v);  // of sixteen
+    if constexpr (W > 16) v += __shfl_xor(v, 16);
+    return v;
+  }
+}
+
+// Sums over the W threads of a row, one of R rows of a workgroup: in a wavefront by themselves, or in wavefronts whose sums meet in
+// LDS.  Two places take turns: who writes one again has passed the other's barrier, before which every wavefront has read it.
 template <int W, int R = 1>
 struct RowSums {
-  typedef float Meet[2][2][R * W / kWave];
+  static constexpr int kParts = W > kWave ? W / kWave : 1;  // wavefronts of a row
+  typedef float Meet[2][2][R * kParts];
   Meet& meet;
   int slot, turn = 0;
   __device__ explicit RowSums(Meet& m, int slot = 0) : meet(m), slot(slot) {}
 
   __device__ float gather(int which) const {
-    const float* at = meet[turn][which] + slot * (W / kWave);
+    const float* at = meet[turn][which] + slot * kParts;
     float v = at[0];
 #pragma unroll
-    for (int i = 1; i < W / kWave; ++i) v += at[i];
+    for (int i = 1; i < kParts; ++i) v += at[i];
     return v;
   }
   __device__ void two(float& a, float& b) {
-    a = wave_total(a);
-    b = wave_total(b);
-    if constexpr (W > kWave) {
+    if constexpr (W <= kWave) {
+      a = lanes_total<W>(a);
+      b = lanes_total<W>(b);
+    } else {
+      a = wave_total(a);
+      b = wave_total(b);
       if ((threadIdx.x & 63) == 0) {
         meet[turn][0][threadIdx.x >> 6] = a;
         meet[turn][1][threadIdx.x >> 6] = b;
@@ -139,8 +169,10 @@ struct RowSums {
     }
   }
   __device__ float one(float a) {
-    a = wave_total(a);
-    if constexpr (W > kWave) {
+    if constexpr (W <= kWave) {
+      a = lanes_total<W>(a);
+    } else {
+      a = wave_total(a);
       if ((threadIdx.x & 63) == 0) meet[turn][0][threadIdx.x >> 6] = a;
       __syncthreads();
       a = gather(0);
