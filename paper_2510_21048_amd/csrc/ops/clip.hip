@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kTable = 128;          // gradients of a launch: two a lane
 constexpr int kThreads = 256;
-constexpr int kParts = 1024;         // workgroups of a norm, each with a sum of its own
+constexpr int kParts = 2048;         // workgroups of a norm at most, each with a sum of its own
 constexpr int kLoads = 4;            // of 16 bytes, a thread and piece of work
 constexpr int kSpan = kThreads * kLoads * 16;  // bytes of a piece of work
 constexpr int64_t kMostSize = int64_t(1) << 48;
@@ -156,8 +156,7 @@ __global__ __launch_bounds__(kThreads) void k_scale(Table t, const double* part,
   const float f = factor_of(part, parts, max_norm, scale, stats);
   if (f == 1.0f) return;
   const Finder find(t);
-  const int64_t all = t.first[t.count];
-  for (int64_t w = blockIdx.x; w < all; w += gridDim.x) {
+  for (int64_t w = t.first[t.count] - 1 - blockIdx.x; w >= 0; w -= gridDim.x) {
     const int i = find.of(w);
     if (t.type[i] == XMEM_BF16)
       scale_of<bf16>(t, i, w, f);
@@ -172,19 +171,22 @@ __global__ __launch_bounds__(kThreads) void k_stats(const double* part, int part
   factor_of(part, parts, INFINITY, scale, stats);
 }
 
-// The next launch's gradients from the list's `at`-th on; empty ones are left out.
-Table table_of(void* const* tensors, const int64_t* sizes, const int* dtypes, int64_t count, int64_t& at) {
+int64_t pieces_of(const void* at, int64_t size, int dtype) {
+  return (int64_t(reinterpret_cast<uintptr_t>(at) & 15) + size * bytes_of(dtype) + kSpan - 1) / kSpan;
+}
+
+// A launch's gradients, from the list's `at`-th on; empty ones are left out.
+Table table_of(void* const* tensors, const int64_t* sizes, const int* dtypes, int64_t count, int64_t at) {
   Table t;
   t.count = 0;
   t.first[0] = 0;
   for (; at < count && t.count < kTable; ++at) {
     if (sizes[at] == 0) continue;
     const int i = t.count++;
-    const int64_t head = int64_t(reinterpret_cast<uintptr_t>(tensors[at]) & 15);
     t.at[i] = tensors[at];
     t.size[i] = sizes[at];
     t.type[i] = static_cast<unsigned char>(dtypes[at]);
-    t.first[i + 1] = t.first[i] + (head + sizes[at] * bytes_of(dtypes[at]) + kSpan - 1) / kSpan;
+    t.first[i + 1] = t.first[i] + pieces_of(tensors[at], sizes[at], dtypes[at]);
   }
   return t;
 }
@@ -219,32 +221,40 @@ int xmem_clip_grad_norm(void* const* d_tensors, const int64_t* sizes, const int*
         reinterpret_cast<uintptr_t>(d_tensors[i]) % bytes_of(dtypes[i]))
       return XMEM_EINVAL;
   const bool writes = max_norm != INFINITY || scale != 1.0f;
+  struct Launch {
+    int64_t start, pieces;  // its first gradient, its pieces of work
+  };
+  std::vector<Launch> launches;
+  int64_t parts = 1;
   try {
     if (writes && overlap(d_tensors, sizes, dtypes, count)) return XMEM_EINVAL;
-  } catch (...) {  // no memory for the list of ranges
+    for (int64_t at = 0; at < count || launches.empty();) {
+      Launch next{at, 0};
+      for (int taken = 0; at < count && taken < kTable; ++at)
+        if (sizes[at] > 0) {
+          next.pieces += pieces_of(d_tensors[at], sizes[at], dtypes[at]);
+          ++taken;
+        }
+      launches.push_back(next);
+      parts = std::max(parts, std::min(next.pieces, int64_t(kParts)));
+    }
+  } catch (...) {  // no memory on the host
     return XMEM_EINVAL;
   }
   if (!d_workspace || workspace_bytes < xmem_clip_grad_norm_workspace_bytes() || !aligned(d_workspace, 256)) return XMEM_EWORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   double* part = static_cast<double*>(d_workspace);
-  int64_t at = 0;
-  bool first = true;
-  do {
-    const Table t = table_of(d_tensors, sizes, dtypes, count, at);
-    k_squares<<<kParts, kThreads, 0, st>>>(t, first, part);
-    first = false;
-  } while (at < count);
+  const auto table = [&](size_t i) { return table_of(d_tensors, sizes, dtypes, count, launches[i].start); };
+  for (size_t i = 0; i < launches.size(); ++i) k_squares<<<unsigned(parts), kThreads, 0, st>>>(table(i), i == 0, part);
   if (!writes) {
-    k_stats<<<1, kThreads, 0, st>>>(part, kParts, scale, d_stats);
+    k_stats<<<1, kThreads, 0, st>>>(part, int(parts), scale, d_stats);
     return launched();
   }
-  at = 0;
-  first = true;
-  do {
-    const Table t = table_of(d_tensors, sizes, dtypes, count, at);
-    k_scale<<<2 * kParts, kThreads, 0, st>>>(t, part, kParts, max_norm, scale, first ? d_stats : nullptr);
-    first = false;
-  } while (at < count);
+  // the last gradients first, which the caches may still hold
+  for (size_t i = launches.size(); i-- > 0;) {
+    const int64_t grid = std::max(int64_t(1), std::min(launches[i].pieces, int64_t(kParts)));
+    k_scale<<<unsigned(grid), kThreads, 0, st>>>(table(i), part, int(parts), max_norm, scale, i == 0 ? d_stats : nullptr);
+  }
   return launched();
 }
 

@@ -10,9 +10,10 @@ recorded, and what a call overwrites counts as modified.
 from __future__ import annotations
 
 import ctypes
+from array import array
 
 from .binding import XmemError, _ptr
-from .ops import _ANY, XMEM_F32, _check, _dtype, _matrix, _on, _vector, _workspace, _written, load_ops
+from .ops import _ANY, XMEM_F32, _check, _dtype, _dtypes, _matrix, _on, _vector, _workspace, _written, load_ops
 
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 GATES = {"none": 0, "sigmoid": 1, "silu": 2}
@@ -86,6 +87,10 @@ def _gate(name: str) -> int:
     return GATES[name]
 
 
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
 def _no(what: str, why: str, *given) -> None:
     for t in given:
         if t is not None:
@@ -101,7 +106,7 @@ def residual_norm_forward(residual, h=None, gate=None, scale=None, alpha: float 
     gate itself, "sigmoid", "silu").  Without h, y is the norm of residual.  Returns (out, which is residual itself with in_place or
     without h; y, or None with pre "none"; stats float32 [4, t] where save_stats (what ``residual_norm_backward`` needs), else None)."""
     import torch
-    load_ops()
+    lib = load_ops()
     code, dt, dev, ldr = _dtype(residual, "residual", _ANY), residual.dtype, residual.device, _matrix(residual, "residual")
     t, n = residual.shape
     k1, k2, act = _norm(post, "post"), _norm(pre, "pre"), _gate(gate_activation)
@@ -125,8 +130,9 @@ def residual_norm_forward(residual, h=None, gate=None, scale=None, alpha: float 
         out, ldo = (residual, ldr) if in_place or h is None else (residual.new_empty((t, n)), n)
         y = residual.new_empty((t, n)) if k2 else None
         stats = torch.empty((4, t), dtype=torch.float32, device=dev) if save_stats else None
-        _check(xmem_residual_norm_forward(residual, ldr, h, ldh, gate, ldg, scale, alpha, k1, post_weight, post_bias, k2, pre_weight, pre_bias,
-                                          act, eps, t, n, code, None if h is None else out, ldo, y, n, stats, on.raw),
+        _check(lib.xmem_residual_norm_forward(residual.data_ptr(), ldr, _at(h), ldh, _at(gate), ldg, _at(scale), alpha, k1, _at(post_weight),
+                                              _at(post_bias), k2, _at(pre_weight), _at(pre_bias), act, eps, t, n, code,
+                                              None if h is None else out.data_ptr(), ldo, _at(y), n, _at(stats), on.raw),
                "xmem_residual_norm_forward")
         if out is residual and h is not None:
             _written(residual)
@@ -141,7 +147,7 @@ def residual_norm_backward(dy, dout, out, stats, h=None, gate=None, scale=None, 
     in_place; h; gate; scale; post_weight; post_bias; pre_weight; pre_bias), None in the place of what was not given, and of the five
     vectors without need_vectors."""
     import torch
-    load_ops()
+    lib = load_ops()
     k1, k2, act = _norm(post, "post"), _norm(pre, "pre"), _gate(gate_activation)
     if (dy is None) == (k2 != 0):
         raise XmemError("dy: wanted with a norm before the next block, and only then")
@@ -180,10 +186,11 @@ def residual_norm_backward(dy, dout, out, stats, h=None, gate=None, scale=None, 
         dg = None if gate is None else first.new_empty((t, n))
         sums = [None if v is None or not need_vectors else torch.empty(n, dtype=torch.float32, device=dev) for v in vectors]
         wanted = any(v is not None for v in sums)
-        workspace, size = _workspace(workspace, xmem_residual_norm_backward_workspace_bytes(t, n, code) if wanted else 0, dev)
-        _check(xmem_residual_norm_backward(dy, lddy, dout, lddo, out if dy is not None else None, ldo, stats, h, ldh, gate, ldg, scale, alpha,
-                                           k1, post_weight, post_bias, k2, pre_weight, act, t, n, code, dr, lddr, dh, n, dg, n, *sums,
-                                           workspace, size, on.raw), "xmem_residual_norm_backward")
+        workspace, size = _workspace(workspace, lib.xmem_residual_norm_backward_workspace_bytes(t, n, code) if wanted else 0, dev)
+        _check(lib.xmem_residual_norm_backward(_at(dy), lddy, _at(dout), lddo, None if dy is None else out.data_ptr(), ldo, stats.data_ptr(),
+                                               _at(h), ldh, _at(gate), ldg, _at(scale), alpha, k1, _at(post_weight), _at(post_bias), k2,
+                                               _at(pre_weight), act, t, n, code, dr.data_ptr(), lddr, _at(dh), n, _at(dg), n, *map(_at, sums),
+                                               _at(workspace), size, on.raw), "xmem_residual_norm_backward")
         if in_place:
             _written(dout)
         return on.out(dr, dh, dg, *sums)
@@ -238,21 +245,25 @@ def clip_grad_norm(grads, max_norm: float, scale: float = 1.0, workspace=None, s
     transpose of one that is), None among them left out.  Returns float32 [2]: norm and factor, on the device.  max_norm = math.inf
     with scale 1 computes the norm alone."""
     import torch
-    load_ops()
+    lib = load_ops()
     grads = [g for g in grads if g is not None]
     if not grads:
         raise XmemError("grads: at least one tensor is wanted")
     dev = grads[0].device
-    kinds = []
+    where = dev.index if dev.type == "cuda" else None
+    try:
+        kinds = [_dtypes[g.dtype] for g in grads]
+    except KeyError as e:
+        raise XmemError(f"grads: {e.args[0]} is not supported here") from None
     for g in grads:
-        kinds.append(_dtype(g, "grads", _ANY))
-        if not g.is_cuda or g.device != dev or not (g.is_contiguous() or (g.dim() > 1 and g.mT.is_contiguous())):
+        if g.get_device() != where or not (g.is_contiguous() or (g.dim() > 1 and g.mT.is_contiguous())):
             raise XmemError(f"grads: contiguous tensors on one GPU are wanted, got strides {g.stride()} on {g.device}")
+    at, sizes, kinds = array("Q", [g.data_ptr() for g in grads]), array("q", [g.numel() for g in grads]), array("i", kinds)
     with _on(dev, stream, *grads, workspace) as on:
         stats = torch.empty(2, dtype=torch.float32, device=dev)
-        workspace, size = _workspace(workspace, xmem_clip_grad_norm_workspace_bytes(), dev)
-        _check(xmem_clip_grad_norm(grads, [g.numel() for g in grads], kinds, len(grads), max_norm, scale, stats, workspace, size, on.raw),
-               "xmem_clip_grad_norm")
+        workspace, size = _workspace(workspace, lib.xmem_clip_grad_norm_workspace_bytes(), dev)
+        _check(lib.xmem_clip_grad_norm(at.buffer_info()[0], sizes.buffer_info()[0], kinds.buffer_info()[0], len(grads), max_norm, scale,
+                                       stats.data_ptr(), workspace.data_ptr(), size, on.raw), "xmem_clip_grad_norm")
         if max_norm != float("inf") or scale != 1.0:
             _written(grads)
         return on.out(stats)
