@@ -134,7 +134,6 @@ __global__ __launch_bounds__(256) void k_scan(TableGrad p) {
 
 // Rows are spread over groups of kKeys or fewer by a multiplication: key = id * mul mod 2^bits, of which the upper bits are
 // the group, so that frequent tokens (whose numbers are often neighbours) do not meet in one.
-constexpr int kMostBits = 22;  // of a key: products of 24 bits
 constexpr int kGroups = 256, kKeyBits = 10, kKeys = 1 << kKeyBits, kWaves = 16;
 constexpr int kNotes = 1024;  // of a wavefront
 constexpr int kRun = 16;  // entries of the sorted list that one wavefront adds up
@@ -142,11 +141,11 @@ constexpr int kRun = 16;  // entries of the sorted list that one wavefront adds 
 struct Groups {
   int bits, low;  // of a key, and of its place in the group
   unsigned mul, inverse;
-  int64_t count() const { return int64_t(1) << (bits - low); }
+  __host__ __device__ int64_t count() const { return int64_t(1) << (bits - low); }
   __host__ __device__ int words() const { return low > 6 ? 1 << (low - 6) : 1; }  // of 64 keys, in a group
   __host__ __device__ unsigned mask() const { return (1u << bits) - 1; }
-  __device__ unsigned key(unsigned id) const { return __umul24(id, mul) & mask(); }
-  __device__ unsigned id(unsigned key) const { return __umul24(key, inverse) & mask(); }
+  __device__ unsigned key(unsigned id) const { return id * mul & mask(); }
+  __device__ unsigned id(unsigned key) const { return key * inverse & mask(); }
 };
 Groups groups_of(int64_t vocab) {
   Groups g{0, 0, 0, 0};
@@ -154,7 +153,6 @@ Groups groups_of(int64_t vocab) {
   g.mul = unsigned(0.6180339887 * double(int64_t(1) << g.bits)) | 1;
   g.inverse = 1;
   for (int i = 0; i < 5; ++i) g.inverse *= 2 - g.mul * g.inverse;  // twice the bits a step
-  g.inverse &= g.mask();
   while ((int64_t(1) << (g.bits - g.low)) > kGroups && (1 << g.low) < kKeys) ++g.low;
   return g;
 }
@@ -196,7 +194,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64
   __shared__ unsigned notes[kWaves][kNotes];  // place in the group, and the token's number in the wavefront's share
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int keys = 1 << groups.low;
-  const unsigned mine = blockIdx.x, mask = groups.mask(), width = groups.bits - groups.low;
+  const unsigned mine = blockIdx.x, width = groups.bits - groups.low;
   for (int i = threadIdx.x; i < kWaves * keys; i += kWaves * 64) hist[i >> groups.low][i & (keys - 1)] = 0;
   if (blockIdx.x == 0 && threadIdx.x == 0) lists.count[1] = 0;
   const int64_t share = ((t + kWaves - 1) / kWaves + 63) / 64 * 64, from = wave * share < t ? wave * share : t;
@@ -213,7 +211,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64
       for (int j = 0; j < kBatch; ++j) id[j] = ids[i0 + j * 64 + lane < n ? i0 + j * 64 + lane : 0];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const unsigned low = unsigned(id[j]), high = unsigned(id[j] >> 32), key = __umul24(low, groups.mul) & mask;
+        const unsigned low = unsigned(id[j]), high = unsigned(id[j] >> 32), key = groups.key(low);
         const uint64_t there = __ballot(high == 0) & __ballot(low < vocab) & __ballot(low != padding) & __ballot(i0 + j * 64 + lane < n);
         const unsigned group = __builtin_amdgcn_ubfe(key, groups.low, width);
         f(there & __ballot(group == mine), there & __ballot(group < mine), int(key & (keys - 1)), i0 + j * 64);
@@ -313,26 +311,29 @@ __device__ inline int64_t place_of(int64_t c, int64_t n, int w) { return c < n -
 // A wavefront adds up the entries of a run over 64 pieces of their rows, as many of them alike as slabs come to.  A row that begins in
 // the run and ends in the next is finished here, and left out there.  A longer one leaves its part in part row 2 r + 1 where it
 // begins and in 2 r where it goes on or ends.  The next entries' loads are on their way while a batch is added up.
-// Workgroups past the launch's `runs` clear the rows without a token, those of 64 keys each.
-template <class T, class O, bool ADD>
+// Workgroups past the launch's `runs` clear the rows without a token, those of 64 keys at a time.
+// E: elements of a piece, one where rows have fewer than eight.
+template <class T, class O, bool ADD, int E>
 __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists lists, int64_t first_run, unsigned runs) {
-  constexpr int E = kPiece<T>, U = ADD ? 4 : 8, Q = E * int(sizeof(O)) / 16;
+  constexpr int U = ADD ? 4 : 8;
   if (!ADD && blockIdx.x >= runs) {
-    const unsigned word = (blockIdx.x - runs) * gridDim.y + blockIdx.y, words = unsigned(groups.words());
-    if (word >= words << (groups.bits - groups.low)) return;
-    uint64_t left = lists.empty[word];
-    const unsigned key = (word / words << groups.low) + word % words * 64;
-    for (int turn = 0; left; ++turn) {
-      const int k = __builtin_ctzll(left);
-      left &= left - 1;
-      if (turn % 4 != __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) continue;
-      O* out = static_cast<O*>(p.out) + int64_t(groups.id(key + k)) * p.ldd;
-      constexpr int Z = kPiece<O>;
-      const int64_t pieces = (p.n + Z - 1) / Z;
+    const unsigned words = unsigned(groups.words());
+    const int64_t all = groups.count() * words, step = int64_t(gridDim.x - runs) * gridDim.y;
+    for (int64_t word = int64_t(blockIdx.x - runs) * gridDim.y + blockIdx.y; word < all; word += step) {
+      uint64_t left = lists.empty[word];
+      const unsigned key = (unsigned(word / words) << groups.low) + unsigned(word % words) * 64;
+      for (int turn = 0; left; ++turn) {
+        const int k = __builtin_ctzll(left);
+        left &= left - 1;
+        if (turn % 4 != __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) continue;
+        O* out = static_cast<O*>(p.out) + int64_t(groups.id(key + k)) * p.ldd;
+        constexpr int Z = E == 1 ? 1 : kPiece<O>;
+        const int64_t pieces = (p.n + Z - 1) / Z;
 #pragma unroll 4
-      for (int64_t i = threadIdx.x & 63; i < pieces; i += 64) {
-        const u32x4 zero = {};
-        __builtin_memcpy(out + place_of(i * Z, p.n, Z), &zero, 16);
+        for (int64_t i = threadIdx.x & 63; i < pieces; i += 64) {
+          const u32x4 zero = {};
+          __builtin_memcpy(out + place_of(i * Z, p.n, Z), &zero, Z * sizeof(O));
+        }
       }
     }
     return;
@@ -372,13 +373,14 @@ __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists l
     const T* dy = static_cast<const T*>(p.dy) + c0;
     O* out = static_cast<O*>(p.out) + c0;
     struct Batch {
-      u32x4 dy[U], old[ADD ? U : 1][Q];
+      T dy[U][E];
+      O old[ADD ? U : 1][E];
     };
     const auto load = [&](int g, Batch& to) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (g + u < end) {
-          __builtin_memcpy(&to.dy[u], dy + int64_t(__builtin_amdgcn_readlane(token, g + u)) * p.lddy + unsigned(off), 16);
+          __builtin_memcpy(to.dy[u], dy + int64_t(__builtin_amdgcn_readlane(token, g + u)) * p.lddy + unsigned(off), sizeof(to.dy[u]));
           if constexpr (ADD)
             if (last >> (g + u) & 1) __builtin_memcpy(to.old[u], out + int64_t(row_at(g + u)) * p.ldd + unsigned(off), sizeof(to.old[u]));
         }
@@ -393,10 +395,8 @@ __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists l
       for (int u = 0; u < U; ++u) {
         const int e = g + u;
         if (e >= end) break;
-        float v[E];
-        unpack<T>(now.dy[u], v);
 #pragma unroll
-        for (int k = 0; k < E; ++k) sum[k] += v[k];
+        for (int k = 0; k < E; ++k) sum[k] += float(now.dy[u][k]);
         if (!(last >> e & 1)) continue;
         const int id = row_at(e);
         const bool to_part = (part && id == head) || (state == kBegins && e == end - 1);
@@ -405,9 +405,8 @@ __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists l
             __builtin_memcpy(lists.part + (2 * run + (part && id == head ? 0 : 1)) * p.n + c0 + off, sum, sizeof(sum));
           } else {
             O o[E];
-            if constexpr (ADD) __builtin_memcpy(o, now.old[u], sizeof(o));
 #pragma unroll
-            for (int k = 0; k < E; ++k) o[k] = O(ADD ? float(o[k]) + p.scale * sum[k] : p.scale * sum[k]);
+            for (int k = 0; k < E; ++k) o[k] = O(ADD ? float(now.old[ADD ? u : 0][k]) + p.scale * sum[k] : p.scale * sum[k]);
             __builtin_memcpy(out + int64_t(id) * p.ldd + unsigned(off), o, sizeof(o));
           }
         }
@@ -420,13 +419,13 @@ __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists l
 }
 
 // The parts of the rows that went past two runs, added up in order: four wavefronts a share of them each, then their sums.
-template <class O>
+template <class O, int E>
 __global__ __launch_bounds__(256) void k_join(TableGrad p, Lists lists) {
   constexpr int U = 8;
-  __shared__ f32x4 sums[3][64];
+  __shared__ __attribute__((aligned(16))) float sums[3][64][E];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t runs = (*lists.count + kRun - 1) / kRun, rows = lists.count[1];
-  const int64_t pieces = (p.n + 3) / 4, slabs = (pieces + 63) / 64;
+  const int64_t pieces = (p.n + E - 1) / E, slabs = (pieces + 63) / 64;
   for (int64_t item = blockIdx.x; item < rows * slabs; item += gridDim.x) {
     const int64_t run = lists.begin[item / slabs], slab = item % slabs, row = lists.row[run * kRun + kRun - 1];
     int64_t last = run + 1;  // the run in which the row ends
@@ -440,27 +439,31 @@ __global__ __launch_bounds__(256) void k_join(TableGrad p, Lists lists) {
     }
     const int64_t parts = last - run + 1, share = (parts + 3) / 4, from = wave * share, to = from + share < parts ? from + share : parts;
     const int64_t p0 = pieces * slab / slabs, wide = pieces * (slab + 1) / slabs - p0;
-    const int64_t c = place_of((p0 + (lane < wide ? lane : wide - 1)) * 4, p.n, 4);
-    f32x4 sum = {};
+    const int64_t c = place_of((p0 + (lane < wide ? lane : wide - 1)) * E, p.n, E);
+    float sum[E] = {};
     for (int64_t k0 = from; k0 < to; k0 += U) {
-      f32x4 v[U];
+      float v[U][E];
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (k0 + u < to) __builtin_memcpy(&v[u], lists.part + (k0 + u == 0 ? 2 * run + 1 : 2 * (run + k0 + u)) * p.n + c, 16);
+        if (k0 + u < to) __builtin_memcpy(v[u], lists.part + (k0 + u == 0 ? 2 * run + 1 : 2 * (run + k0 + u)) * p.n + c, sizeof(v[u]));
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (k0 + u < to) sum += v[u];
+        if (k0 + u < to)
+#pragma unroll
+          for (int k = 0; k < E; ++k) sum[k] += v[u][k];
     }
-    if (wave > 0) sums[wave - 1][lane] = sum;
+    if (wave > 0) __builtin_memcpy(sums[wave - 1][lane], sum, sizeof(sum));
     __syncthreads();
     if (wave == 0) {
       O* out = static_cast<O*>(p.out) + row * p.ldd + c;
-      O o[4];
+      O o[E];
       if (p.add) __builtin_memcpy(o, out, sizeof(o));
 #pragma unroll
-      for (int w = 0; w < 3; ++w) sum += sums[w][lane];
+      for (int w = 0; w < 3; ++w)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = O(p.add ? float(o[k]) + p.scale * sum[k] : p.scale * sum[k]);
+        for (int k = 0; k < E; ++k) sum[k] += sums[w][lane][k];
+#pragma unroll
+      for (int k = 0; k < E; ++k) o[k] = O(p.add ? float(o[k]) + p.scale * sum[k] : p.scale * sum[k]);
       if (lane < wide) __builtin_memcpy(out, o, sizeof(o));
     }
     __syncthreads();
@@ -471,21 +474,22 @@ __global__ __launch_bounds__(256) void k_join(TableGrad p, Lists lists) {
 // 50304 rows 37 against 28 (8 tokens: 3.7 against 9.6, 32 against 22).
 constexpr int64_t kFewTokens = 256, kFewItems = 8192;
 inline bool scans(int64_t t, int64_t vocab, int64_t n) {
-  return (t <= kFewTokens && (vocab + 3) / 4 * ((n + 511) / 512) <= kFewItems) || vocab > (int64_t(1) << kMostBits) || n < 8;
+  return t <= kFewTokens && (vocab + 3) / 4 * ((n + 511) / 512) <= kFewItems;
 }
 
-template <class T, class O, bool ADD>
+template <class T, class O, bool ADD, int E>
 void launch_sums(const TableGrad& p, const Groups& groups, const Lists& lists, hipStream_t st) {
+  constexpr int J = E == 1 ? 1 : 4;  // columns of a lane in the joins
   const int64_t runs = (p.t + kRun - 1) / kRun, most = int64_t(1) << 19;
-  const int64_t slabs = ((p.n + kPiece<T> - 1) / kPiece<T> + 63) / 64, four = (slabs + 3) / 4, high = four < 8 ? four : 8;
+  const int64_t slabs = ((p.n + E - 1) / E + 63) / 64, four = (slabs + 3) / 4, high = four < 8 ? four : 8;
   for (int64_t first = 0; first < runs; first += most) {
-    const int64_t here = runs - first < most ? runs - first : most;
-    const int64_t clear = ADD || first ? 0 : (groups.count() * groups.words() + high - 1) / high;
-    k_sum<T, O, ADD><<<dim3(unsigned(here + clear), unsigned(high)), 256, 0, st>>>(p, groups, lists, first, unsigned(here));
+    const int64_t here = runs - first < most ? runs - first : most, words = (groups.count() * groups.words() + high - 1) / high;
+    const int64_t clear = ADD || first ? 0 : words < most ? words : most;
+    k_sum<T, O, ADD, E><<<dim3(unsigned(here + clear), unsigned(high)), 256, 0, st>>>(p, groups, lists, first, unsigned(here));
   }
   if (runs > 2) {
-    const int64_t items = (runs - 2) * ((p.n + 255) / 256);
-    k_join<O><<<unsigned(items < 2048 ? items : 2048), 256, 0, st>>>(p, lists);
+    const int64_t items = (runs - 2) * ((p.n + 64 * J - 1) / (64 * J));
+    k_join<O, J><<<unsigned(items < 2048 ? items : 2048), 256, 0, st>>>(p, lists);
   }
 }
 
@@ -501,10 +505,15 @@ int launch_grad(const TableGrad& p, void* workspace, hipStream_t st) {
   const unsigned vocab = unsigned(p.vocab), padding = p.padding >= 0 && p.padding < p.vocab ? unsigned(p.padding) : ~0u;
   const unsigned grid = unsigned(groups.count());
   k_group<<<grid, kWaves * 64, 0, st>>>(p.ids, p.t, vocab, padding, groups, lists);
-  if (p.add)
-    launch_sums<T, O, true>(p, groups, lists, st);
+  constexpr int E = kPiece<T>;
+  if (p.n < 8 && p.add)
+    launch_sums<T, O, true, 1>(p, groups, lists, st);
+  else if (p.n < 8)
+    launch_sums<T, O, false, 1>(p, groups, lists, st);
+  else if (p.add)
+    launch_sums<T, O, true, E>(p, groups, lists, st);
   else
-    launch_sums<T, O, false>(p, groups, lists, st);
+    launch_sums<T, O, false, E>(p, groups, lists, st);
   return launched();
 }
 

@@ -153,6 +153,8 @@ def residual_norm_backward(dy, dout, out, stats, h=None, gate=None, scale=None, 
         raise XmemError("dy: wanted with a norm before the next block, and only then")
     if dy is None and dout is None:
         raise XmemError("dout: wanted without dy")
+    if stats is None or (out is None and dy is not None):
+        raise XmemError("out, stats: wanted as residual_norm_forward returned them (save_stats)")
     first = dout if dy is None else dy
     code, dt, dev = _dtype(first, "dout" if dy is None else "dy", _ANY), first.dtype, first.device
     lddy = 0 if dy is None else _matrix(dy, "dy")

@@ -82,7 +82,8 @@ def test_embedding_backward(i, size, dtype):
 
 # frequent tokens among many, more tokens than one workgroup sorts, a vocabulary of more bits, long runs of one token
 LARGE = [(20000, 50304, 136, "frequent"), (33000, 200000, 64, "even"), (40000, 7, 72, "even"), (70001, 1000, 40, "frequent"),
-         (30000, 30000, 520, "one"), (9000, 1 << 21, 8, "frequent"), (150000, 50304, 16, "outside")]
+         (30000, 30000, 520, "one"), (9000, 1 << 21, 8, "frequent"), (150000, 50304, 16, "outside"),
+         (5000, 6_000_000, 9, "frequent"), (3000, 12345, 1, "frequent"), (40000, 5, 7, "even"), (2000, 700, 3, "outside")]
 
 
 @pytest.mark.parametrize("t,vocab,n,kind", LARGE)

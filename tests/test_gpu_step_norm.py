@@ -147,6 +147,24 @@ def test_residual_norm_in_place_and_same_bits():
         assert again[0] is v["r"] and more[0] is v["dout"]
 
 
+def test_residual_norm_in_place_without_sums_between():
+    """Nothing is summed between the reads of a row and its writes: no norm of the block, and no norm after the sum.  In rows whose last
+    piece begins a wavefront and shares columns with the one before it."""
+    g = torch.Generator().manual_seed(31)
+    for n, dtype in ((513, BF), (1025, HF), (259, FF), (2049, BF), (4097, BF), (8193, HF), (8195, FF), (70001, BF)):
+        r, h, d = (torch.randn(600, n, generator=g).to(dtype).cuda() for _ in range(3))
+        want = xm.residual_norm_forward(r, h, alpha=0.3, pre="none", save_stats=True)
+        grads = xm.residual_norm_backward(None, d, None if dtype == BF else want[0], want[2], h, alpha=0.3, pre="none")
+        log(f"[step] residual_norm in place without sums n={n} {dtype}")
+        for _ in range(3):
+            mine, grad = r.clone(), d.clone()
+            got = xm.residual_norm_forward(mine, h, alpha=0.3, pre="none", save_stats=True, in_place=True)
+            back = xm.residual_norm_backward(None, grad, None if dtype == BF else got[0], got[2], h, alpha=0.3, pre="none", in_place=True)
+            torch.cuda.synchronize()
+            assert got[0] is mine and torch.equal(mine, want[0]) and back[0] is grad and torch.equal(grad, grads[0])
+            assert torch.equal(back[1], grads[1]) and torch.equal(grad, d)
+
+
 def test_residual_norm_keeps_to_its_rows():
     """Through the C ABI with padded outputs: nothing between the rows is written, and the rows are the same."""
     g = torch.Generator().manual_seed(3)
