@@ -2,11 +2,12 @@
 """A training step of the package's operators, its memory estimated beside it.
 
 A residual MLP policy (embedding, blocks of two linear layers, vocabulary head) takes steps of the clipped policy
-loss with Newton-Schulz updates.  Every tensor that a step takes and gives back is written down as the profiler would (time,
+loss with Newton-Schulz updates; with --normed its blocks stand between norms, the embedding learns too and all gradients are
+clipped together.  Every tensor that a step takes and gives back is written down as the profiler would (time,
 address, bytes); the package's estimate of these events (pairing, orchestration, replay through the caching
 allocator's model) stands beside what the device's allocator saw.
 
-    python examples/policy_step.py [--hidden 2048 --layers 24 --vocab 50304 --tokens 8192 --steps 3]
+    python examples/policy_step.py [--hidden 2048 --layers 24 --vocab 50304 --tokens 8192 --steps 3] [--normed]
 """
 from __future__ import annotations
 
@@ -132,10 +133,103 @@ class Policy:
         return stats
 
 
-def train(hidden=256, layers=4, vocab=1024, tokens=512, steps=4, seed=0):
+class NormedPolicy(Policy):
+    """Blocks between norms: x <- x + scale norm(block(norm(x))), norms of the root mean square."""
+
+    def __init__(self, hidden, layers, vocab, tokens, seed=0):
+        super().__init__(hidden, layers, vocab, tokens, seed)
+        one = lambda *s: torch.ones(*s, device="cuda")
+        # each block's scale, the norm after it and the one before the next (the head); the norm before the first block
+        self.scale, self.post, self.pre, self.first = 0.5 * one(layers, hidden), one(layers, hidden), one(layers, hidden), one(hidden)
+        need = max(xm.xmem_residual_norm_backward_workspace_bytes(tokens, hidden, xm.XMEM_BF16), xm.xmem_clip_grad_norm_workspace_bytes(),
+                   xm.xmem_embedding_backward_workspace_bytes(tokens, vocab, hidden))
+        if need > self.workspace.numel():
+            self.workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+
+    def vectors(self):
+        return [self.scale, self.post, self.pre, self.first, self.up_b, self.down_b]
+
+    def state(self):
+        return super().state() + [self.scale, self.post, self.pre, self.first]
+
+    def how(self, i):
+        return dict(scale=self.scale[i], post="rms", post_weight=self.post[i], pre="rms", pre_weight=self.pre[i])
+
+    def forward(self, ids, led):
+        x = led.take(xm.embedding_forward(self.table, ids))
+        _, y, stats = xm.residual_norm_forward(x, pre_weight=self.first, save_stats=True)
+        led.take(y, stats)
+        kept = [(x, stats)]
+        for i in range(len(self.up)):
+            mid, z = led.take(*xm.linear_forward(y, self.up[i], self.up_b[i], activation="gelu", save_z=True, workspace=self.workspace))
+            out = led.take(xm.linear_forward(mid, self.down[i], self.down_b[i], workspace=self.workspace)[0])
+            x, y_next, stats = led.take(*xm.residual_norm_forward(x, out, save_stats=True, **self.how(i)))
+            kept.append((y, mid, z, out, x, stats))
+            y = y_next
+        return led.take(xm.linear_forward(y, self.head, workspace=self.workspace)[0]), y, kept
+
+    def gradients(self, ids, tokens, weights, old_logp, advantages, ref_logp, led, kl_coef=0.02):
+        """Stats and log-probabilities of the loss, and the gradients of (table, up, down, head, *vectors())."""
+        logits, y, kept = self.forward(ids, led)
+        stats, logp, dlogits = xm.policy_loss(logits, tokens, weights, old_logp, advantages, ref_logp, clip_high=0.28, kl_coef=kl_coef,
+                                              in_place=True, workspace=self.workspace)
+        led.take(stats, logp)
+        dy, dhead, _ = xm.linear_backward(dlogits, y, self.head, need_db=False, workspace=self.workspace)
+        led.take(dy, dhead)
+        led.give(logits, y)
+        del logits, dlogits, y
+        vectors = [led.take(torch.empty_like(v)) for v in self.vectors()]
+        dscale, dpost, dpre, dfirst, dup_b, ddown_b = vectors
+        dx = None
+        for i in reversed(range(len(self.up))):
+            y, mid, z, out, x, saved = kept.pop()
+            dx_next, dout, _, *sums = xm.residual_norm_backward(dy, dx, x, saved, out, in_place=dx is not None, workspace=self.workspace, **self.how(i))
+            led.take(*(t for t in (None if dx is not None else dx_next, dout, *sums) if t is not None))
+            dscale[i], dpost[i], dpre[i] = sums[0], sums[1], sums[3]
+            led.give(dy, out, x, saved, *sums)
+            dx = dx_next
+            del dx_next, sums, out, x, saved, dy
+            dmid, dw, db = led.take(*xm.linear_backward(dout, mid, self.down[i], workspace=self.workspace))
+            self.grads[1][i].copy_(dw)
+            ddown_b[i] = db
+            led.give(dout, mid, dw, db)
+            del dout, mid, dw, db
+            dy, dw, db = led.take(*xm.linear_backward(dmid, y, self.up[i], z, "gelu", workspace=self.workspace))
+            self.grads[0][i].copy_(dw)
+            dup_b[i] = db
+            led.give(dmid, y, z, dw, db)
+            del dmid, y, z, dw, db
+        x, saved = kept.pop()
+        made = dx is None
+        dx, _, _, _, _, _, dw, _ = xm.residual_norm_backward(dy, dx, x, saved, pre_weight=self.first, in_place=not made, workspace=self.workspace)
+        led.take(*((dx, dw) if made else (dw,)))
+        dfirst.copy_(dw)
+        led.give(dy, x, saved, dw)
+        del dy, x, saved, dw
+        dtable = led.take(xm.embedding_backward(dx, ids, len(self.table), workspace=self.workspace))
+        led.give(dx)
+        return stats, logp, [dtable, *self.grads, dhead, *vectors]
+
+    def step(self, ids, tokens, weights, old_logp, advantages, ref_logp, led, lr=0.02, kl_coef=0.02, max_norm=1.0):
+        stats, logp, grads = self.gradients(ids, tokens, weights, old_logp, advantages, ref_logp, led, kl_coef)
+        norm = led.take(xm.clip_grad_norm(grads, max_norm, workspace=self.workspace))
+        dtable, dup, ddown, dhead, *vectors = grads
+        for w, grad, momentum in zip((self.up, self.down, self.head), (dup, ddown, dhead), self.momenta):
+            scale = max(1.0, w.shape[-2] / w.shape[-1]) ** 0.5
+            update = led.take(xm.muon_update(grad, momentum, scale=scale, workspace=self.workspace))
+            w.add_(update, alpha=-lr)
+            led.give(update)
+            del update
+        for w, grad in zip((self.table, *self.vectors()), (dtable, *vectors)):
+            w.add_(grad, alpha=-lr)
+        led.give(dtable, dhead, logp, norm, *vectors)
+        return stats
+
+
+def train(hidden=256, layers=4, vocab=1024, tokens=512, steps=4, seed=0, normed=False):
     """Returns a dict: the loss of each step, the log-probability that tokens of positive (and of negative) advantage gained, and
     the estimated and measured peaks in bytes."""
-    policy = Policy(hidden, layers, vocab, tokens, seed)
+    policy = (NormedPolicy if normed else Policy)(hidden, layers, vocab, tokens, seed)
     g = torch.Generator(device="cuda").manual_seed(seed + 1)
     ids = torch.randint(0, vocab, (tokens,), generator=g, device="cuda")
     sampled = torch.randint(0, vocab, (tokens,), generator=g, device="cuda")
@@ -168,6 +262,7 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, default in (("hidden", 1024), ("layers", 12), ("vocab", 50304), ("tokens", 4096), ("steps", 4)):
         ap.add_argument("--" + name, type=int, default=default)
+    ap.add_argument("--normed", action="store_true")
     got = train(**vars(ap.parse_args()))
     for i, (loss, clipped) in enumerate(zip(got["loss"], got["clipped"])):
         print(f"step {i}: loss {loss:+.5f}, clipped {100 * clipped:.1f}%")
