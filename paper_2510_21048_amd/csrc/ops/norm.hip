@@ -20,6 +20,7 @@ struct Norms {
   void *out, *y;
   int64_t ldo, ldy;
   float* stats;
+  bool past_caches;   // outputs
   int64_t first = 0;  // row of the launch
 };
 
@@ -81,7 +82,10 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_norm(Norms p) {
   const auto place = [&](int j) { return Place<E>(j * W + tid, n); };
   const auto row = [&](const void* x, int64_t ld, int j) { return piece_at(static_cast<const T*>(x) + at * ld, place(j).at); };
   const auto put = [&](void* x, int64_t ld, int j, const float (&v)[E]) {
-    if (here) put_piece_at(static_cast<T*>(x) + at * ld, place(j).at, v);
+    if (here && p.past_caches)
+      put_piece_past(static_cast<T*>(x) + at * ld, place(j).at, v);
+    else if (here)
+      put_piece_at(static_cast<T*>(x) + at * ld, place(j).at, v);
   };
   // over the thread's elements of pieces that `piece` gives
   const auto total = [&](const auto& piece, const auto& f) {
@@ -320,11 +324,13 @@ __device__ inline float column_of(const NormGrads& p, int q, int64_t c) {
 // registers, half of them in LDS where they are four vectors', and all where a thread has more than eight columns of two.  The vectors are in LDS where they fit (VLDS).  With more than a piece a thread,
 // what the first norm does not need is loaded after its sums.
 template <class T, int W, int NCH, bool BIASES, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void k_norm_back(NormGrads p) {
+__global__ __launch_bounds__(BLOCK, 4) void k_norm_back(NormGrads p) {
   constexpr int E = kPiece<T>, R = BLOCK / W, VECTORS = BIASES ? 4 : 3;
   constexpr bool VLDS = NCH == 1, LATE = NCH > 1, APART = BIASES ? W < 1024 || NCH > 1 : NCH * E > 8;
   constexpr int HELD = BIASES ? APART ? 2 : 4 : APART ? 0 : 2;
-  constexpr int ROWS = BLOCK / kWave * (W < kWave ? W : kWave) * E, COLUMNS = VLDS ? VECTORS * W * E : 0;  // floats
+  // vectors in LDS: as many as leave room for two workgroups of 512 on a CU
+  constexpr int VL = VLDS ? (W == 512 && APART && E == 8 ? 2 : VECTORS) : 0;
+  constexpr int ROWS = BLOCK / kWave * (W < kWave ? W : kWave) * E, COLUMNS = VL * W * E;  // floats
   __shared__ typename RowSums<W, R>::Meet meet;
   __shared__ float apart[APART ? 2 : 1][APART ? NCH * E : 1][APART ? BLOCK : 1];
   __shared__ __attribute__((aligned(16))) float shared[R > 1 && ROWS > COLUMNS ? ROWS : COLUMNS > 4 ? COLUMNS : 4];  // vectors, then rows' sums
@@ -340,11 +346,10 @@ __global__ __launch_bounds__(BLOCK) void k_norm_back(NormGrads p) {
     __syncthreads();
   }
   const auto vector = [&](int q, int j, float (&v)[E]) {
-    if constexpr (VLDS) {
+    if (q < VL) {
 #pragma unroll
       for (int h = 0; h < E / 4; ++h) {
-        f32x4 part = {};
-        if (q < VECTORS) part = *reinterpret_cast<const f32x4*>(shared + ((q * (E / 4) + h) * W + tid) * 4);
+        const f32x4 part = *reinterpret_cast<const f32x4*>(shared + ((q * (E / 4) + h) * W + tid) * 4);
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[4 * h + k] = part[k];
       }
@@ -745,8 +750,11 @@ int xmem_residual_norm_forward(const void* d_r, int64_t ldr, const void* d_h, in
   if (tokens > 0 && !d_h && (d_gate || d_scale || d_out || post != XMEM_NORM_NONE)) return XMEM_EINVAL;  // of no rows no pointer is needed
   if (d_out && d_out == d_r && ldo != ldr) return XMEM_EINVAL;
   if (tokens > 0 && (!d_r || (pre != XMEM_NORM_NONE && !d_y) || (d_h && !d_out))) return XMEM_EINVAL;
+  // Outputs that the cache behind the L2s cannot hold are gone from it before anyone reads them: 2048 x 16384 in float32 (268 MB) 127 us,
+  // written past it 104; 32768 x 4096 in bfloat16 268 and 264.
+  const bool past_caches = tokens * width * (dtype == XMEM_F32 ? 4 : 2) * ((d_out != nullptr) + (d_y != nullptr)) >= kCacheBytes;
   const Norms p{d_r, d_h, d_gate, ldr, ldh, ldg, d_scale, d_w1, d_b1, d_w2, d_b2, tokens, width, post, pre, gate_activation, eps, alpha,
-                d_out, d_y, ldo, ldy, d_stats};
+                d_out, d_y, ldo, ldy, d_stats, past_caches};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (tokens == 0 || (!d_h && !d_y && !d_stats)) return XMEM_OK;
   return (dtype == XMEM_BF16 ? launch_norm<bf16> : dtype == XMEM_F16 ? launch_norm<f16> : launch_norm<float>)(p, st);

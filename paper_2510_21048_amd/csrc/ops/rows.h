@@ -49,6 +49,20 @@ __device__ inline void put_piece_at(T* x, int at, const float (&v)[kPiece<T>]) {
   for (int k = 0; k < kPiece<T>; ++k) e[k] = T(v[k]);
   __builtin_memcpy(reinterpret_cast<char*>(x) + unsigned(at) * unsigned(sizeof(T)), e, 16);
 }
+// 16 bytes to a place of any alignment, past the caches: where they would only push out what is read again.
+__device__ inline void store_past(void* to, u32x4 c) {
+  typedef unsigned any4 __attribute__((ext_vector_type(4), aligned(2)));
+  __builtin_nontemporal_store(any4(c), static_cast<any4*>(to));
+}
+template <class T>
+__device__ inline void put_piece_past(T* x, int at, const float (&v)[kPiece<T>]) {
+  T e[kPiece<T>];
+#pragma unroll
+  for (int k = 0; k < kPiece<T>; ++k) e[k] = T(v[k]);
+  u32x4 c;
+  __builtin_memcpy(&c, e, 16);
+  store_past(reinterpret_cast<char*>(x) + unsigned(at) * unsigned(sizeof(T)), c);
+}
 template <int E>
 __device__ inline void vector_at(const float* w, int at, float without, float (&v)[E]) {
   if (w) {
@@ -182,6 +196,7 @@ struct RowSums {
   }
 };
 
+constexpr int64_t kCacheBytes = int64_t(256) << 20;  // of the cache behind the L2s
 constexpr int64_t kMostRows = int64_t(1) << 31, kMostLd = int64_t(1) << 40;
 inline bool ld_ok(int64_t ld, int64_t width) { return ld >= width && ld < kMostLd; }
 inline bool type_ok(int dtype) { return dtype >= XMEM_BF16 && dtype <= XMEM_F32; }
