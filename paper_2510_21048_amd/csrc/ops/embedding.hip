@@ -136,7 +136,6 @@ __global__ __launch_bounds__(256) void k_scan(TableGrad p) {
 // Rows are spread over groups of kKeys or fewer by a multiplication: key = id * mul mod 2^bits, of which the upper bits are
 // the group, so that frequent tokens (whose numbers are often neighbours) do not meet in one.
 constexpr int kGroups = 256, kKeyBits = 10, kKeys = 1 << kKeyBits, kWaves = 16;
-constexpr int kNotes = 1024;  // of a wavefront
 constexpr int kRun = 16;  // entries of the sorted list that one wavefront adds up
 
 struct Groups {
@@ -187,16 +186,50 @@ Lists carve(void* base, int64_t t, const Groups& groups, int64_t n) {
   return w;
 }
 
+// A wavefront clears a row: 16 bytes a lane, the last ones moved down to the row's end.
+__device__ inline void clear_row(char* row, int64_t bytes, bool past_caches) {
+  const int lane = threadIdx.x & 63;
+  const u32x4 zero = {};
+  if (bytes < 16) {
+    if (lane < bytes / 2) reinterpret_cast<short*>(row)[lane] = 0;
+  } else if (past_caches) {
+#pragma unroll 4
+    for (int64_t i = lane * 16; i < bytes; i += 64 * 16) store_past(row + (i < bytes - 16 ? i : bytes - 16), zero);
+  } else {
+#pragma unroll 4
+    for (int64_t i = lane * 16; i < bytes; i += 64 * 16) __builtin_memcpy(row + (i < bytes - 16 ? i : bytes - 16), &zero, 16);
+  }
+}
+
+// The table's rows, by bytes.  Those from `early` on are cleared beside the grouping, whether they have tokens or not, the others without
+// a token beside the sums.
+struct Clear {
+  char* table;
+  int64_t row, distance, early, vocab;
+  bool past_caches;
+  __device__ void at(int64_t v) const { clear_row(table + v * distance, row, past_caches); }
+};
+
 // A workgroup has the rows of one group.  It looks at every token, each wavefront at a sixteenth of them in order, counts those of the
 // groups before and notes its own in LDS; then it counts its rows' tokens and puts them where these counts say.  Where a wavefront has
-// more than kNotes of its own, its workgroup reads the tokens again for each of the two.
-__global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64_t t, unsigned vocab, unsigned padding, Groups groups, Lists lists) {
-  __shared__ int hist[kWaves][kKeys], meet[kWaves][2], sums[kWaves];
-  __shared__ unsigned notes[kWaves][kNotes];  // place in the group, and the token's number in the wavefront's share
+// more than `most` of its own, its workgroup reads the tokens again for each of the two.  This takes few of the memory's cycles: workgroups
+// past the groups' clear rows beside it.
+__global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64_t t, unsigned vocab, unsigned padding, Groups groups, Lists lists,
+                                                       int most, Clear clear) {
+  __shared__ int meet[kWaves][2], sums[kWaves];
+  extern __shared__ int dynamic[];  // counts of each wavefront and row, then notes: place in the group, and the token's number in the share
+  if (blockIdx.x >= groups.count()) {
+    const int64_t step = (int64_t(gridDim.x) - groups.count()) * kWaves;
+    for (int64_t v = clear.early + (blockIdx.x - groups.count()) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); v < clear.vocab; v += step)
+      clear.at(v);
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int keys = 1 << groups.low;
   const unsigned mine = blockIdx.x, width = groups.bits - groups.low;
-  for (int i = threadIdx.x; i < kWaves * keys; i += kWaves * 64) hist[i >> groups.low][i & (keys - 1)] = 0;
+  int* const hist = dynamic + wave * keys;
+  unsigned* const notes = reinterpret_cast<unsigned*>(dynamic + kWaves * keys) + wave * most;
+  for (int i = threadIdx.x; i < kWaves * keys; i += kWaves * 64) dynamic[i] = 0;
   if (blockIdx.x == 0 && threadIdx.x == 0) lists.count[1] = 0;
   const int64_t share = ((t + kWaves - 1) / kWaves + 63) / 64 * 64, from = wave * share < t ? wave * share : t;
   const int n = int(from + share < t ? share : t - from);
@@ -224,7 +257,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64
     before += __popcll(less);
     if (hit) {
       const int at = own + __popcll(hit & ((uint64_t(1) << lane) - 1));
-      if (hit >> lane & 1 && at < kNotes) notes[wave][at] = unsigned(i0 + lane) << kKeyBits | unsigned(local);
+      if (hit >> lane & 1 && at < most) notes[at] = unsigned(i0 + lane) << kKeyBits | unsigned(local);
       own += __popcll(hit);
     }
   });
@@ -238,13 +271,13 @@ __global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     base += meet[w][0];
-    fits = fits && meet[w][1] <= kNotes;
+    fits = fits && meet[w][1] <= most;
   }
   if (fits) {
-    for (int i = lane; i < own; i += 64) atomicAdd(&hist[wave][notes[wave][i] & (kKeys - 1)], 1);
+    for (int i = lane; i < own; i += 64) atomicAdd(&hist[notes[i] & (kKeys - 1)], 1);
   } else {
     each([&](uint64_t hit, uint64_t, int local, int) {
-      if (hit >> lane & 1) atomicAdd(&hist[wave][local], 1);
+      if (hit >> lane & 1) atomicAdd(&hist[local], 1);
     });
   }
   __syncthreads();
@@ -252,32 +285,32 @@ __global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64
   int here = 0;
   if (int(threadIdx.x) < keys)
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) here += hist[w][threadIdx.x];
+    for (int w = 0; w < kWaves; ++w) here += dynamic[w * keys + threadIdx.x];
   int place = here;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const int up = __shfl_up(place, d);
     if (lane >= d) place += up;
   }
-  const uint64_t empty = __ballot(int(threadIdx.x) < keys && here == 0 && groups.id((mine << groups.low) + threadIdx.x) < vocab);
+  const uint64_t empty = __ballot(int(threadIdx.x) < keys && here == 0 && groups.id((mine << groups.low) + threadIdx.x) < clear.early);
   if (lane == 0 && wave < groups.words()) lists.empty[mine * groups.words() + wave] = empty;
   if (lane == 63) sums[wave] = place;
   __syncthreads();
   for (int w = 0; w < wave; ++w) place += sums[w];
   place += base;
-  if (mine + 1 == gridDim.x && int(threadIdx.x) == keys - 1) *lists.count = place;  // all of them
+  if (mine + 1 == groups.count() && int(threadIdx.x) == keys - 1) *lists.count = place;  // all of them
   place -= here;
   if (int(threadIdx.x) < keys)
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const int c = hist[w][threadIdx.x];
-      hist[w][threadIdx.x] = place;
+      const int c = dynamic[w * keys + threadIdx.x];
+      dynamic[w * keys + threadIdx.x] = place;
       place += c;
     }
   __syncthreads();
   // up to 64 tokens in their order, those of one row at a time
   const auto put = [&](uint64_t left, int local, int token) {
-    volatile int* next = hist[wave];
+    volatile int* next = hist;
     while (left) {
       const int leader = __builtin_ctzll(left), which = __builtin_amdgcn_readlane(local, leader);
       const uint64_t same = left & __ballot(local == which);
@@ -294,7 +327,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64
   if (fits) {
 #pragma unroll 1
     for (int i = 0; i < own; i += 64) {
-      const unsigned note = notes[wave][i + lane < own ? i + lane : i];
+      const unsigned note = notes[i + lane < own ? i + lane : i];
       put(__ballot(i + lane < own), int(note & (kKeys - 1)), int(note >> kKeyBits));
     }
   } else {
@@ -315,7 +348,7 @@ __device__ inline int64_t place_of(int64_t c, int64_t n, int w) { return c < n -
 // Workgroups past the launch's `runs` clear the rows without a token, those of 64 keys at a time.
 // E: elements of a piece, one where rows have fewer than eight.
 template <class T, class O, bool ADD, int E>
-__global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists lists, int64_t first_run, unsigned runs) {
+__global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists lists, int64_t first_run, unsigned runs, Clear clear) {
   constexpr int U = ADD ? 4 : 8;
   if (!ADD && blockIdx.x >= runs) {
     const unsigned words = unsigned(groups.words());
@@ -326,18 +359,7 @@ __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists l
       for (int turn = 0; left; ++turn) {
         const int k = __builtin_ctzll(left);
         left &= left - 1;
-        if (turn % 4 != __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) continue;
-        O* out = static_cast<O*>(p.out) + int64_t(groups.id(key + k)) * p.ldd;
-        constexpr int Z = E == 1 ? 1 : kPiece<O>;
-        const int64_t pieces = (p.n + Z - 1) / Z;
-        const u32x4 zero = {};
-        if (Z > 1 && p.past_caches) {
-#pragma unroll 4
-          for (int64_t i = threadIdx.x & 63; i < pieces; i += 64) store_past(out + place_of(i * Z, p.n, Z), zero);
-        } else {
-#pragma unroll 4
-          for (int64_t i = threadIdx.x & 63; i < pieces; i += 64) __builtin_memcpy(out + place_of(i * Z, p.n, Z), &zero, Z * sizeof(O));
-        }
+        if (turn % 4 == __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) clear.at(groups.id(key + k));
       }
     }
     return;
@@ -482,14 +504,14 @@ inline bool scans(int64_t t, int64_t vocab, int64_t n) {
 }
 
 template <class T, class O, bool ADD, int E>
-void launch_sums(const TableGrad& p, const Groups& groups, const Lists& lists, hipStream_t st) {
+void launch_sums(const TableGrad& p, const Groups& groups, const Lists& lists, const Clear& clear, hipStream_t st) {
   constexpr int J = E == 1 ? 1 : 4;  // columns of a lane in the joins
   const int64_t runs = (p.t + kRun - 1) / kRun, most = int64_t(1) << 19;
   const int64_t slabs = ((p.n + E - 1) / E + 63) / 64, four = (slabs + 3) / 4, high = four < 8 ? four : 8;
   for (int64_t first = 0; first < runs; first += most) {
     const int64_t here = runs - first < most ? runs - first : most, words = (groups.count() * groups.words() + high - 1) / high;
-    const int64_t clear = ADD || first ? 0 : words < most ? words : most;
-    k_sum<T, O, ADD, E><<<dim3(unsigned(here + clear), unsigned(high)), 256, 0, st>>>(p, groups, lists, first, unsigned(here));
+    const int64_t beside = ADD || first || clear.early == 0 ? 0 : words < most ? words : most;
+    k_sum<T, O, ADD, E><<<dim3(unsigned(here + beside), unsigned(high)), 256, 0, st>>>(p, groups, lists, first, unsigned(here), clear);
   }
   if (runs > 2) {
     const int64_t items = (runs - 2) * ((p.n + 64 * J - 1) / (64 * J));
@@ -507,17 +529,23 @@ int launch_grad(const TableGrad& p, void* workspace, hipStream_t st) {
   const Groups groups = groups_of(p.vocab);
   const Lists lists = carve(workspace, p.t, groups, p.n);
   const unsigned vocab = unsigned(p.vocab), padding = p.padding >= 0 && p.padding < p.vocab ? unsigned(p.padding) : ~0u;
-  const unsigned grid = unsigned(groups.count());
-  k_group<<<grid, kWaves * 64, 0, st>>>(p.ids, p.t, vocab, padding, groups, lists);
+  const int64_t share = (p.t + kWaves - 1) / kWaves;
+  const int notes = share >= 4096 ? 1024 : share >= 256 ? int(share / 4) : 64;
+  // Grouping many tokens leaves the memory idle for as long as it takes to clear 1,500 bytes a token: 32768 x 2048 88.5 us without, 85.1
+  // with, 86.3 with 2,500.  With 8192 tokens it is not worth the rows that are then written twice (31.0, 32.1).
+  const int64_t row = p.n * int64_t(sizeof(O)), early = p.add || p.t < 16384 ? 0 : p.t * 1500 / row;
+  const Clear clear{static_cast<char*>(p.out), row, p.ldd * int64_t(sizeof(O)), early < p.vocab ? p.vocab - early : 0, p.vocab, p.past_caches};
+  const unsigned grid = unsigned(groups.count()) + (early ? kCus : 0);
+  k_group<<<grid, kWaves * 64, size_t(kWaves) * ((1 << groups.low) + notes) * 4, st>>>(p.ids, p.t, vocab, padding, groups, lists, notes, clear);
   constexpr int E = kPiece<T>;
   if (p.n < 8 && p.add)
-    launch_sums<T, O, true, 1>(p, groups, lists, st);
+    launch_sums<T, O, true, 1>(p, groups, lists, clear, st);
   else if (p.n < 8)
-    launch_sums<T, O, false, 1>(p, groups, lists, st);
+    launch_sums<T, O, false, 1>(p, groups, lists, clear, st);
   else if (p.add)
-    launch_sums<T, O, true, E>(p, groups, lists, st);
+    launch_sums<T, O, true, E>(p, groups, lists, clear, st);
   else
-    launch_sums<T, O, false, E>(p, groups, lists, st);
+    launch_sums<T, O, false, E>(p, groups, lists, clear, st);
   return launched();
 }
 
