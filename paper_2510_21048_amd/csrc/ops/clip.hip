@@ -1,7 +1,14 @@
 // clip.hip -- the norm of many gradients as one vector, and their scaling, on MI355X (gfx950).
 //
-// The gradients' places and sizes travel as kernel arguments, kTable of them a launch: nothing is copied to the device and a
-// captured graph holds them.  Squares are added up in 64 bits (their range is no matter then), in a fixed order.
+// norm = scale sqrt(sum g^2), g <- scale min(1, max_norm / (norm + 1e-6)) g.  The gradients' places and sizes travel as kernel arguments, kTable of
+// them a launch: nothing is copied to the device, and a captured graph holds them.  Squares are added up in 64 bits (their range
+// is no matter then, and 64-bit products cost nothing beside the memory), in a fixed order: each workgroup's share, then every workgroup of the
+// scaling adds up all shares for itself, which saves a launch between the two.  A gradient is looked at from the 16-byte boundary
+// before it, so that its loads are aligned wherever it begins.
+//
+// Bound by memory: the norm has to be known before the first gradient is written, so all are read twice.  147 gradients of 2.03 GB: squares 362 us
+// (5.6 TB/s), scaling 747 (4.05 GB, 5.4 TB/s).  The scaling begins with the last gradients, which the caches may still hold; with the
+// first ones 8 us more.  27 gradients of 5 MB take 4.6 and 6.6.
 #include <math.h>
 
 #include <algorithm>
@@ -15,7 +22,7 @@ namespace {
 
 constexpr int kTable = 128;          // gradients of a launch: two a lane
 constexpr int kThreads = 256;
-constexpr int kParts = 2048;         // workgroups of a norm at most, each with a sum of its own
+constexpr int kParts = 2048;         // workgroups of a norm at most, each with a sum of its own (500 MB in float32 70 us; with 1024 82)
 constexpr int kLoads = 4;            // of 16 bytes, a thread and piece of work
 constexpr int kSpan = kThreads * kLoads * 16;  // bytes of a piece of work
 constexpr int64_t kMostSize = int64_t(1) << 48;

@@ -1,7 +1,18 @@
 // norm.hip -- the norms before and after a block with its gate, scale and residual sum, and their gradients, on MI355X (gfx950).
 //
-// A row is read once: what it needs of its inputs stays in registers (a wavefront a row where they hold it, else a workgroup),
-// two or four sums are taken of it, and its outputs are written once.  A norm's mean is taken before its squares, so nothing cancels.
+// Forward, with xhat = (x - mu) rho: out = r + alpha s a(g) (hhat w1 + b1), y = outhat w2 + b2.  A row is read once: its inputs stay in
+// registers, each norm takes one sum of it (two with a mean: squares are taken of what is left without it, so nothing cancels), and
+// its outputs are written once.  y comes from the 32-bit sum, so that it is rounded once; the stored out is what the backward pass sees.
+//
+// Backward: e = dy w2, dr = dout + rho2 (e - [layer] mean(e) - outhat mean(e outhat)); with b = dr a(g) and f = alpha s b w1: dh = rho1 (f -
+// [layer] mean(f) - hhat mean(f hhat)), dgate = dr alpha s (hhat w1 + b1) a'(g).  The vectors' gradients are sums over rows of b hhat, b, dy outhat
+// and dy, times what a column has in common: a workgroup goes over rows with its threads on the same columns, keeps their sums, and writes
+// one part a workgroup; k_norm_sums adds the parts up in order.
+//
+// Bound by memory.  Forward, bfloat16, both norms, gate, scale: 32768 x 4096 258 us (5.2 TB/s of 1.34 GB; a large copy reaches 4.9).
+// Backward of the same 426 and 9 (2.15 GB, 5.0 TB/s), 8192 x 2048 55.4 and 6.3 (268 MB, 4.8 TB/s; with means and biases 60 and 9).  Wide
+// gradients are not: 4096 x 16384 288 and 8 (1.07 GB, 3.7 TB/s): one workgroup a CU, whose second loads wait for its first sums.
+// One row of 2048 takes 2.4 us, of which a launch is 2.1.
 #include "rows.h"
 
 using namespace xops;
@@ -69,7 +80,8 @@ __device__ inline void moments(Sums& sums, const Each& each, int kind, int64_t n
   rho = 1.0f / sqrtf(sums.one(each([&](float x) { return (x - mu) * (x - mu); })) / float(n) + eps);
 }
 
-// W threads of a row, with NCH pieces of it in each thread's registers; as many rows a workgroup as make 256 threads.
+// W threads of a row, with NCH pieces of it in each thread's registers; as many rows a workgroup as make 256 threads.  The last piece
+// is moved down to the row's end (Place), so that no thread has a tail: 8192 x 2047 with tails 40 us, without 34.
 template <class T, int W, int NCH>
 __global__ __launch_bounds__(W < 256 ? 256 : W) void k_norm(Norms p) {
   constexpr int E = kPiece<T>, R = W < 256 ? 256 / W : 1;
@@ -230,6 +242,10 @@ template <class T, int W, int NCH>
 int launch_norm(const Norms& p, hipStream_t st) {
   return launch_rows(k_norm<T, W, NCH>, p, W < 256 ? 256 / W : 1, W < 256 ? 256 : W, st);
 }
+// A piece a thread up to 512 pieces, two or four beyond.  Measured in us, bfloat16 without a gate: rows of 2048 in 256 threads 25.0 (8192
+// of them) and 6.1 (1003), in a wavefront of four pieces a lane 28.2 and 8.5; of 4096 in 512 threads 25.4 (4096 rows) and 4.5 (200), in 256 25.9
+// and 5.6; of 8192 in 512 threads 26.3 (2048) and 5.7 (100), in 256 29.5 and 8.1, in 1024 27.6 and 5.5; of 16,384 in 1024 threads 27.5
+// (1024) and 6.8 (60), in 512 30.8 and 8.1.  Rows below a wavefront share one: 32768 of 40 5.4, one a wavefront 26.
 template <class T>
 int launch_norm(const Norms& p, hipStream_t st) {
   const int64_t pieces = (p.n + kPiece<T> - 1) / kPiece<T>;
@@ -240,8 +256,8 @@ int launch_norm(const Norms& p, hipStream_t st) {
   if (pieces <= 64) return launch_norm<T, 64, 1>(p, st);
   if (pieces <= 128) return launch_norm<T, 128, 1>(p, st);
   if (pieces <= 256) return launch_norm<T, 256, 1>(p, st);
-  if (pieces <= 512) return launch_norm<T, 256, 2>(p, st);
-  if (pieces <= 1024) return launch_norm<T, 256, 4>(p, st);
+  if (pieces <= 512) return launch_norm<T, 512, 1>(p, st);
+  if (pieces <= 1024) return launch_norm<T, 512, 2>(p, st);
   if (pieces <= 2048) return launch_norm<T, 1024, 2>(p, st);
   if (pieces <= 4096) return launch_norm<T, 1024, 4>(p, st);
   return launch_rows(k_norm_any<T>, p, 1, 1024, st);
@@ -321,8 +337,11 @@ __device__ inline float column_of(const NormGrads& p, int q, int64_t c) {
 }
 
 // BLOCK / W rows at a time, W threads and NCH pieces a thread each, whose columns' sums over all of the workgroup's rows stay in
-// registers, half of them in LDS where they are four vectors', and all where a thread has more than eight columns of two.  The vectors are in LDS where they fit (VLDS).  With more than a piece a thread,
-// what the first norm does not need is loaded after its sums.
+// registers, half of them in LDS where they are four vectors' (BIASES), and all where a thread has more than eight columns of two.  The
+// vectors are in LDS too (a thread would spend 24 to 32 registers on them), those of rows past 1024 pieces in the L2s.  With more than
+// a piece a thread, what the first norm does not need is loaded after its sums.  128 registers, so that a CU has 16 wavefronts:
+// 131 made 8192 x 2048 74 us instead of 55.  Two workgroups of 512 a CU wait less for each other's sums than one of 1024 (55, 63); of
+// 256 threads they write more parts (62 and 8.5 for the sums).
 template <class T, int W, int NCH, bool BIASES, int BLOCK>
 __global__ __launch_bounds__(BLOCK, 4) void k_norm_back(NormGrads p) {
   constexpr int E = kPiece<T>, R = BLOCK / W, VECTORS = BIASES ? 4 : 3;

@@ -215,8 +215,8 @@ def embedding_forward(table, ids, scale: float = 1.0, padding_id: int | None = N
 
 def embedding_backward(dy, ids, vocab: int, scale: float = 1.0, padding_id: int | None = None, into=None, dtype=None, workspace=None,
                        stream=None):
-    """The gradient [vocab, n] of ``embedding_forward``'s table for dy [t, n]: scale times the sum of each token's rows, in the tokens'
-    order and 32 bits.  It is of dy's type, or float32 with ``dtype``; with ``into`` (either type, rows may be strided) it is added to
+    """The gradient [vocab, n] of ``embedding_forward``'s table for dy [t, n]: scale times the sum of each token's rows, in 32 bits and
+    a fixed order.  Tokens equal to padding_id or outside [0, vocab) add nothing.  It is of dy's type, or float32 with ``dtype``; with ``into`` (either type, rows may be strided) it is added to
     that, which is returned."""
     import torch
     load_ops()
