@@ -89,55 +89,108 @@ struct TableGrad {
   bool past_caches;  // the rows without a token
 };
 
-constexpr int kIds = 1024;  // tokens looked at together
+// W columns of a row of n >= W from c on: the last place is moved so far down that it ends with the row.  Two lanes of a wavefront have
+// its columns twice then, and write the same values to them.
+__device__ inline int64_t place_of(int64_t c, int64_t n, int w) { return c < n - w ? c : n - w; }
 
-// A wavefront has one row of the table, 64 pieces of it at a time, and looks at every token.
-template <class T, class O>
+// What one lane of a wavefront writes is there for the others.
+__device__ inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ---- few tokens: every row looks at all of them
+
+constexpr int kTile = 2048;  // tokens looked at together
+
+// A workgroup has four rows of the table (far apart: neighbours may all be frequent) and 64 pieces of them.  Each wavefront looks at every
+// fourth 64 of the tokens, notes those of the four rows, loads their rows of dy eight at a time and adds them up; then each has one of the
+// rows and the four sums of it.  E: elements of a piece, one where rows have fewer than eight.
+template <class T, class O, int E>
 __global__ __launch_bounds__(256) void k_scan(TableGrad p) {
-  constexpr int E = kPiece<T>;
-  __shared__ int ids[kIds];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t slabs = (p.n + 64 * E - 1) / (64 * E), rows = (p.vocab + 3) / 4;
-  for (int64_t item = blockIdx.x; item < rows * slabs; item += gridDim.x) {
-    const int64_t v = item / slabs * 4 + wave, i = item % slabs * 64 + lane;
-    float sum[E] = {};
-    bool any = false;
-    for (int64_t t0 = 0; t0 < p.t; t0 += kIds) {
-      __syncthreads();
-      for (int k = threadIdx.x; k < kIds; k += 256) {
-        const int64_t id = t0 + k < p.t ? p.ids[t0 + k] : -1;
-        ids[k] = id >= 0 && id < p.vocab && id != p.padding ? int(id) : -1;
-      }
-      __syncthreads();
-      for (int k = 0; k < kIds && t0 + k < p.t; k += 64) {
-        uint64_t hit = __ballot(ids[k + lane] == int(v));
-        any = any || hit;
-        while (hit) {
-          const int at = __builtin_ctzll(hit);
-          hit &= hit - 1;
-          float g[E];
-          unpack<T>(piece_of(static_cast<const T*>(p.dy) + (t0 + k + at) * p.lddy, i, p.n), g);
+  constexpr int U = 8, QUARTER = kTile / 4, PER = QUARTER / 64;
+  __shared__ unsigned short notes[4][QUARTER];  // token behind the wavefront's first, row
+  __shared__ float parts[4][4][E][64];
+  __shared__ unsigned touched[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t pieces = (p.n + E - 1) / E, slabs = (pieces + 63) / 64, apart = (p.vocab + 3) / 4;
+  for (int64_t item = blockIdx.x; item < apart * slabs; item += gridDim.x) {
+    const int64_t row0 = item / slabs, slab = item % slabs, p0 = pieces * slab / slabs, c0 = p0 * E;
+    const int wide = int(pieces * (slab + 1) / slabs - p0), off = int(place_of(c0 + (lane < wide ? lane : wide - 1) * E, p.n, E) - c0);
+    const T* dy = static_cast<const T*>(p.dy) + c0;
+    float sum[4][E] = {};
+    unsigned mine = 0;  // rows with a token
+    for (int64_t t0 = wave * 64; t0 < p.t; t0 += kTile) {
+      uint64_t id[PER];
+      const int here = int(p.t - t0 < kTile ? p.t - t0 : kTile);
 #pragma unroll
-          for (int q = 0; q < E; ++q) sum[q] += g[q];
+      for (int j = 0; j < PER; ++j)
+        if (j * 256 < here) id[j] = p.ids[t0 + (j * 256 + lane < here ? j * 256 + lane : here - 1)];
+      int own = 0;
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+        if (j * 256 < here) {
+          // which of the four rows
+          const unsigned low = unsigned(id[j]), far = low - unsigned(row0);
+          const int r = far == 0 ? 0 : far == unsigned(apart) ? 1 : far == 2 * unsigned(apart) ? 2 : 3;
+          const uint64_t hit = __ballot(far == r * unsigned(apart) && (id[j] >> 32) == 0 && low < unsigned(p.vocab) && int64_t(id[j]) != p.padding &&
+                                        j * 256 + lane < here);
+          if (hit) {
+            if (hit >> lane & 1) notes[wave][own + __popcll(hit & ((uint64_t(1) << lane) - 1))] = static_cast<unsigned short>((j * 256 + lane) << 2 | r);
+            own += __popcll(hit);
+          }
         }
+      wave_sync();
+#pragma unroll 1
+      for (int k = 0; k < own; k += U) {
+        const int note = notes[wave][k + (lane & (U - 1)) < own ? k + (lane & (U - 1)) : k];
+        u32x4 c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (k + u < own)
+            __builtin_memcpy(&c[u], dy + (t0 + (__builtin_amdgcn_readlane(note, u) >> 2)) * p.lddy + unsigned(off), E * sizeof(T));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (k + u < own) {
+            const int r = __builtin_amdgcn_readlane(note, u) & 3;
+            mine |= 1u << r;
+            T piece[E];
+            __builtin_memcpy(piece, &c[u], sizeof(piece));
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (r == q)
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[q][e] += float(piece[e]);
+          }
       }
+      wave_sync();
     }
-    if (v >= p.vocab || (p.add && !any)) continue;
-    O* out = static_cast<O*>(p.out) + v * p.ldd;
-    O e[E];
+    if (lane == 0) touched[wave] = mine;
 #pragma unroll
-    for (int q = 0; q < E; ++q) {
-      float s = p.scale * sum[q];
-      if (p.add && i * E + q < p.n) s += float(out[i * E + q]);
-      e[q] = O(s);
-    }
-    if ((i + 1) * E <= p.n) {
-      __builtin_memcpy(out + i * E, e, sizeof(e));
-    } else {
+    for (int q = 0; q < 4; ++q)
+      if (mine >> q & 1)
 #pragma unroll
-      for (int q = 0; q < E; ++q)
-        if (i * E + q < p.n) out[i * E + q] = e[q];
+        for (int e = 0; e < E; ++e) parts[wave][q][e][lane] = sum[q][e];
+    __syncthreads();
+    const int64_t row = row0 + wave * apart;
+    bool any = false;
+    float total[E] = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      if (touched[w] >> wave & 1) {
+        any = true;
+#pragma unroll
+        for (int e = 0; e < E; ++e) total[e] += parts[w][wave][e][lane];
+      }
+    if (row < p.vocab && (any || !p.add) && lane < wide) {
+      O* out = static_cast<O*>(p.out) + row * p.ldd + c0 + off;
+      O o[E];
+      if (p.add) __builtin_memcpy(o, out, sizeof(o));
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = O(p.add ? float(o[e]) + p.scale * total[e] : p.scale * total[e]);
+      __builtin_memcpy(out, o, sizeof(o));
     }
+    __syncthreads();
   }
 }
 
@@ -323,12 +376,13 @@ __global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64
   __syncthreads();
   // up to 64 tokens in their order, those of one row at a time
   const auto put = [&](uint64_t left, int local, int token) {
-    volatile int* next = hist;
     while (left) {
       const int leader = __builtin_ctzll(left), which = __builtin_amdgcn_readlane(local, leader);
       const uint64_t same = left & __ballot(local == which);
-      const int first = next[which];
-      if (lane == leader) next[which] = first + __popcll(same);
+      const int first = hist[which];
+      wave_sync();
+      if (lane == leader) hist[which] = first + __popcll(same);
+      wave_sync();
       if (same >> lane & 1) {
         const int at = first + __popcll(same & ((uint64_t(1) << lane) - 1));
         lists.token[at] = int(from) + token;
@@ -350,10 +404,6 @@ __global__ __launch_bounds__(kWaves * 64) void k_group(const int64_t* ids, int64
 
 // What a run leaves: its last row begins in it and ends past the next run; all of it is one row that began before and goes on.
 constexpr int kBegins = 1, kPasses = 2;
-
-// W columns of a row of n >= W from c on: the last place is moved so far down that it ends with the row.  Two lanes of a wavefront have
-// its columns twice then, and write the same values to them.
-__device__ inline int64_t place_of(int64_t c, int64_t n, int w) { return c < n - w ? c : n - w; }
 
 // A wavefront adds up the entries of a run over 64 pieces of their rows, as many of them alike as slabs come to.  A row that begins in
 // the run and ends in the next is finished here, and left out there.  A longer one leaves its part in part row 2 r + 1 where it
@@ -509,9 +559,9 @@ __global__ __launch_bounds__(256) void k_join(TableGrad p, Lists lists) {
   }
 }
 
-// Looking at every token for every row takes one launch, grouping three.  256 tokens of width 1024: 1021 rows 6.1 us against 14.5,
-// 50304 rows 37 against 28 (8 tokens: 3.7 against 9.6, 32 against 22).
-constexpr int64_t kFewTokens = 256, kFewItems = 8192;
+// Looking at every token for every row takes one launch, grouping three.  In us, 895 rows of 147: 16 tokens 4.2 against 11.3, 600 7.6 against
+// 17.1, 2000 15.8 against 18.2; 1224 rows of 3904: 10.4 and 12.9, 13.4 and 19.6, 21.6 and 22.4; 8 tokens of 50304 rows of 1024 67 and 22.
+constexpr int64_t kFewTokens = 2048, kFewItems = 2560;
 inline bool scans(int64_t t, int64_t vocab, int64_t n) {
   return t <= kFewTokens && (vocab + 3) / 4 * ((n + 511) / 512) <= kFewItems;
 }
@@ -535,8 +585,13 @@ void launch_sums(const TableGrad& p, const Groups& groups, const Lists& lists, c
 template <class T, class O>
 int launch_grad(const TableGrad& p, void* workspace, hipStream_t st) {
   if (scans(p.t, p.vocab, p.n)) {
-    const int64_t items = (p.vocab + 3) / 4 * ((p.n + 64 * kPiece<T> - 1) / (64 * kPiece<T>)), most = 1 << 20;
-    k_scan<T, O><<<unsigned(items < most ? items : most), 256, 0, st>>>(p);
+    constexpr int E = kPiece<T>;
+    const int64_t items = (p.vocab + 3) / 4 * ((p.n + 64 * E - 1) / (64 * E)), most = 1 << 20;
+    const unsigned grid = unsigned(items < most ? items : most);
+    if (p.n < 8)
+      k_scan<T, O, 1><<<grid, 256, 0, st>>>(p);
+    else
+      k_scan<T, O, E><<<grid, 256, 0, st>>>(p);
     return launched();
   }
   const Groups groups = groups_of(p.vocab);

@@ -242,10 +242,11 @@ template <class T, int W, int NCH>
 int launch_norm(const Norms& p, hipStream_t st) {
   return launch_rows(k_norm<T, W, NCH>, p, W < 256 ? 256 / W : 1, W < 256 ? 256 : W, st);
 }
-// A piece a thread up to 512 pieces, two or four beyond.  Measured in us, bfloat16 without a gate: rows of 2048 in 256 threads 25.0 (8192
-// of them) and 6.1 (1003), in a wavefront of four pieces a lane 28.2 and 8.5; of 4096 in 512 threads 25.4 (4096 rows) and 4.5 (200), in 256 25.9
-// and 5.6; of 8192 in 512 threads 26.3 (2048) and 5.7 (100), in 256 29.5 and 8.1, in 1024 27.6 and 5.5; of 16,384 in 1024 threads 27.5
-// (1024) and 6.8 (60), in 512 30.8 and 8.1.  Rows below a wavefront share one: 32768 of 40 5.4, one a wavefront 26.
+// A piece a thread up to 256 pieces (512 where rows are few), two or four beyond.  Measured in us, bfloat16 without a gate: rows of 2048 in
+// 256 threads 25.0 (8192 of them) and 6.1 (1003), in a wavefront of four pieces a lane 28.2 and 8.5; of 4096 with a gate in 256 threads 264 to 272
+// (32768), in 512 265 to 288, and without one 5.6 and 4.5 (200); of 8192 in 512 threads 26.3 (2048) and 5.7 (100), in 256 29.5 and 8.1, in
+// 1024 27.6 and 5.5; of 16,384 in 1024 threads 27.5 (1024) and 6.8 (60), in 512 30.8 and 8.1.  Rows below a wavefront share one: 32768 of
+// 40 5.4, one a wavefront 26.
 template <class T>
 int launch_norm(const Norms& p, hipStream_t st) {
   const int64_t pieces = (p.n + kPiece<T> - 1) / kPiece<T>;
@@ -256,7 +257,7 @@ int launch_norm(const Norms& p, hipStream_t st) {
   if (pieces <= 64) return launch_norm<T, 64, 1>(p, st);
   if (pieces <= 128) return launch_norm<T, 128, 1>(p, st);
   if (pieces <= 256) return launch_norm<T, 256, 1>(p, st);
-  if (pieces <= 512) return launch_norm<T, 512, 1>(p, st);
+  if (pieces <= 512) return p.t < 2048 ? launch_norm<T, 512, 1>(p, st) : launch_norm<T, 256, 2>(p, st);
   if (pieces <= 1024) return launch_norm<T, 512, 2>(p, st);
   if (pieces <= 2048) return launch_norm<T, 1024, 2>(p, st);
   if (pieces <= 4096) return launch_norm<T, 1024, 4>(p, st);
