@@ -93,7 +93,7 @@ struct TableGrad {
 // its columns twice then, and write the same values to them.
 __device__ inline int64_t place_of(int64_t c, int64_t n, int w) { return c < n - w ? c : n - w; }
 
-// What one lane of a wavefront writes is there for the others.
+// What one lane of a wavefront wrote is there for the others, and what it read is not yet what they write.
 __device__ inline void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
@@ -186,6 +186,7 @@ __global__ __launch_bounds__(256) void k_scan(TableGrad p) {
       O* out = static_cast<O*>(p.out) + row * p.ldd + c0 + off;
       O o[E];
       if (p.add) __builtin_memcpy(o, out, sizeof(o));
+      wave_sync();  // elements that two lanes have are read by both before one writes them
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] = O(p.add ? float(o[e]) + p.scale * total[e] : p.scale * total[e]);
       __builtin_memcpy(out, o, sizeof(o));
@@ -480,6 +481,7 @@ __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists l
 #pragma unroll 1
     for (int g = begin; g < end; g += U) {
       load(g + U, next);
+      if (ADD) wave_sync();  // elements that two lanes have are read by both before one writes them
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int e = g + u;
@@ -547,6 +549,7 @@ __global__ __launch_bounds__(256) void k_join(TableGrad p, Lists lists) {
       O* out = static_cast<O*>(p.out) + row * p.ldd + c;
       O o[E];
       if (p.add) __builtin_memcpy(o, out, sizeof(o));
+      wave_sync();  // elements that two lanes have are read by both before one writes them
 #pragma unroll
       for (int w = 0; w < 3; ++w)
 #pragma unroll
@@ -571,10 +574,11 @@ void launch_sums(const TableGrad& p, const Groups& groups, const Lists& lists, c
   constexpr int J = E == 1 ? 1 : 4;  // columns of a lane in the joins
   const int64_t runs = (p.t + kRun - 1) / kRun, most = int64_t(1) << 19;
   const int64_t slabs = ((p.n + E - 1) / E + 63) / 64, four = (slabs + 3) / 4, high = four < 8 ? four : 8;
-  for (int64_t first = 0; first < runs; first += most) {
+  for (int64_t first = 0; first == 0 || first < runs; first += most) {  // no tokens: the table is cleared all the same
     const int64_t here = runs - first < most ? runs - first : most, words = (groups.count() * groups.words() + high - 1) / high;
     const int64_t beside = ADD || first || clear.early == 0 ? 0 : words < most ? words : most;
-    k_sum<T, O, ADD, E><<<dim3(unsigned(here + beside), unsigned(high)), 256, 0, st>>>(p, groups, lists, first, unsigned(here), clear);
+    if (here + beside > 0)
+      k_sum<T, O, ADD, E><<<dim3(unsigned(here + beside), unsigned(high)), 256, 0, st>>>(p, groups, lists, first, unsigned(here), clear);
   }
   if (runs > 2) {
     const int64_t items = (runs - 2) * ((p.n + 64 * J - 1) / (64 * J));

@@ -118,6 +118,31 @@ def test_embedding_backward_of_no_tokens():
     assert bool((xm.embedding_backward(dy, ids, 50, into=into) == 3).all())
 
 
+@pytest.mark.parametrize("vocab,n", [(50304, 264), (300000, 5), (7, 300000)])
+@pytest.mark.parametrize("o", [BF, FF])
+def test_embedding_backward_of_no_tokens_clears_large_tables(vocab, n, o):
+    dy, ids = torch.empty(0, n, dtype=BF, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda")
+    full = torch.full((vocab, n), 3.0, dtype=o, device="cuda")  # freed, so that the outputs are likely to lie where it lay
+    del full
+    log(f"[step] embedding_backward of no tokens, table {vocab} x {n} {o}")
+    assert bool((xm.embedding_backward(dy, ids, vocab, dtype=o) == 0).all())
+    into = torch.full((vocab, n), 3.0, dtype=o, device="cuda")
+    assert bool((xm.embedding_backward(dy, ids, vocab, into=into) == 3).all())
+
+
+def test_embedding_backward_with_the_most_notes_and_keys():
+    """A group of 1024 rows, and as many notes of tokens as a wavefront keeps: 128 KiB of LDS."""
+    g = torch.Generator().manual_seed(70)
+    t, vocab, n = 70000, 300000, 8
+    dy, c = rows(g, t, n, BF, 0)
+    ids = some_ids(g, t, vocab, "frequent")
+    log("[step] embedding_backward 70000 tokens of 300000, width 8")
+    got = xm.embedding_backward(dy, ids.cuda(), vocab)
+    torch.cuda.synchronize()
+    want, bound = ref.table_grad(c, ids, vocab, 1.0, None, None, BF)
+    within(got, want, bound, "dtable")
+
+
 def test_embedding_rows_keep_to_themselves():
     """What lies between rows stays; NaN and infinity of one token stay in its row, those of padding and of unnamed rows are not seen."""
     g = torch.Generator().manual_seed(6)
