@@ -97,6 +97,24 @@ def _no(what: str, why: str, *given) -> None:
             raise XmemError(f"{what}: not without {why}")
 
 
+def _apart(over, name: str, **read) -> None:
+    """Refuses tensors that a call reads while it writes `over`: their rows may lie between its rows (halves of one matrix), not on them."""
+    def rows(t):  # first byte, bytes of a row, from row to row, rows
+        (r, c), size = t.shape, t.element_size()
+        return t.data_ptr(), c * size, (t.stride(0) if r > 1 else c) * size, r
+
+    for what, t in read.items():
+        if t is None or not t.numel() or not over.numel():
+            continue
+        (at, wide, ld, r), (at2, wide2, ld2, r2) = sorted((rows(over), rows(t)))
+        gap = at2 - at
+        if gap >= (r - 1) * ld + wide:
+            continue
+        if r > 1 and r2 > 1 and ld == ld2 and wide <= gap % ld <= ld - wide2:
+            continue
+        raise XmemError(f"{what}: shares memory with {name}, which is overwritten")
+
+
 def residual_norm_forward(residual, h=None, gate=None, scale=None, alpha: float = 1.0, post: str = "none", post_weight=None, post_bias=None,
                           pre: str = "rms", pre_weight=None, pre_bias=None, gate_activation: str = "none", eps: float = 1e-5,
                           save_stats: bool = False, in_place: bool = False, stream=None):
@@ -126,6 +144,8 @@ def residual_norm_forward(residual, h=None, gate=None, scale=None, alpha: float 
     for v, name in ((scale, "scale"), (post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"), (pre_bias, "pre_bias")):
         if v is not None:
             _vector(v, name, n, torch.float32, dev)
+    if in_place:
+        _apart(residual, "residual", h=h, gate=gate)
     with _on(dev, stream, residual, h, gate, scale, post_weight, post_bias, pre_weight, pre_bias) as on:
         out, ldo = (residual, ldr) if in_place or h is None else (residual.new_empty((t, n)), n)
         y = residual.new_empty((t, n)) if k2 else None
@@ -176,8 +196,10 @@ def residual_norm_backward(dy, dout, out, stats, h=None, gate=None, scale=None, 
         _no("post_weight, post_bias", "post", post_weight, post_bias)
     if not k2:
         _no("pre_weight, pre_bias", "pre", pre_weight, pre_bias)
-    if in_place and dout is None:
-        raise XmemError("in_place: dout is wanted")
+    if in_place:
+        if dout is None:
+            raise XmemError("in_place: dout is wanted")
+        _apart(dout, "dout", dy=dy, out=None if dy is None else out, h=h, gate=gate)
     vectors = (scale, post_weight, post_bias, pre_weight, pre_bias)
     for v, name in zip(vectors, ("scale", "post_weight", "post_bias", "pre_weight", "pre_bias")):
         if v is not None:
@@ -216,8 +238,8 @@ def embedding_forward(table, ids, scale: float = 1.0, padding_id: int | None = N
 def embedding_backward(dy, ids, vocab: int, scale: float = 1.0, padding_id: int | None = None, into=None, dtype=None, workspace=None,
                        stream=None):
     """The gradient [vocab, n] of ``embedding_forward``'s table for dy [t, n]: scale times the sum of each token's rows, in 32 bits and
-    a fixed order.  Tokens equal to padding_id or outside [0, vocab) add nothing.  It is of dy's type, or float32 with ``dtype``; with ``into`` (either type, rows may be strided) it is added to
-    that, which is returned."""
+    a fixed order.  Tokens equal to padding_id or outside [0, vocab) add nothing.  It is of dy's type, or float32 with ``dtype``; with
+    ``into`` (either type, rows may be strided) it is added to that, which is returned."""
     import torch
     load_ops()
     code, dev, lddy = _dtype(dy, "dy", _ANY), dy.device, _matrix(dy, "dy")
@@ -230,6 +252,8 @@ def embedding_backward(dy, ids, vocab: int, scale: float = 1.0, padding_id: int 
     ldd = n if into is None else _matrix(into, "into", vocab, n, dtype, dev)
     if vocab < 1:
         raise XmemError("vocab: at least 1 is wanted")
+    if into is not None:
+        _apart(into, "into", dy=dy)
     with _on(dev, stream, dy, ids, into, workspace) as on:
         out = torch.empty((vocab, n), dtype=dtype, device=dev) if into is None else into
         workspace, size = _workspace(workspace, xmem_embedding_backward_workspace_bytes(t, vocab, n), dev)

@@ -108,6 +108,30 @@ def test_no_call_drops_a_gradient():
     torch.cuda.synchronize()
 
 
+def test_outputs_over_other_inputs_are_refused():
+    """What a call overwrites shares no element with what else it reads; the halves of one matrix are apart."""
+    g = torch.Generator().manual_seed(12)
+    both, other = torch.randn(6, 48, generator=g).cuda(), torch.randn(6, 24, generator=g).cuda()
+    a, b, c = both[:, :24], both[:, 24:], both[:, 16:40]
+    stats, ids = torch.ones(4, 6, device="cuda"), torch.tensor([3, 1, 3], device="cuda")
+    for call in (lambda x, y: xm.residual_norm_forward(x, y, in_place=True), lambda x, y: xm.residual_norm_forward(x, other, y, in_place=True),
+                 lambda x, y: xm.residual_norm_backward(y, x, other, stats, in_place=True),
+                 lambda x, y: xm.residual_norm_backward(other, x, y, stats, in_place=True),
+                 lambda x, y: xm.residual_norm_backward(other, x, other, stats, y, in_place=True),
+                 lambda x, y: xm.residual_norm_backward(other, x, other, stats, other, y, in_place=True),
+                 lambda x, y: xm.embedding_backward(y[2:5], ids, 6, into=x)):
+        for x, y in ((a, a), (a, c), (c, a), (c, b), (both.view(12, 24)[:6], both.view(12, 24)[2:8])):
+            before = both.clone()
+            with pytest.raises(xm.XmemError, match="shares memory"):
+                call(x, y)
+            assert torch.equal(both, before)
+        for x, y in ((a, b), (b, a)):
+            call(x, y)
+            both.copy_(before)
+    want = xm.residual_norm_forward(a.clone(), b.clone())[0]
+    assert torch.equal(xm.residual_norm_forward(a, b, in_place=True)[0], want) and torch.equal(a, want) and torch.equal(b, before[:, 24:])
+
+
 def test_overwritten_inputs_are_seen_by_autograd():
     """A graph that saved what a call overwrites raises instead of using the new values; one that saved what is only read does not."""
     g = torch.Generator().manual_seed(5)
