@@ -6,9 +6,9 @@
 // scaling adds up all shares for itself, which saves a launch between the two.  A gradient is looked at from the 16-byte boundary
 // before it, so that its loads are aligned wherever it begins.
 //
-// Bound by memory: the norm has to be known before the first gradient is written, so all are read twice.  147 gradients of 2.03 GB: squares 362 us
-// (5.6 TB/s), scaling 747 (4.05 GB, 5.4 TB/s).  The scaling begins with the last gradients, which the caches may still hold; with the
-// first ones 8 us more.  27 gradients of 5 MB take 4.6 and 6.6.
+// Bound by memory: the norm has to be known before the first gradient is written, so all are read twice.  147 gradients of 2.03 GB:
+// squares 362 to 384 us by the card (5.3 to 5.6 TB/s), scaling 747 to 761 (4.05 GB, 5.4 TB/s).  The scaling begins with the last gradients,
+// which the caches may still hold; with the first ones 8 us more.  27 gradients of 5 MB take 4.6 and 6.6.
 #include <math.h>
 
 #include <algorithm>

@@ -9,9 +9,9 @@
 // and dy, times what a column has in common: a workgroup goes over rows with its threads on the same columns, keeps their sums, and writes
 // one part a workgroup; k_norm_sums adds the parts up in order.
 //
-// Bound by memory.  Forward, bfloat16, both norms, gate, scale: 32768 x 4096 258 us (5.2 TB/s of 1.34 GB; a large copy reaches 4.9).
-// Backward of the same 426 and 9 (2.15 GB, 5.0 TB/s), 8192 x 2048 55.4 and 6.3 (268 MB, 4.8 TB/s; with means and biases 60 and 9).  Wide
-// gradients are not: 4096 x 16384 288 and 8 (1.07 GB, 3.7 TB/s): one workgroup a CU, whose second loads wait for its first sums.
+// Bound by memory.  Forward, bfloat16, both norms, gate, scale: 32768 x 4096 256 to 274 us by the card (4.9 to 5.2 TB/s of 1.34 GB; a large
+// copy reaches 4.9).  Backward of the same 426 and 9 (2.15 GB, 5.0 TB/s), 8192 x 2048 56 and 6.3 (268 MB, 4.8 TB/s; with means and biases 60
+// and 9).  Wide gradients are not: 4096 x 16384 288 and 8 (1.07 GB, 3.7 TB/s): one workgroup a CU, whose second loads wait for its first sums.
 // One row of 2048 takes 2.4 us, of which a launch is 2.1.
 #include "rows.h"
 
