@@ -7,8 +7,8 @@
 // in registers, in a fixed order and without atomics on numbers, and written once; rows without a token are cleared beside that.  A frequent
 // token may have thousands of rows of dy and most have one or two, so wavefronts take equal runs of the sorted list, whoever's they are
 // (k_sum), and rows that go past two runs are joined from 32-bit parts (k_join).
-// 32768 x 2048 into 50304 rows in bfloat16, tokens by 1 / (rank + 1): k_group 19 us, k_sum 44, k_join 6.6 (340 MB in all: 70 at a large copy's
-// rate).  8192 x 1024 added to float32: 8.2, 17.5 and 4.2, each bound by the latency of what it reads one after another.
+// 32768 x 2048 into 50304 rows in bfloat16, tokens by 1 / (rank + 1): k_group 19 us, k_sum 44, k_join 6.6 (340 MB in all: 69 at a large copy's
+// rate).  8192 x 1024 added to float32: 8.2, 12.8 and 4.4, each bound by the latency of what it reads one after another.
 // Few tokens of a small table take one launch (k_scan), in which each row of the table looks at all of them: 37 x 515 4.9 us.
 #include "rows.h"
 
@@ -202,9 +202,11 @@ __global__ __launch_bounds__(256) void k_scan(TableGrad p) {
 // the group, so that frequent tokens (whose numbers are often neighbours) do not meet in one.  256 groups or more, one a CU (of 64 and
 // 128 the grouping of 32768 tokens took 27.6 and 23.3 us where it took 21.7).
 constexpr int kGroups = 256, kKeyBits = 10, kKeys = 1 << kKeyBits, kWaves = 16;
-// Entries of the sorted list that one wavefront adds up.  32768 x 2048: sums and joins 75 us, with 8 entries 88, with 32 80; 8192 x 1024,
-// added: 20.8, 18.6 and 30.1.
-constexpr int kRun = 16;
+// Entries of the sorted list that one wavefront adds up: 8 where few tokens are added to a gradient, each row of which is read first, else
+// 16.  Sums and joins in us, of 16 and 8: added, 8192 x 1024 19.7 and 17.4, 4096 x 256 14.5 and 11.1, 16384 x 1024 24.9 and 25.6, 32768 x 2048
+// 61 and 67; written, 8192 x 1024 22.7 and 25.1, 32768 x 2048 50 and 64.  32 are slower in all of them.
+constexpr int kRun = 16, kShortRun = 8;
+constexpr int64_t kShortTokens = 16384;  // fewer
 
 struct Groups {
   int bits, low;  // of a key, and of its place in the group
@@ -227,7 +229,7 @@ Groups groups_of(int64_t vocab) {
 
 struct Lists {
   int *token, *row;  // sorted: tokens of one row together and in their order
-  int* count;        // entries, and rows that go past two runs of kRun entries
+  int* count;        // entries, and rows that go past two runs
   int* state;        // of a run, see k_sum
   int* begin;        // the runs in which those rows begin, in any order
   uint64_t* empty;   // a bit for each key whose row is in the table and has no token
@@ -242,7 +244,7 @@ Lists carve(void* base, int64_t t, const Groups& groups, int64_t n) {
     at += up256(b);
     return r;
   };
-  const int64_t runs = (t + kRun - 1) / kRun;
+  const int64_t shortest = t < kShortTokens ? kShortRun : kRun, runs = (t + shortest - 1) / shortest;
   w.token = reinterpret_cast<int*>(take(size_t(t) * 4));
   w.row = reinterpret_cast<int*>(take(size_t(t) * 4));
   w.count = reinterpret_cast<int*>(take(8));
@@ -411,10 +413,12 @@ constexpr int kBegins = 1, kPasses = 2;
 // the run and ends in the next is finished here, and left out there.  A longer one leaves its part in part row 2 r + 1 where it
 // begins and in 2 r where it goes on or ends.  The next entries' loads are on their way while a batch is added up.
 // Workgroups past the launch's `runs` clear the rows without a token, those of 64 keys at a time.
-// E: elements of a piece, one where rows have fewer than eight.
-template <class T, class O, bool ADD, int E>
+// E: elements of a piece, one where rows have fewer than eight.  In 16 bits eight, of what is added to a gradient four: its rows, which are
+// read first, may have 32 bits, and few tokens make more wavefronts.  Whole calls in us, of four and eight: added, 8192 x 1024 25.6 and 27.9,
+// 16384 x 1024 35.8 and 37.8; written, 8192 x 1024 29.5 and 30.6, 32768 x 2048 94 and 84, 32768 x 4096 179 and 163.
+template <class T, class O, bool ADD, int E, int RUN>
 __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists lists, int64_t first_run, unsigned runs, Clear clear) {
-  constexpr int U = ADD ? 4 : 8;
+  constexpr int U = 4;
   if (!ADD && blockIdx.x >= runs) {
     const unsigned words = unsigned(groups.words());
     const int64_t all = groups.count() * words, step = int64_t(gridDim.x - runs) * gridDim.y;
@@ -430,24 +434,24 @@ __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists l
     return;
   }
   const int lane = threadIdx.x & 63;
-  const int64_t run = first_run + blockIdx.x, start = run * kRun, count = *lists.count;
+  const int64_t run = first_run + blockIdx.x, start = run * RUN, count = *lists.count;
   if (start >= count) return;
   const int row = start + lane < count ? lists.row[start + lane] : -1, token = start + lane < count ? lists.token[start + lane] : 0;
-  const int before = start > 0 ? lists.row[start - 1] : -1, earlier = start > kRun ? lists.row[start - kRun - 1] : -1;
-  const int after = start + 2 * kRun < count ? lists.row[start + 2 * kRun] : -1;
+  const int before = start > 0 ? lists.row[start - 1] : -1, earlier = start > RUN ? lists.row[start - RUN - 1] : -1;
+  const int after = start + 2 * RUN < count ? lists.row[start + 2 * RUN] : -1;
   const auto row_at = [&](int e) { return __builtin_amdgcn_readlane(row, e); };
-  const int head = row_at(0), tail = row_at(kRun - 1);
-  const bool on = tail >= 0 && tail == row_at(kRun);  // the run's last row goes on
+  const int head = row_at(0), tail = row_at(RUN - 1);
+  const bool on = tail >= 0 && tail == row_at(RUN);  // the run's last row goes on
   const bool open = head == before, passes = open && on && head == tail, part = open && (passes || head == earlier);
-  int begin = 0, end = int(count - start < kRun ? count - start : kRun);
+  int begin = 0, end = int(count - start < RUN ? count - start : RUN);
   if (open && !part) begin = __builtin_ctzll(__ballot(row != head));
   int state = passes ? kPasses : 0;
   if (on && !passes) {
-    if (tail == row_at(2 * kRun - 1) && tail == after) {
+    if (tail == row_at(2 * RUN - 1) && tail == after) {
       state = kBegins;
     } else {
-      const uint64_t other = __ballot(row != tail) >> kRun;
-      end = other ? kRun + __builtin_ctzll(other) : 2 * kRun;
+      const uint64_t other = __ballot(row != tail) >> RUN;
+      end = other ? RUN + __builtin_ctzll(other) : 2 * RUN;
     }
   }
   // entries that are their row's last here
@@ -511,15 +515,15 @@ __global__ __launch_bounds__(256) void k_sum(TableGrad p, Groups groups, Lists l
 }
 
 // The parts of the rows that went past two runs, added up in order: four wavefronts a share of them each, then their sums.
-template <class O, int E>
+template <class O, int E, int RUN>
 __global__ __launch_bounds__(256) void k_join(TableGrad p, Lists lists) {
   constexpr int U = 8;
   __shared__ __attribute__((aligned(16))) float sums[3][64][E];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t runs = (*lists.count + kRun - 1) / kRun, rows = lists.count[1];
+  const int64_t runs = (*lists.count + RUN - 1) / RUN, rows = lists.count[1];
   const int64_t pieces = (p.n + E - 1) / E, slabs = (pieces + 63) / 64;
   for (int64_t item = blockIdx.x; item < rows * slabs; item += gridDim.x) {
-    const int64_t run = lists.begin[item / slabs], slab = item % slabs, row = lists.row[run * kRun + kRun - 1];
+    const int64_t run = lists.begin[item / slabs], slab = item % slabs, row = lists.row[run * RUN + RUN - 1];
     int64_t last = run + 1;  // the run in which the row ends
     for (;;) {
       const uint64_t which = __ballot(last + lane >= runs || lists.state[last + lane] != kPasses);
@@ -570,21 +574,31 @@ inline bool scans(int64_t t, int64_t vocab, int64_t n) {
   return t <= kFewTokens && (vocab + 3) / 4 * ((n + 511) / 512) <= kFewItems;
 }
 
-template <class T, class O, bool ADD, int E>
-void launch_sums(const TableGrad& p, const Groups& groups, const Lists& lists, const Clear& clear, hipStream_t st) {
+template <class T, class O, bool ADD, int E, int RUN>
+void launch_runs(const TableGrad& p, const Groups& groups, const Lists& lists, const Clear& clear, hipStream_t st) {
   constexpr int J = E == 1 ? 1 : 4;  // columns of a lane in the joins
-  const int64_t runs = (p.t + kRun - 1) / kRun, most = int64_t(1) << 19;
+  const int64_t runs = (p.t + RUN - 1) / RUN, most = int64_t(1) << 19;
   const int64_t slabs = ((p.n + E - 1) / E + 63) / 64, four = (slabs + 3) / 4, high = four < 8 ? four : 8;
   for (int64_t first = 0; first == 0 || first < runs; first += most) {  // no tokens: the table is cleared all the same
     const int64_t here = runs - first < most ? runs - first : most, words = (groups.count() * groups.words() + high - 1) / high;
     const int64_t beside = ADD || first || clear.early == 0 ? 0 : words < most ? words : most;
     if (here + beside > 0)
-      k_sum<T, O, ADD, E><<<dim3(unsigned(here + beside), unsigned(high)), 256, 0, st>>>(p, groups, lists, first, unsigned(here), clear);
+      k_sum<T, O, ADD, E, RUN><<<dim3(unsigned(here + beside), unsigned(high)), 256, 0, st>>>(p, groups, lists, first, unsigned(here), clear);
   }
   if (runs > 2) {
     const int64_t items = (runs - 2) * ((p.n + 64 * J - 1) / (64 * J));
-    k_join<O, J><<<unsigned(items < 2048 ? items : 2048), 256, 0, st>>>(p, lists);
+    k_join<O, J, RUN><<<unsigned(items < 2048 ? items : 2048), 256, 0, st>>>(p, lists);
   }
+}
+
+template <class T, class O, bool WHOLE>
+void launch_sums(const TableGrad& p, const Groups& groups, const Lists& lists, const Clear& clear, hipStream_t st) {
+  if (!p.add)
+    launch_runs<T, O, false, WHOLE ? kPiece<T> : 1, kRun>(p, groups, lists, clear, st);
+  else if (p.t < kShortTokens)
+    launch_runs<T, O, true, WHOLE ? 4 : 1, kShortRun>(p, groups, lists, clear, st);
+  else
+    launch_runs<T, O, true, WHOLE ? 4 : 1, kRun>(p, groups, lists, clear, st);
 }
 
 template <class T, class O>
@@ -604,21 +618,16 @@ int launch_grad(const TableGrad& p, void* workspace, hipStream_t st) {
   const unsigned vocab = unsigned(p.vocab), padding = p.padding >= 0 && p.padding < p.vocab ? unsigned(p.padding) : ~0u;
   const int64_t share = (p.t + kWaves - 1) / kWaves;
   const int notes = share >= 4096 ? 1024 : share >= 256 ? int(share / 4) : 64;
-  // Grouping many tokens leaves the memory idle for as long as it takes to clear 1,500 bytes a token: 32768 x 2048 88.5 us without, 85.1
-  // with, 86.3 with 2,500.  With 8192 tokens it is not worth the rows that are then written twice (31.0, 32.1).
+  // Grouping many tokens leaves the memory idle for as long as it takes to clear 1,500 bytes a token: 32768 x 2048 88.3 us without, 84.1
+  // with, 85.5 with 2,500.  With 8192 tokens it is not worth the rows that are then written twice (31.0, 32.1).
   const int64_t row = p.n * int64_t(sizeof(O)), early = p.add || p.t < 16384 ? 0 : p.t * 1500 / row;
   const Clear clear{static_cast<char*>(p.out), row, p.ldd * int64_t(sizeof(O)), early < p.vocab ? p.vocab - early : 0, p.vocab, p.past_caches};
   const unsigned grid = unsigned(groups.count()) + (early ? kCus : 0);
   k_group<<<grid, kWaves * 64, size_t(kWaves) * ((1 << groups.low) + notes) * 4, st>>>(p.ids, p.t, vocab, padding, groups, lists, notes, clear);
-  constexpr int E = kPiece<T>;
-  if (p.n < 8 && p.add)
-    launch_sums<T, O, true, 1>(p, groups, lists, clear, st);
-  else if (p.n < 8)
-    launch_sums<T, O, false, 1>(p, groups, lists, clear, st);
-  else if (p.add)
-    launch_sums<T, O, true, E>(p, groups, lists, clear, st);
+  if (p.n < 8)
+    launch_sums<T, O, false>(p, groups, lists, clear, st);
   else
-    launch_sums<T, O, false, E>(p, groups, lists, clear, st);
+    launch_sums<T, O, true>(p, groups, lists, clear, st);
   return launched();
 }
 
