@@ -422,7 +422,9 @@ __global__ __launch_bounds__(BLOCK, 4) void k_norm_back(NormGrads p) {
       }
     // elements that two wavefronts have are read by both before one writes them
     if (W > kWave && !p.dy && p.dr == p.dout) __syncthreads();
-    const Piece<T> q{p, p.stats[at], p.stats[p.t + at], p.stats[2 * p.t + at], p.stats[3 * p.t + at]};
+    // Of a row that is not there they are 0 too: another row's mean times its rho may pass 32 bits, and 0 times that is NaN.
+    const auto stat = [&](int i) { return R == 1 || here ? p.stats[i * p.t + at] : 0.0f; };
+    const Piece<T> q{p, stat(0), stat(1), stat(2), stat(3)};
     float s1 = 0.0f, s2 = 0.0f;
     if (p.dy) {
       float e[E], hat[E], dy[E], w[E];
