@@ -561,6 +561,8 @@ __global__ __launch_bounds__(1024) void k_norm_back_any(NormGrads p) {
 #pragma unroll
         for (int k = 0; k < E; ++k) v[k] *= p.alpha;
     };
+    // behind the row's end xhat is what is left of 0, which may pass 32 bits: 0 times that is no 0
+    const auto product = [&](int64_t i, int k, const float (&v)[E], const float (&xhat)[E]) { return i * E + k < n ? v[k] * xhat[k] : 0.0f; };
     const Piece<T> q{p, p.stats[t], p.stats[p.t + t], p.stats[2 * p.t + t], p.stats[3 * p.t + t]};
     float s1 = 0.0f, s2 = 0.0f, s3 = 0.0f, s4 = 0.0f, e[E], hat[E], dy[E], d[E], b[E], f[E], dg[E], s[E], w[E], add[E];
     if (p.dy) {
@@ -569,7 +571,7 @@ __global__ __launch_bounds__(1024) void k_norm_back_any(NormGrads p) {
         q.first(row(p.dy, p.lddy, i), row(p.out, p.ldo, i), w, e, hat, dy);
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-          s1 += e[k] * hat[k];
+          s1 += product(i, k, e, hat);
           s2 += e[k];
         }
       }
@@ -599,7 +601,7 @@ __global__ __launch_bounds__(1024) void k_norm_back_any(NormGrads p) {
 #pragma unroll
         for (int k = 0; k < E; ++k) {
           if (i * E + k >= n) f[k] = 0.0f;
-          s3 += f[k] * hat[k];
+          s3 += product(i, k, f, hat);
           s4 += f[k];
         }
       }

@@ -1,5 +1,6 @@
 """Norm gradients of a batch in which a row lies far out, so that its mean times its reciprocal deviation passes 32 bits while the
-row's own normed values are 0: a row that a workgroup takes but the batch does not have is not multiplied with it."""
+row's own normed values are 0: a row that a workgroup takes but the batch does not have is not multiplied with it, nor is what lies
+behind a row's end."""
 import pytest
 import torch
 
@@ -56,4 +57,12 @@ def check(t, n, dtype, seed):
 def test_rows_that_are_not_there(n, dtype):
     """Widths of which a workgroup takes several rows, and batches that do not fill it."""
     for t in (2, 3, 65):
+        check(t, n, dtype, n + t)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FF])
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 7, 16391, 32775])
+def test_elements_behind_a_row(n, dtype):
+    """Rows shorter than a piece, and long ones that end inside one."""
+    for t in (1, 2, 5):
         check(t, n, dtype, n + t)
