@@ -92,9 +92,9 @@ int xmem_embedding_forward(const void* d_table, int64_t ldt, const int64_t* d_id
 /* Workspace of xmem_embedding_backward.  0 for invalid sizes; it may be 0 otherwise too. */
 size_t xmem_embedding_backward_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width);
 
-/* dtable_v = scale * (the sum of dy_t over the tokens t with id_t = v), added to what d_dtable holds where add is not 0
- * (rows that no token names are not looked at then).  Sums are in 32 bits, in a fixed order, and rounded once.
- * Tokens equal to padding_id and tokens outside [0, vocab) add nothing.
+/* dtable_v = scale * (the sum of dy_t over the tokens t with id_t = v), added to what d_dtable holds where add is not 0.
+ * Rows that no token names are not looked at then, and are 0 without it, whatever scale is.  Sums are in 32 bits, in a fixed
+ * order, and rounded once.  Tokens equal to padding_id and tokens outside [0, vocab) add nothing and name no row.
  *   d_dy    : [tokens, width] of dtype, rows lddy apart
  *   d_dtable: [vocab, width] of dtype or of XMEM_F32 (out_dtype), rows ldd apart, written
  *   d_workspace: >= its size, 256-byte aligned

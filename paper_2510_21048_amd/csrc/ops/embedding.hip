@@ -188,8 +188,9 @@ __global__ __launch_bounds__(256) void k_scan(TableGrad p) {
       O o[E];
       if (p.add) __builtin_memcpy(o, out, sizeof(o));
       wave_sync();  // elements that two lanes have are read by both before one writes them
+      const float scale = any ? p.scale : 0.0f;  // of no token nothing is scaled: 0 times a factor that is not finite is NaN
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = O(p.add ? float(o[e]) + p.scale * total[e] : p.scale * total[e]);
+      for (int e = 0; e < E; ++e) o[e] = O(p.add ? float(o[e]) + scale * total[e] : scale * total[e]);
       __builtin_memcpy(out, o, sizeof(o));
     }
     __syncthreads();
