@@ -53,7 +53,7 @@ int xmem_residual_norm_forward(const void* d_r, int64_t ldr, const void* d_h, in
                                int dtype, void* d_out, int64_t ldo, void* d_y, int64_t ldy, float* d_stats, void* hip_stream);
 
 /* Workspace of xmem_residual_norm_backward: partial sums of the vectors' gradients (none of these wanted: it may be 0
- * bytes and NULL).  0 for invalid sizes and for 0 tokens. */
+ * bytes and NULL).  0 for invalid sizes and for 0 tokens.  It never shrinks with more tokens. */
 size_t xmem_residual_norm_backward_workspace_bytes(int64_t tokens, int64_t width, int dtype);
 
 /* The gradients of xmem_residual_norm_forward, for dy of y and dout of out (what comes to the sum past y).
@@ -89,7 +89,8 @@ int xmem_residual_norm_backward(const void* d_dy, int64_t lddy, const void* d_do
 int xmem_embedding_forward(const void* d_table, int64_t ldt, const int64_t* d_ids, int64_t tokens, int64_t vocab, int64_t width,
                            int dtype, float scale, int64_t padding_id, void* d_y, int64_t ldy, void* hip_stream);
 
-/* Workspace of xmem_embedding_backward.  0 for invalid sizes; it may be 0 otherwise too. */
+/* Workspace of xmem_embedding_backward, whether it adds or not.  0 for invalid sizes; it may be 0 otherwise too.  It never shrinks with
+ * more tokens: that of the largest batch holds every smaller one of the same table. */
 size_t xmem_embedding_backward_workspace_bytes(int64_t tokens, int64_t vocab, int64_t width);
 
 /* dtable_v = scale * (the sum of dy_t over the tokens t with id_t = v), added to what d_dtable holds where add is not 0.

@@ -245,7 +245,9 @@ Lists carve(void* base, int64_t t, const Groups& groups, int64_t n) {
     at += up256(b);
     return r;
   };
-  const int64_t shortest = t < kShortTokens ? kShortRun : kRun, runs = (t + shortest - 1) / shortest;
+  // room for the runs of any batch of so many tokens or fewer: few tokens may make more runs
+  const int64_t few = ((t < kShortTokens ? t : kShortTokens - 1) + kShortRun - 1) / kShortRun, many = (t + kRun - 1) / kRun;
+  const int64_t runs = few > many ? few : many;
   w.token = reinterpret_cast<int*>(take(size_t(t) * 4));
   w.row = reinterpret_cast<int*>(take(size_t(t) * 4));
   w.count = reinterpret_cast<int*>(take(8));
