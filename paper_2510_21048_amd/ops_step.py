@@ -97,16 +97,25 @@ def _no(what: str, why: str, *given) -> None:
             raise XmemError(f"{what}: not without {why}")
 
 
+def _rows(t):
+    """First byte, bytes of a row, from row to row, and rows of a matrix or of what lies in one piece."""
+    if t.is_contiguous():
+        return t.data_ptr(), t.nbytes, t.nbytes, 1
+    (r, c), size = t.shape, t.element_size()
+    return t.data_ptr(), c * size, t.stride(0) * size, r
+
+
 def _apart(over, name: str, **read) -> None:
     """Refuses tensors that a call reads while it writes `over`: their rows may lie between its rows (halves of one matrix), not on them."""
-    def rows(t):  # first byte, bytes of a row, from row to row, rows
-        (r, c), size = t.shape, t.element_size()
-        return t.data_ptr(), c * size, (t.stride(0) if r > 1 else c) * size, r
-
+    mine = _rows(over)
+    begin, end = mine[0], mine[0] + (mine[3] - 1) * mine[2] + mine[1]
     for what, t in read.items():
-        if t is None or not t.numel() or not over.numel():
+        if t is None:
             continue
-        (at, wide, ld, r), (at2, wide2, ld2, r2) = sorted((rows(over), rows(t)))
+        first = t.data_ptr()
+        if first >= end or (first + t.nbytes <= begin and t.is_contiguous()) or not t.numel() or begin == end:  # most are far away
+            continue
+        (at, wide, ld, r), (at2, wide2, ld2, r2) = sorted((mine, _rows(t)))
         gap = at2 - at
         if gap >= (r - 1) * ld + wide:
             continue
@@ -144,8 +153,9 @@ def residual_norm_forward(residual, h=None, gate=None, scale=None, alpha: float 
     for v, name in ((scale, "scale"), (post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"), (pre_bias, "pre_bias")):
         if v is not None:
             _vector(v, name, n, torch.float32, dev)
-    if in_place:
-        _apart(residual, "residual", h=h, gate=gate)
+    if in_place and h is not None:
+        _apart(residual, "residual", h=h, gate=gate, scale=scale, post_weight=post_weight, post_bias=post_bias, pre_weight=pre_weight,
+               pre_bias=pre_bias)
     with _on(dev, stream, residual, h, gate, scale, post_weight, post_bias, pre_weight, pre_bias) as on:
         out, ldo = (residual, ldr) if in_place or h is None else (residual.new_empty((t, n)), n)
         y = residual.new_empty((t, n)) if k2 else None
@@ -196,14 +206,15 @@ def residual_norm_backward(dy, dout, out, stats, h=None, gate=None, scale=None, 
         _no("post_weight, post_bias", "post", post_weight, post_bias)
     if not k2:
         _no("pre_weight, pre_bias", "pre", pre_weight, pre_bias)
-    if in_place:
-        if dout is None:
-            raise XmemError("in_place: dout is wanted")
-        _apart(dout, "dout", dy=dy, out=None if dy is None else out, h=h, gate=gate)
+    if in_place and dout is None:
+        raise XmemError("in_place: dout is wanted")
     vectors = (scale, post_weight, post_bias, pre_weight, pre_bias)
     for v, name in zip(vectors, ("scale", "post_weight", "post_bias", "pre_weight", "pre_bias")):
         if v is not None:
             _vector(v, name, n, torch.float32, dev)
+    if in_place:
+        _apart(dout, "dout", dy=dy, out=None if dy is None else out, stats=stats, h=h, gate=gate, scale=scale, post_weight=post_weight,
+               post_bias=post_bias, pre_weight=pre_weight, pre_bias=pre_bias)
     with _on(dev, stream, dy, dout, out, stats, h, gate, *vectors, workspace) as on:
         dr, lddr = (dout, lddo) if in_place else (first.new_empty((t, n)), n)
         dh = None if h is None else first.new_empty((t, n))
@@ -253,7 +264,7 @@ def embedding_backward(dy, ids, vocab: int, scale: float = 1.0, padding_id: int 
     if vocab < 1:
         raise XmemError("vocab: at least 1 is wanted")
     if into is not None:
-        _apart(into, "into", dy=dy)
+        _apart(into, "into", dy=dy, ids=ids)
     with _on(dev, stream, dy, ids, into, workspace) as on:
         out = torch.empty((vocab, n), dtype=dtype, device=dev) if into is None else into
         workspace, size = _workspace(workspace, xmem_embedding_backward_workspace_bytes(t, vocab, n), dev)

@@ -26,3 +26,35 @@ def test_one_workspace_for_every_smaller_batch(add):
         assert bool((hold[need:] == 255).all())
         want = xm.embedding_backward(dy[:t], ids[:t], vocab, 0.5, into=torch.ones(vocab, n, device="cuda") if add else None, dtype=FF)
         assert torch.equal(got, want)
+
+
+def test_vectors_and_tokens_in_what_is_overwritten_are_refused():
+    """Scale, weights, biases, statistics or tokens that lie in what a call overwrites: refused before anything is written."""
+    n = 24
+    flat = torch.randn(2000, device="cuda")
+    over, before = flat[200:680].view(10, 48)[:, :n], flat.clone()
+    other, w = torch.randn(10, n, device="cuda"), torch.randn(n, device="cuda")
+    stats, ids = torch.ones(4, 10, device="cuda"), torch.arange(10, device="cuda")
+    inside, behind = flat[248:272], flat[700:724]
+    forward = lambda **how: xm.residual_norm_forward(over, other, in_place=True, **dict(dict(post="layer", pre="layer"), **how))
+    backward = lambda **how: xm.residual_norm_backward(other, over, other, how.pop("stats", stats), other, in_place=True,
+                                                       **dict(dict(post="layer", pre="layer"), **how))
+    for name in ("scale", "post_weight", "post_bias", "pre_weight", "pre_bias"):
+        for call in (forward, backward):
+            with pytest.raises(xm.XmemError, match=name + ": shares memory"):
+                call(**{name: inside})
+            assert torch.equal(flat, before)
+            call(**{name: w})
+            flat.copy_(before)
+            call(**{name: behind})
+            flat.copy_(before)
+    with pytest.raises(xm.XmemError, match="stats: shares memory"):
+        backward(stats=flat[170:210].view(4, 10))
+    mine = flat[600:620].view(torch.int64)
+    with pytest.raises(xm.XmemError, match="ids: shares memory"):
+        xm.embedding_backward(other, mine, 10, into=over)
+    torch.cuda.synchronize()
+    assert torch.equal(flat, before)
+    xm.embedding_backward(other, ids, 10, into=over)
+    torch.cuda.synchronize()
+    assert torch.equal(over, before[200:680].view(10, 48)[:, :n] + other)
