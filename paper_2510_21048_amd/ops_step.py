@@ -119,7 +119,7 @@ def _apart(over, name: str, **read) -> None:
         gap = at2 - at
         if gap >= (r - 1) * ld + wide:
             continue
-        if r > 1 and r2 > 1 and ld == ld2 and wide <= gap % ld <= ld - wide2:
+        if r > 1 and (r2 == 1 or ld == ld2) and wide <= gap % ld <= ld - wide2:
             continue
         raise XmemError(f"{what}: shares memory with {name}, which is overwritten")
 

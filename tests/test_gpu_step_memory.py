@@ -58,3 +58,21 @@ def test_vectors_and_tokens_in_what_is_overwritten_are_refused():
     xm.embedding_backward(other, ids, 10, into=over)
     torch.cuda.synchronize()
     assert torch.equal(over, before[200:680].view(10, 48)[:, :n] + other)
+
+
+def test_one_row_between_the_rows_that_are_overwritten_is_taken():
+    """A single token's row of dy, and vectors, between the rows of what a call overwrites: the bits of copies elsewhere."""
+    n = 24
+    flat = torch.randn(500, device="cuda")
+    over, between, before = flat[:480].view(10, 48)[:, :n], flat[24:48], flat.clone()
+    one = torch.tensor([3], device="cuda")
+    want = xm.embedding_backward(between.clone().view(1, n), one, 10, into=over.clone())
+    got = xm.embedding_backward(between.view(1, n), one, 10, into=over)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(between, before[24:48])
+    flat.copy_(before)
+    h = torch.randn(10, n, device="cuda")
+    want = xm.residual_norm_forward(over.clone(), h, scale=between.clone())
+    got = xm.residual_norm_forward(over, h, scale=between, in_place=True)
+    torch.cuda.synchronize()
+    assert got[0] is over and torch.equal(over, want[0]) and torch.equal(got[1], want[1]) and torch.equal(between, before[24:48])

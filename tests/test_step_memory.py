@@ -60,3 +60,18 @@ def test_what_is_overwritten_is_apart_from_every_input():
         else:
             with pytest.raises(xm.XmemError, match="shares memory"):
                 _apart(a, "over", x=b)
+
+
+def test_what_lies_between_two_rows_is_apart():
+    """One row, a vector or a whole small matrix in the gap between two rows of what is overwritten, up to both of its ends."""
+    flat = torch.zeros(1000)
+    over = flat[100:484].view(8, 48)[:, :24]
+    row = lambda at, n: flat[at:at + n]
+    for free in (row(124, 24), row(124, 1), row(147, 1), row(412, 24), row(130, 6), row(124, 24).view(1, 24), row(172, 24).view(4, 6),
+                 flat[124:].as_strided((1, 24), (1000, 1))):
+        _apart(over, "over", x=free)
+        _apart(free, "free", x=over)
+    for bad in (row(123, 25), row(123, 1), row(124, 25), row(148, 1), row(412, 25), row(172, 25).view(5, 5)):
+        for a, b in ((over, bad), (bad, over)):
+            with pytest.raises(xm.XmemError, match="shares memory"):
+                _apart(a, "over", x=b)
