@@ -67,8 +67,8 @@ size_t xmem_residual_norm_backward_workspace_bytes(int64_t tokens, int64_t width
  *   d_dgate: [tokens, width] of dtype, or NULL, written
  *   d_dscale, d_dw1, d_db1, d_dw2, d_db2 : float32 [width], or NULL, written
  *   d_workspace: >= its size, 256-byte aligned, where one of those five is wanted
- * tokens == 0 gives 0 for the five.  No output may overlap another operand (d_dr on d_dout apart).
- * Returns as the forward pass, or XMEM_EWORKSPACE. */
+ * tokens == 0 gives 0 for the five.  No output may overlap another operand (d_dr on d_dout apart); a workspace that does is refused.
+ * Returns as the forward pass, XMEM_EINVAL for a workspace that overlaps too, or XMEM_EWORKSPACE. */
 int xmem_residual_norm_backward(const void* d_dy, int64_t lddy, const void* d_dout, int64_t lddout, const void* d_out, int64_t ldo,
                                 const float* d_stats, const void* d_h, int64_t ldh, const void* d_gate, int64_t ldg,
                                 const float* d_scale, float alpha, int post, const float* d_w1, const float* d_b1, int pre,
@@ -99,7 +99,8 @@ size_t xmem_embedding_backward_workspace_bytes(int64_t tokens, int64_t vocab, in
  *   d_dy    : [tokens, width] of dtype, rows lddy apart
  *   d_dtable: [vocab, width] of dtype or of XMEM_F32 (out_dtype), rows ldd apart, written
  *   d_workspace: >= its size, 256-byte aligned
- * Returns as xmem_embedding_forward, or XMEM_EWORKSPACE. */
+ * d_dtable may overlap neither d_dy nor d_ids; a workspace that overlaps one of the three is refused.
+ * Returns as xmem_embedding_forward, XMEM_EINVAL for a workspace that overlaps too, or XMEM_EWORKSPACE. */
 int xmem_embedding_backward(const void* d_dy, int64_t lddy, const int64_t* d_ids, int64_t tokens, int64_t vocab, int64_t width,
                             int dtype, float scale, int64_t padding_id, int add, int out_dtype, void* d_dtable, int64_t ldd,
                             void* d_workspace, size_t workspace_bytes, void* hip_stream);
@@ -119,7 +120,7 @@ size_t xmem_clip_grad_norm_workspace_bytes(void);
  *   d_stats  : float32 [2], written: norm and factor
  *   d_workspace: >= its size, 256-byte aligned
  * Returns XMEM_OK, XMEM_EINVAL (null pointer, negative or too large count (2^31) or size (2^48), unknown type, max_norm
- * negative or NaN, scale negative or not finite, overlap), XMEM_EWORKSPACE or XMEM_EHIP. */
+ * negative or NaN, scale negative or not finite, overlap, a workspace on a gradient or on d_stats), XMEM_EWORKSPACE or XMEM_EHIP. */
 int xmem_clip_grad_norm(void* const* d_tensors, const int64_t* sizes, const int* dtypes, int64_t count, float max_norm, float scale,
                         float* d_stats, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 

@@ -248,7 +248,11 @@ int xmem_clip_grad_norm(void* const* d_tensors, const int64_t* sizes, const int*
   } catch (...) {  // no memory on the host
     return XMEM_EINVAL;
   }
-  if (!d_workspace || workspace_bytes < xmem_clip_grad_norm_workspace_bytes() || !aligned(d_workspace, 256)) return XMEM_EWORKSPACE;
+  const size_t need = xmem_clip_grad_norm_workspace_bytes();
+  if (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 256)) return XMEM_EWORKSPACE;
+  if (shares(d_workspace, need, d_stats, 1, 2, 2, 4)) return XMEM_EINVAL;
+  for (int64_t i = 0; i < count; ++i)
+    if (sizes[i] > 0 && shares(d_workspace, need, d_tensors[i], 1, sizes[i], sizes[i], bytes_of(dtypes[i]))) return XMEM_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   double* part = static_cast<double*>(d_workspace);
   const auto table = [&](size_t i) { return table_of(d_tensors, sizes, dtypes, count, launches[i].start); };

@@ -666,9 +666,13 @@ int xmem_embedding_backward(const void* d_dy, int64_t lddy, const int64_t* d_ids
   if (!d_dtable || (tokens > 0 && (!d_dy || !d_ids))) return XMEM_EINVAL;
   const size_t need = xmem_embedding_backward_workspace_bytes(tokens, vocab, width);
   if (need > 0 && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 256))) return XMEM_EWORKSPACE;
+  const int element = dtype == XMEM_F32 ? 4 : 2, out_element = out_dtype == XMEM_F32 ? 4 : 2;
+  if (shares(d_workspace, need, d_dy, tokens, lddy, width, element) || shares(d_workspace, need, d_ids, 1, tokens, tokens, 8) ||
+      shares(d_workspace, need, d_dtable, vocab, ldd, width, out_element))
+    return XMEM_EINVAL;
   // Clearing a table of 206 MB past the caches leaves them to the sums' reads (with them 64.8 us, past them 53.9); one of 103 MB
   // stays in the cache behind the L2s (18.2 and 21.9).
-  const bool past_caches = vocab * width * (out_dtype == XMEM_F32 ? 4 : 2) >= kCacheBytes / 2;
+  const bool past_caches = vocab * width * out_element >= kCacheBytes / 2;
   const TableGrad p{d_dy, lddy, d_ids, tokens, vocab, width, scale, padding_id, add != 0, d_dtable, ldd, past_caches};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (dtype == XMEM_F32) return launch_grad<float, float>(p, d_workspace, st);

@@ -820,9 +820,16 @@ int xmem_residual_norm_backward(const void* d_dy, int64_t lddy, const void* d_do
   }
   const bool sums = d_dscale || d_dw1 || d_db1 || d_dw2 || d_db2;
   const Plan q = plan_of(tokens, width, dtype);
-  if (sums && tokens > 0 &&
-      (!d_workspace || workspace_bytes < xmem_residual_norm_backward_workspace_bytes(tokens, width, dtype) || !aligned(d_workspace, 256)))
-    return XMEM_EWORKSPACE;
+  if (sums && tokens > 0) {
+    const size_t need = xmem_residual_norm_backward_workspace_bytes(tokens, width, dtype);
+    if (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 256)) return XMEM_EWORKSPACE;
+    for (const auto& m : all)
+      if (shares(d_workspace, need, m.at, tokens, m.ld, width, dtype == XMEM_F32 ? 4 : 2)) return XMEM_EINVAL;
+    const float* const vectors[] = {d_scale, d_w1, d_b1, d_w2, d_dscale, d_dw1, d_db1, d_dw2, d_db2};
+    for (const float* v : vectors)
+      if (shares(d_workspace, need, v, 1, width, width, 4)) return XMEM_EINVAL;
+    if (shares(d_workspace, need, d_stats, 4, tokens, tokens, 4)) return XMEM_EINVAL;
+  }
   if (tokens == 0 && !sums) return XMEM_OK;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   float* part = sums ? static_cast<float*>(d_workspace) : nullptr;

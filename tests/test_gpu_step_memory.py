@@ -76,3 +76,32 @@ def test_one_row_between_the_rows_that_are_overwritten_is_taken():
     got = xm.residual_norm_forward(over, h, scale=between, in_place=True)
     torch.cuda.synchronize()
     assert got[0] is over and torch.equal(over, want[0]) and torch.equal(got[1], want[1]) and torch.equal(between, before[24:48])
+
+
+def test_a_workspace_on_an_operand_is_refused():
+    """One that lies on an input or on what is overwritten: refused before anything is written, and taken beside them."""
+    g = torch.Generator().manual_seed(23)
+    t, n, vocab = 300, 72, 20000  # a table whose gradient needs a workspace
+    hold = torch.randn(1 << 21, generator=g).cuda()
+    before, raw = hold.clone(), hold.view(torch.uint8)
+    x, h, dy = hold[:t * n].view(t, n), hold[30000:30000 + t * n].view(t, n), hold[60000:60000 + t * n].view(t, n)
+    ids = torch.randint(0, vocab, (t,), generator=g).cuda()
+    out, _, stats = xm.residual_norm_forward(x, h, save_stats=True, pre_weight=hold[90000:90000 + n])
+    w, into, grads = hold[90000:90000 + n], hold[100000:100000 + vocab * n].view(vocab, n), [hold[:17], hold[500000:500100]]
+    calls = {"norms": (lambda ws: xm.residual_norm_backward(dy, None, out, stats, h, pre_weight=w, workspace=ws), (60000, 90000, 30000)),
+             "in place": (lambda ws: xm.residual_norm_backward(dy, x, out, stats, h, pre_weight=w, in_place=True, workspace=ws), (0, 60000, 90000)),
+             "table": (lambda ws: xm.embedding_backward(dy, ids, vocab, into=into, workspace=ws), (60000, 100000, 400000)),
+             "clip": (lambda ws: xm.clip_grad_norm(grads, 1.0, workspace=ws), (0, 500000))}
+    assert xm.xmem_embedding_backward_workspace_bytes(t, vocab, n) > 0
+    torch.cuda.synchronize()
+    for name, (call, at) in calls.items():
+        for a in at:
+            a = a // 64 * 64  # a 256-byte boundary
+            with pytest.raises(xm.XmemError):
+                call(raw[4 * a:4 * a + (1 << 20)])
+            torch.cuda.synchronize()
+            assert torch.equal(hold, before), name
+        log(f"[step] {name} with a workspace beside its operands")
+        call(torch.empty(1 << 22, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        hold.copy_(before)
