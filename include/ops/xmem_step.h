@@ -113,7 +113,7 @@ size_t xmem_clip_grad_norm_workspace_bytes(void);
  * With max_norm = INFINITY and scale = 1 the factor is 1: nothing but the norm is computed and no gradient is written.
  * A factor of 1 leaves the gradients as they are.  scale is what the gradients are to be multiplied with anyway (1 over a loss
  * scale, or over the number of batches that were added up).  Squares are added up in 64 bits.  A norm of NaN makes every
- * gradient NaN; where it is infinite they become 0, or NaN where infinite themselves.
+ * gradient NaN; where it is infinite they become 0, or NaN where infinite themselves (under an infinite limit the factor stays scale).
  *   d_tensors: host array of `count` device pointers; sizes, dtypes: host arrays of their elements and element types.
  *              All three are read before the call returns.  Elements of a gradient are contiguous and need no more than their
  *              own alignment.  Gradients that overlap are refused where they would be written.

@@ -7,8 +7,8 @@
 // before it, so that its loads are aligned wherever it begins.
 //
 // Bound by memory: the norm has to be known before the first gradient is written, so all are read twice.  147 gradients of 2.03 GB:
-// squares 362 to 384 us by the card (5.3 to 5.6 TB/s), scaling 747 to 761 (4.05 GB, 5.4 TB/s).  The scaling begins with the last gradients,
-// which the caches may still hold; with the first ones 8 us more.  27 gradients of 5 MB take 4.6 and 6.6.
+// squares 360 to 384 us by the card (5.3 to 5.6 TB/s), scaling 747 to 761 (4.05 GB, 5.4 TB/s).  The scaling begins with the last gradients,
+// which the caches may still hold; with the first ones 8 us more.  27 gradients of 5 MB take 4.6 and 7.2; 425 MB in float32 96 and 129.
 #include <math.h>
 
 #include <algorithm>
@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kTable = 128;          // gradients of a launch: two a lane
 constexpr int kThreads = 256;
-constexpr int kParts = 2048;         // workgroups of a norm at most, each with a sum of its own (500 MB in float32 70 us; with 1024 82)
+constexpr int kParts = 2048;         // workgroups of a norm at most, each with a sum of its own (425 MB in float32, partly in the caches, 70 us; with 1024 82)
 constexpr int kLoads = 4;            // of 16 bytes, a thread and piece of work
 constexpr int kSpan = kThreads * kLoads * 16;  // bytes of a piece of work
 constexpr int64_t kMostSize = int64_t(1) << 48;

@@ -8,7 +8,8 @@
 // token may have thousands of rows of dy and most have one or two, so wavefronts take equal runs of the sorted list, whoever's they are
 // (k_sum), and rows that go past two runs are joined from 32-bit parts (k_join).
 // 32768 x 2048 into 50304 rows in bfloat16, tokens by 1 / (rank + 1): k_group 19 us, k_sum 44, k_join 6.6 (340 MB in all: 69 at a large copy's
-// rate).  8192 x 1024 added to float32: 8.2, 12.8 and 4.4, each bound by the latency of what it reads one after another.
+// rate).  8192 x 1024 added to float32: 8.1, 13 and 4.4, each bound by the latency of what it reads one after another (k_sum the list's length,
+// then the places around its run, then dy).
 // Few tokens of a small table take one launch (k_scan), in which each row of the table looks at all of them: 37 x 515 4.9 us.
 #include "rows.h"
 

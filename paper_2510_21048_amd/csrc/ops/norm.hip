@@ -10,9 +10,13 @@
 // one part a workgroup; k_norm_sums adds the parts up in order.
 //
 // Bound by memory.  Forward, bfloat16, both norms, gate, scale: 32768 x 4096 256 to 274 us by the card (4.9 to 5.2 TB/s of 1.34 GB; a large
-// copy reaches 4.9).  Backward of the same 426 and 9 (2.15 GB, 5.0 TB/s), 8192 x 2048 56 and 6.3 (268 MB, 4.8 TB/s; with means and biases 60
-// and 9).  Wide gradients are not: 4096 x 16384 288 and 8 (1.07 GB, 3.7 TB/s): one workgroup a CU, whose second loads wait for its first sums.
-// One row of 2048 takes 2.4 us, of which a launch is 2.1.
+// copy reaches 4.9).  Backward of the same 426 and 9 (2.15 GB, 5.0 TB/s), 8192 x 2048 56 and 6.4 (268 MB, 4.8 TB/s; with means and biases 61
+// and 9; in float32 106 and 6, 108 and 9).  The norm alone 14 forward and 25 + 4.4 back (8192 x 2048).  One row of 2048 takes 2.4 us, of which a
+// launch is 2.1.
+// Wide gradients are not: 4096 x 16384 289 and 8 (1.07 GB, 3.7 TB/s), with means and biases 484 and 13; 2048 x 16384 in float32, no gate, 258 and 8, 430
+// and 13.  One workgroup a CU, whose second loads wait for its first sums, and 124 to 352 bytes a thread in scratch memory: at 1024 threads 240 bytes
+// are nearly as much as the row's eight values in 16 bits.  Narrow ones are far from the memory's rate (32768 x 40 3.3): 8.2 and 4.1, with means
+// and biases 13.4 and 4.2; the 16-bit forms below a wavefront keep up to 56 bytes of scratch.
 #include "rows.h"
 
 using namespace xops;
@@ -174,6 +178,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_norm(Norms p) {
 }
 
 // A row that no registers hold, or of less than a piece: its inputs are read again for each sum, and outputs written last (out may be r).
+// Short rows are right here, not fast, with a workgroup each: 32768 x 7 in bfloat16 431 us, where 32768 x 8 takes 5.0.
 template <class T>
 __global__ __launch_bounds__(1024) void k_norm_any(Norms p) {
   constexpr int E = kPiece<T>, THREADS = 1024;
@@ -341,7 +346,9 @@ __device__ inline float column_of(const NormGrads& p, int q, int64_t c) {
 // registers, half of them in LDS where they are four vectors' (BIASES), and all where a thread has more than eight columns of two.  The
 // vectors are in LDS too (a thread would spend 24 to 32 registers on them), those of rows past 1024 pieces in the L2s.  With more than
 // a piece a thread, what the first norm does not need is loaded after its sums.  128 registers, so that a CU has 16 wavefronts:
-// 131 made 8192 x 2048 74 us instead of 55.  Two workgroups of 512 a CU wait less for each other's sums than one of 1024 (55, 63); of
+// 131 made 8192 x 2048 74 us instead of 55.  What they do not hold goes to scratch memory: nothing from 64 to 512 threads a row and in
+// float32 below, up to 56 bytes a thread below in 16 bits, 40 and 48 at 1024 in 16 bits with biases, 124 and (with biases) 240 with two
+// pieces a thread in 16 bits, 160 and 352 with four in float32.  Two workgroups of 512 a CU wait less for each other's sums than one of 1024 (55, 63); of
 // 256 threads they write more parts (62 and 8.5 for the sums).
 template <class T, int W, int NCH, bool BIASES, int BLOCK>
 __global__ __launch_bounds__(BLOCK, 4) void k_norm_back(NormGrads p) {
@@ -545,6 +552,7 @@ __global__ __launch_bounds__(BLOCK, 4) void k_norm_back(NormGrads p) {
 }
 
 // Rows that no registers hold, or of less than a piece: each is read three times, and a workgroup's sums are kept where its parts go.
+// 32768 x 7 in bfloat16 take 1,290 us, where 32768 x 8 take 8.
 template <class T>
 __global__ __launch_bounds__(1024) void k_norm_back_any(NormGrads p) {
   constexpr int E = kPiece<T>, THREADS = 1024;

@@ -5,7 +5,8 @@ The functions named ``xmem_*`` mirror the C ABI one to one and take raw device p
 ``residual_norm_forward``, ``residual_norm_backward``, ``embedding_forward``, ``embedding_backward`` and
 ``clip_grad_norm`` check their tensors, allocate outputs and workspace with torch and run on the current torch stream
 or the raw ``stream`` given, as the calls in ``ops`` do: inputs that require a gradient are refused while one is
-recorded, and what a call overwrites counts as modified.
+recorded, and what a call overwrites counts as modified.  An input or a workspace that shares memory with what a
+call overwrites is refused.
 """
 from __future__ import annotations
 
@@ -249,7 +250,7 @@ def embedding_forward(table, ids, scale: float = 1.0, padding_id: int | None = N
 def embedding_backward(dy, ids, vocab: int, scale: float = 1.0, padding_id: int | None = None, into=None, dtype=None, workspace=None,
                        stream=None):
     """The gradient [vocab, n] of ``embedding_forward``'s table for dy [t, n]: scale times the sum of each token's rows, in 32 bits and
-    a fixed order.  Tokens equal to padding_id or outside [0, vocab) add nothing.  It is of dy's type, or float32 with ``dtype``; with
+    a fixed order.  Tokens equal to padding_id or outside [0, vocab) add nothing; rows without a token are 0.  It is of dy's type, or float32 with ``dtype``; with
     ``into`` (either type, rows may be strided) it is added to that, which is returned."""
     import torch
     load_ops()

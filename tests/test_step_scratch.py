@@ -4,8 +4,8 @@ import re
 from test_ops_kernels import resources
 
 # Bytes a thread of k_norm_back, by element type (mangled), threads of a row, pieces a thread and whether there are biases.  128 registers
-# are all that 16 wavefronts a CU have: where a thread has more than a piece of a row, or rows share a wavefront and have no scalar
-# addresses, some of what it holds does not fit.  The others keep nothing.
+# are all that 16 wavefronts a CU have: with 16 or more elements of a row in a thread, with 1024 threads and biases, or where rows share a
+# wavefront and have no scalar addresses, some of what it holds does not fit.  The others keep nothing.
 BF, HF, FF = "DF16b", "DF16_", "f"
 KEPT = {(BF, 8, 1, 0): 20, (BF, 8, 1, 1): 52, (BF, 16, 1, 0): 12, (BF, 16, 1, 1): 44, (BF, 32, 1, 0): 24, (BF, 32, 1, 1): 56,
         (HF, 8, 1, 0): 12, (HF, 8, 1, 1): 28, (HF, 16, 1, 1): 24, (HF, 32, 1, 0): 12, (HF, 32, 1, 1): 40,
