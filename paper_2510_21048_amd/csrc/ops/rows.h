@@ -204,7 +204,7 @@ inline bool type_ok(int dtype) { return dtype >= XMEM_BF16 && dtype <= XMEM_F32;
 // Whether `bytes` of workspace have one in common with a matrix: they may lie between two of its rows.  Sizes and distances as the calls
 // take them pass 64 bits.
 inline bool shares(const void* workspace, size_t bytes, const void* x, int64_t rows, int64_t ld, int64_t width, int element) {
-  if (!x || rows <= 0 || !bytes) return false;
+  if (!x || rows <= 0 || width <= 0 || !bytes) return false;
   typedef __int128 Wide;
   const Wide ws = reinterpret_cast<uintptr_t>(workspace), at = reinterpret_cast<uintptr_t>(x), step = Wide(ld) * element, row = Wide(width) * element;
   if (ws + Wide(bytes) <= at || ws >= at + (rows - 1) * step + row) return false;

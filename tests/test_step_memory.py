@@ -161,6 +161,7 @@ extern "C" int check(uint64_t ws, uint64_t bytes, uint64_t x, int64_t rows, int6
     assert min(seen) > 1000
     # no workspace, no operand, and the largest sizes that a call takes
     assert not check(64, 0, 64, 1, 1, 1, 4) and not check(64, 8, 0, 1, 1, 1, 4)
+    assert not check(64, 64, 80, 1, 0, 0, 8) and not check(64, 64, 80, 0, 8, 8, 4)  # no tokens, wherever their pointer points
     most = (1 << 31) - 1, (1 << 40) - 1
     assert check((1 << 60) + (1 << 42), 8, 1 << 60, most[0], most[1], most[0], 4) and not check((1 << 60) - 8, 8, 1 << 60, most[0], most[1], most[0], 4)
     assert not check((1 << 60) + (1 << 41), 8, 1 << 60, most[0], most[1], most[0], 4)
